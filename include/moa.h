@@ -59,6 +59,7 @@ enum {
     MOA_DEV_EMPTY_KEYS = 4,   /* cross-attention over an empty memory (output row = 0)      */
     MOA_DEV_CACHE_FULL = 8,   /* kv append would pass P_cap (rows beyond it are dropped)    */
     MOA_DEV_BAD_MESSAGE = 16, /* a token id or tree position does not fit its message field */
+    MOA_DEV_BAD_PAGE = 32,    /* a page table names no page of the pool where a row is wanted */
 };
 
 #define MOA_MAX_TREE 256      /* a tree position fits one byte (client message format, Sec. 4.2) */
@@ -302,6 +303,62 @@ int32_t moa_topk_logprob(int32_t dtype, const void *logits, int32_t F, int32_t V
 int32_t moa_lm_head_workspace_bytes(int32_t V, size_t *bytes_host);
 int32_t moa_lm_head_argmax(int32_t dtype, const void *x, int32_t R, int32_t d, const void *w, int32_t V,
                            int32_t *tgt, float *best, void *ws, size_t ws_bytes, void *stream);
+
+/* A KV cache in pages, and decoding one token per sequence over it without a draft: what a server does for the requests it
+ * does not speculate on (Sec. 2.1, autoregressive decoding: one token per forward pass, keys and values of the tokens before
+ * it kept).  Slot s of sequence b is row s % page_size of page table[b][s / page_size]; slots 0 .. len[b]-1 hold tokens.  A
+ * cache [B, Hkv, P_cap, dh] as moa_tree_verify_attn and the others read it is one of these too: n_pages = B, page_size = P_cap,
+ * max_pages = 1, table[b] = b, len = prefix_len.
+ *   k, v  [n_pages, Hkv, page_size, dh] in `dtype` (keys as they are to be attended: rotated, if they are);
+ *   table [B, max_pages]: entries behind the last slot in use are not read.  Two sequences may share a page that neither
+ *         call below writes to: the append writes slots len[b] .., the eviction any slot below len[b];
+ *   len   [B], within the capacity cap = max_pages * page_size (clamped, MOA_DEV_BAD_LENGTH);
+ *   pos   [B, Hkv, cap] the position of the token in each slot and seen [B] the tokens ever appended (both or neither);
+ *   score [B, Hkv, cap] the attention weight each slot has received (or NULL).
+ * moa_kv_evict needs pos, seen and score.  All of it belongs to the caller and is only described here.  Limits: head_dim <= 256,
+ * cap <= 2^30, n_pages * Hkv * page_size < 2^31, B * Hkv <= 2^20, B * n_q_heads * ceil(cap / 128) <= 2^30.
+ *
+ * moa_kv_append puts rows into the cache (the append of moa_ca_kv_append for keys and values that are there already; with
+ *   path / n_path of moa_tree_accept it commits the accepted nodes of a verified tree, Alg. 1):
+ *   k_new, v_new [B, Hkv, M, dh] (M = 1: a decoded token; a prompt's rows; k_tree / v_tree of a tree of M nodes); sequence b gets
+ *   n = n_new[b] rows (NULL: M), row path[b][i] (NULL: i) to slot len[b] + i with position seen[b] + i and score 0; then len
+ *   and seen grow by n.  n_new outside [0, M] is clamped (MOA_DEV_BAD_LENGTH), a path entry too (MOA_DEV_BAD_PARENT); rows
+ *   beyond the capacity are dropped (MOA_DEV_CACHE_FULL); a row whose table entry is no page of the pool is not written but
+ *   counted (MOA_DEV_BAD_PAGE).  Entries of path from n on are not read.
+ * moa_decode_attn is the attention of one new token per sequence, whose own key and value are appended first:
+ *   q, out [B, H*dh] (H = n_q_heads); one softmax over the len[b] slots.  len[b] = 0: zeros and MOA_DEV_EMPTY_KEYS.  A slot whose
+ *   table entry is no page of the pool is left out (MOA_DEV_BAD_PAGE).  accumulate != 0: score[b][h][s] grows by the weight that
+ *   slot s received, summed over the query heads of KV head h.  Results do not depend on what else is on the GPU, but how a
+ *   sequence's keys are cut (and so the last bits) on the other sequences' lengths.
+ *   Workspace: moa_decode_attn_workspace_bytes (for this cache description; with accounts if it has any), 256-byte aligned.
+ * moa_kv_evict cuts every sequence of more than `budget` slots down to `budget`, for each KV head by itself.  Slots stay in this
+ *   order: tokens with pos >= seen[b] - recent (all alike), then by score, larger first (NaN last); equal ones by lower slot.  A token that
+ *   stays and lies in a slot >= budget moves, with its position and score, into a slot below whose token leaves, the first into the first
+ *   and so on; len[b] = budget.  The attention does not see the order of slots.  Note that len then is no longer the position
+ *   of the next token (seen is), which moa_tli_decoder_layer takes prefix_len for.
+ *   0 <= recent <= budget, 1 <= budget, else MOA_ERR_RANGE.  Workspace: moa_kv_evict_workspace_bytes, 256-byte aligned. */
+typedef struct {
+    int32_t dtype;                    /* MOA_F32 | MOA_BF16                                  */
+    int32_t n_kv_heads, head_dim;
+    int32_t B;                        /* sequences                                           */
+    int32_t n_pages, page_size;       /* pages of the pool, rows of a page                   */
+    int32_t max_pages;                /* row length of the table                             */
+    void *k, *v;
+    const int32_t *table;
+    int32_t *len;
+    int32_t *pos, *seen;              /* both or neither                                     */
+    float *score;                     /* may be NULL                                         */
+} moa_kv_cache_t;
+
+int32_t moa_kv_append(const moa_kv_cache_t *cache, const void *k_new, const void *v_new, int32_t M,
+                      const int32_t *path /*[B,M] or NULL*/, const int32_t *n_new /*[B] or NULL*/,
+                      int32_t *dev_status, void *stream);
+int32_t moa_decode_attn_workspace_bytes(const moa_kv_cache_t *cache, int32_t n_q_heads, size_t *bytes_host);
+int32_t moa_decode_attn(const moa_kv_cache_t *cache, int32_t n_q_heads, const void *q, void *out, int32_t accumulate,
+                        int32_t *dev_status, void *ws, size_t ws_bytes, void *stream);
+int32_t moa_kv_evict_workspace_bytes(const moa_kv_cache_t *cache, int32_t budget, size_t *bytes_host);
+int32_t moa_kv_evict(const moa_kv_cache_t *cache, int32_t budget, int32_t recent,
+                     int32_t *dev_status, void *ws, size_t ws_bytes, void *stream);
 
 /* Client-server messages (Sec. 4.2; appendix table of message lengths).
  * Client -> server: each node of the draft tree as 3 bytes of token id (little-endian) and 1 byte for

@@ -24,7 +24,7 @@ except ImportError as e:
 
 F32, BF16 = 0, 1
 MAX_TREE = 256
-DEV_BAD_PARENT, DEV_BAD_LENGTH, DEV_EMPTY_KEYS, DEV_CACHE_FULL, DEV_BAD_MESSAGE = 1, 2, 4, 8, 16
+DEV_BAD_PARENT, DEV_BAD_LENGTH, DEV_EMPTY_KEYS, DEV_CACHE_FULL, DEV_BAD_MESSAGE, DEV_BAD_PAGE = 1, 2, 4, 8, 16, 32
 _TORCH_DTYPE = {F32: torch.float32, BF16: torch.bfloat16}
 
 
@@ -76,7 +76,8 @@ _SYMBOLS = ["moa_status_str", "moa_last_error", "moa_workspace_bytes", "moa_tree
             "moa_lsa", "moa_ca_kv_append", "moa_cross_attn_draft", "moa_tree_verify_attn", "moa_draft_step",
             "moa_self_attn_draft", "moa_tli_workspace_bytes", "moa_tli_decoder_layer", "moa_tree_expand_level", "moa_tree_finalize", "moa_topk_logprob", "moa_topk_workspace_bytes", "moa_lm_head_workspace_bytes", "moa_lm_head_argmax", "moa_msg_pack_tree", "moa_msg_unpack_tree", "moa_msg_accept_bytes", "moa_msg_pack_accept",
             "moa_msg_unpack_accept", "moa_msg_gzip_bound", "moa_msg_gzip", "moa_msg_gunzip", "moa_linear_workspace_bytes", "moa_linear", "moa_fold_projection", "moa_lsa_packed_weight_bytes", "moa_lsa_pack_weights", "moa_lsa_packed", "moa_mlp_block_workspace_bytes", "moa_mlp_block", "moa_rmsnorm", "moa_profile_enable", "moa_profile_sample_every", "moa_profile_collect", "moa_profile_kernel_name", "moa_profile_site_name", "moa_probe_read", "moa_probe_mfma",
-            "moa_debug_force_attn_kernel", "moa_debug_force_lsa_kernel", "moa_tree_verify_attn_noalloc"]
+            "moa_debug_force_attn_kernel", "moa_debug_force_lsa_kernel", "moa_tree_verify_attn_noalloc",
+            "moa_kv_append", "moa_decode_attn_workspace_bytes", "moa_decode_attn", "moa_kv_evict_workspace_bytes", "moa_kv_evict"]
 
 _lib.moa_status_str.restype = C.c_char_p
 _lib.moa_status_str.argtypes = [C.c_int32]
@@ -450,6 +451,93 @@ def lm_head_argmax(x, w, tgt, ws, best=None, stream=None):
     _check(_lib.moa_lm_head_argmax(BF16 if x.dtype == torch.bfloat16 else F32, _dev(x, x.dtype, R * d, "x"), R, d,
                                    _dev(w, x.dtype, V * d, "w"), V, _dev(tgt, torch.int32, R, "tgt"),
                                    _dev(best, torch.float32, R, "best"), wsp, wsb, _stream(stream)))
+
+
+class _KvCache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_kv_heads", "head_dim", "B", "n_pages", "page_size", "max_pages")] + [
+        (n, C.c_void_p) for n in ("k", "v", "table", "len", "pos", "seen", "score")]
+
+
+_lib.moa_kv_append.argtypes = [C.POINTER(_KvCache), _vp, _vp, _i32, _vp, _vp, _vp, _vp]
+_lib.moa_decode_attn_workspace_bytes.argtypes = [C.POINTER(_KvCache), _i32, C.POINTER(_sz)]
+_lib.moa_decode_attn.argtypes = [C.POINTER(_KvCache), _i32, _vp, _vp, _i32, _vp, _vp, _sz, _vp]
+_lib.moa_kv_evict_workspace_bytes.argtypes = [C.POINTER(_KvCache), _i32, C.POINTER(_sz)]
+_lib.moa_kv_evict.argtypes = [C.POINTER(_KvCache), _i32, _i32, _vp, _vp, _sz, _vp]
+for _n in _SYMBOLS[-5:]:
+    getattr(_lib, _n).restype = C.c_int32
+
+
+class KVCache:
+    """moa_kv_cache_t: a KV cache in pages.  k, v [n_pages, Hkv, page_size, dh]; table [B, max_pages], len [B], optionally pos
+    [B, Hkv, max_pages * page_size] with seen [B], score [B, Hkv, max_pages * page_size] (fp32; all others int32).  The tensors
+    are checked here, once, and kept alive; their contents belong to the caller.  A contiguous cache [B, Hkv, P_cap, dh] is
+    KVCache(k, v, torch.arange(B)[:, None], prefix_len)."""
+
+    def __init__(self, k, v, table, len, pos=None, seen=None, score=None):
+        n_pages, Hkv, page_size, dh = k.shape
+        B, max_pages = table.shape
+        if v.shape != k.shape:
+            raise ValueError("k and v: must have the same shape")
+        if k.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"k: dtype {k.dtype}, expected float32 or bfloat16")
+        i32, slots = torch.int32, B * Hkv * max_pages * page_size
+        for t in (v, table, len, pos, seen, score):
+            if t is not None and t.device != k.device:
+                raise ValueError("the cache's tensors must be on one device")
+        self._c = _KvCache(F32 if k.dtype == torch.float32 else BF16, Hkv, dh, B, n_pages, page_size, max_pages,
+                           _dev(k, k.dtype, 0, "k"), _dev(v, k.dtype, 0, "v"), _dev(table, i32, 0, "table"), _dev(len, i32, B, "len"),
+                           _dev(pos, i32, slots, "pos"), _dev(seen, i32, B, "seen"), _dev(score, torch.float32, slots, "score"))
+        self._ref = C.byref(self._c)
+        self.k, self.v, self.table, self.len, self.pos, self.seen, self.score = k, v, table, len, pos, seen, score
+
+    def _tensor(self, t, numel, name, dtype=None):
+        if t is not None and t.device != self.k.device:
+            raise ValueError(f"{name}: must be on the cache's device")
+        return _dev(t, self.k.dtype if dtype is None else dtype, numel, name)
+
+
+def kv_append(cache: KVCache, k_new, v_new, path=None, n_new=None, dev_status=None, stream=None):
+    """Rows path[b][:n_new[b]] (without path the first n_new[b], without n_new all) of k_new / v_new [B, Hkv, M, dh] go into the
+    slots behind the cache's len[b]; len and seen grow."""
+    c, i32 = cache._c, torch.int32
+    if k_new.shape != v_new.shape or len(k_new.shape) != 4 or k_new.shape[:2] != (c.B, c.n_kv_heads) or k_new.shape[3] != c.head_dim:
+        raise ValueError("k_new and v_new: must be [B, Hkv, M, dh] of the cache")
+    M = k_new.shape[2]
+    n = c.B * c.n_kv_heads * M * c.head_dim
+    _check(_lib.moa_kv_append(cache._ref, cache._tensor(k_new, n, "k_new"), cache._tensor(v_new, n, "v_new"), M,
+                              cache._tensor(path, c.B * M, "path", i32), cache._tensor(n_new, c.B, "n_new", i32),
+                              cache._tensor(dev_status, 1, "dev_status", i32), _stream(stream)))
+
+
+def decode_attn_workspace_bytes(cache: KVCache, n_q_heads: int) -> int:
+    out = _sz(0)
+    _check(_lib.moa_decode_attn_workspace_bytes(cache._ref, int(n_q_heads), C.byref(out)))
+    return int(out.value)
+
+
+def decode_attn(cache: KVCache, q, out, ws, accumulate=False, dev_status=None, stream=None):
+    """Attention of one new token per sequence (q, out [B, H, dh]) over the cache; with accumulate the weights are added to its score."""
+    c = cache._c
+    if len(q.shape) != 3 or q.shape[0] != c.B or q.shape[2] != c.head_dim:
+        raise ValueError("q: must be [B, H, dh] of the cache")
+    H = q.shape[1]
+    n = c.B * H * c.head_dim
+    wsp, wsb = _ws(ws)
+    _check(_lib.moa_decode_attn(cache._ref, H, cache._tensor(q, n, "q"), cache._tensor(out, n, "out"), 1 if accumulate else 0,
+                                cache._tensor(dev_status, 1, "dev_status", torch.int32), wsp, wsb, _stream(stream)))
+
+
+def kv_evict_workspace_bytes(cache: KVCache, budget: int) -> int:
+    out = _sz(0)
+    _check(_lib.moa_kv_evict_workspace_bytes(cache._ref, int(budget), C.byref(out)))
+    return int(out.value)
+
+
+def kv_evict(cache: KVCache, budget: int, recent: int, ws, dev_status=None, stream=None):
+    """Sequences of more than `budget` slots are cut down to it: the `recent` newest tokens and those with the largest score stay."""
+    wsp, wsb = _ws(ws)
+    _check(_lib.moa_kv_evict(cache._ref, int(budget), int(recent), cache._tensor(dev_status, 1, "dev_status", torch.int32),
+                             wsp, wsb, _stream(stream)))
 
 
 def msg_pack_tree(tok, parent, msg, dev_status=None, stream=None):
