@@ -26,7 +26,7 @@ struct DecodeArgs {
     float scale;                  // log2(e) / sqrt(dh)
     float *part_o;                // [runs + B HB][HG][dh]
     float *part_ml;               // [runs + B HB][HG][2]
-    float *raw;                   // [B, H, cap] scores, where accounts are kept; else NULL
+    float *raw;                   // [B, Hkv, cap, G] scores, where accounts are kept; else NULL
 };
 
 __device__ __forceinline__ uint32_t wave_scan(uint32_t x, int lane)
@@ -48,8 +48,9 @@ struct TileList {
     {
         return b < a.c.B ? (uint32_t)(a.c.length(b, false) + TK - 1) / TK : 0u;
     }
-    __device__ __forceinline__ explicit TileList(const DecodeArgs &a)
+    __device__ __forceinline__ explicit TileList(const DecodeArgs &a) : total(0), per(0)
     {
+        if (a.runs == 0) return;
         const int lane = threadIdx.x & 63;
         uint32_t x = 0;
         for (int b = lane; b < a.c.B; b += 64) x += tiles(a, b);
@@ -80,12 +81,12 @@ struct TileList {
 };
 
 // ---------------------------------------------------------------- what either kernel does with a run's result
-// LDS: acc [WAVES][HG][dh], ml [WAVES][HG][2] hold each wavefront's part.
-template <typename T>
+// (DH: the head_dim, 0 where it is not known here.)  LDS: acc [HG][dh] of each wavefront, `stride` floats apart, and ml [WAVES][HG][2].
+template <typename T, int DH>
 __device__ __forceinline__ void finish(const DecodeArgs &a, int b, int hb, uint32_t t0, uint32_t nt, bool whole, int64_t slot, const float *acc,
-                                       const float *ml, float *fin)
+                                       int stride, const float *ml, float *fin)
 {
-    const int tid = threadIdx.x, dh = a.c.dh, h = hb / a.rtiles, rt = hb - h * a.rtiles;
+    const int tid = threadIdx.x, dh = DH ? DH : a.c.dh, h = hb / a.rtiles, rt = hb - h * a.rtiles;
     const int r0 = rt * a.HG, rows = min(a.HG, a.G - r0);
     __syncthreads();
     if (tid < rows) {
@@ -109,7 +110,7 @@ __device__ __forceinline__ void finish(const DecodeArgs &a, int b, int hb, uint3
         const int r = i / dh, d = i - r * dh;
         float o = 0.f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) o += acc[(w * a.HG + r) * dh + d] * fast_exp2(ml[(w * a.HG + r) * 2] - fin[r * 2]);
+        for (int w = 0; w < WAVES; ++w) o += acc[w * stride + i] * fast_exp2(ml[(w * a.HG + r) * 2] - fin[r * 2]);
         o *= fin[r * 2 + 1];
         if (whole) st((T *)a.out + ((int64_t)b * a.H + h * a.G + r0 + r) * dh + d, o);
         else a.part_o[(slot * a.HG + r) * dh + d] = o;
@@ -119,7 +120,8 @@ __device__ __forceinline__ void finish(const DecodeArgs &a, int b, int hb, uint3
         const int n = min((int)((t0 + nt) * TK), a.c.length(b, false));
         for (int s = (int)t0 * TK + tid; s < n; s += 64 * WAVES) {
             float p = 0.f;
-            for (int r = 0; r < rows; ++r) p += fast_exp2(a.raw[((int64_t)b * a.H + h * a.G + r) * a.c.cap + s] - fin[r * 2]) * fin[r * 2 + 1];
+            const float *raw = a.raw + (((int64_t)b * a.c.Hkv + h) * a.c.cap + s) * a.G;
+            for (int r = 0; r < rows; ++r) p += fast_exp2(raw[r] - fin[r * 2]) * fin[r * 2 + 1];
             a.c.score[((int64_t)b * a.c.Hkv + h) * a.c.cap + s] += p;
         }
     }
@@ -130,23 +132,32 @@ __device__ __forceinline__ void finish(const DecodeArgs &a, int b, int hb, uint3
 template <typename F>
 __device__ __forceinline__ void for_each_pair(const DecodeArgs &a, const F &process)
 {
-    if (a.runs == 0) {
-        const int b = (int)blockIdx.x / a.HB, hb = (int)blockIdx.x - b * a.HB;
-        process(b, hb, 0u, (uint32_t)(a.c.length(b, hb == 0 && threadIdx.x == 0) + TK - 1) / TK, true, (int64_t)0);
-        return;
-    }
-    const TileList list(a);
-    uint32_t f = blockIdx.x * list.per;
-    const uint32_t end = min(f + list.per, list.total);
-    if (f >= end) return;
     int b;
-    uint32_t begin, nt;
-    list.find(a, f, b, begin, nt);
+    uint32_t f, end, begin, nt, hb, t, cnt;
+    const bool one = a.runs == 0;
+    const TileList list(a);
+    if (one) {
+        b = (int)blockIdx.x / a.HB;
+        hb = blockIdx.x - (uint32_t)b * a.HB;
+        cnt = nt = uniform(list.tiles(a, b));
+        f = end = begin = t = 0;
+        if (hb == 0 && threadIdx.x == 0) (void)a.c.length(b, true);
+    } else {
+        f = blockIdx.x * list.per;
+        end = min(f + list.per, list.total);
+        if (f >= end) return;
+        list.find(a, f, b, begin, nt);
+    }
     for (;;) {
-        const uint32_t in = f - begin, hb = in / nt, t = in - hb * nt, cnt = min(nt - t, end - f);
+        if (!one) {
+            const uint32_t in = f - begin;
+            hb = in / nt;
+            t = in - hb * nt;
+            cnt = min(nt - t, end - f);
+        }
         process(b, (int)hb, t, cnt, cnt == nt, (int64_t)blockIdx.x + (int64_t)b * a.HB + hb);
         f += cnt;
-        if (f >= end) return;
+        if (one || f >= end) return;
         if (f == begin + nt * (uint32_t)a.HB) {
             begin = f;
             do {
@@ -175,8 +186,8 @@ template <typename T, int LPR, int HG>
 __global__ __launch_bounds__(256) void k_decode_attn(DecodeArgs a)
 {
     constexpr int VE = 16 / sizeof(T), KPW = 64 / LPR, U = 4;
-    extern __shared__ float smem[];
-    float *acc_s = smem, *ml_s = acc_s + WAVES * HG * a.c.dh, *fin = ml_s + WAVES * HG * 2;
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    float *acc_s = (float *)smem, *ml_s = acc_s + WAVES * HG * a.c.dh, *fin = ml_s + WAVES * HG * 2;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane % LPR, grp = lane / LPR, dh = a.c.dh;
     const int e0 = c * VE, ne = min(max(dh - e0, 0), VE);
     for_each_pair(a, [&](int b, int hb, uint32_t t0, uint32_t nt, bool whole, int64_t slot) {
@@ -230,7 +241,7 @@ __global__ __launch_bounds__(256) void k_decode_attn(DecodeArgs a)
                         d = sum_over_lanes<LPR>(d);
                         s[u][r] = row[u] >= 0 ? d : -INFINITY;
                         if (a.raw && c == 0 && slots[u] < len && r < rows)
-                            a.raw[((int64_t)b * a.H + h * a.G + r0 + r) * a.c.cap + slots[u]] = s[u][r];
+                            a.raw[(((int64_t)b * a.c.Hkv + h) * a.c.cap + slots[u]) * a.G + r0 + r] = s[u][r];
                     }
 #pragma unroll
                 for (int u = 0; u < U; ++u) load(a.c.v, row[u], x[u]);
@@ -275,7 +286,202 @@ __global__ __launch_bounds__(256) void k_decode_attn(DecodeArgs a)
                 ml_s[(wave * HG + r) * 2 + 1] = l[r];
             }
         }
-        finish<T>(a, b, hb, t0, nt, whole, slot, acc_s, ml_s, fin);
+        finish<T, 0>(a, b, hb, t0, nt, whole, slot, acc_s, HG * dh, ml_s, fin);
+    });
+}
+
+// ---------------------------------------------------------------- on the matrix cores: bf16, head_dim 64 or 128
+// 64 lanes x 16 (4) bytes, each from an address of its own, to 1 KB (256 bytes) of LDS at `lds`.  (As lds_dma16 in
+// moa_gemm_device.h, but a pool of pages takes 64-bit addresses; the s_nop stands between the write of m0 and its use.)
+__device__ __forceinline__ void lds_gather16(uint32_t lds, uint64_t at)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(at));
+}
+__device__ __forceinline__ void lds_gather4(uint32_t lds, uint64_t at)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(at));
+}
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// Sixteen query heads of a KV head are the columns of a tile: S^T = K Q^T, O^T += V^T P^T.  Every wavefront walks its own 32
+// keys of each tile of the run, with a ring of its own in LDS, so that there is no barrier before the run's end; what a tile
+// needs is loaded NST tiles ahead straight into LDS, its table entries another NST before that.
+template <int DH, bool ACC>
+__global__ __launch_bounds__(256, 1) void k_decode_attn_mfma(DecodeArgs a)
+{
+    constexpr int ROWB = DH * 2, PIECES = ROWB / 16, RPI = 64 / PIECES, NL = WK / RPI;   // bytes and 16-byte pieces of a row; rows of a load, loads of K (or V)
+    constexpr int NST = 256 / DH, NKS = DH / 32, NDB = DH / 16;
+    constexpr uint32_t HALFB = WK * ROWB, STAGEB = 2 * HALFB, IDB = 256, WAVEB = NST * (STAGEB + IDB) + 128;
+    constexpr int YOUNGER = (NST - 1) * (2 * NL + 1);            // loads issued behind those of the current tile
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    __shared__ float ml_s[WAVES * 16 * 2], fin[16 * 2];
+    const int tid = threadIdx.x, lane = tid & 63, n16 = lane & 15, quad = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // [stages: K rows, V rows][table entries][row numbers] of this wavefront.  Rows lie in LDS in the order in which the loads
+    // bring them: load j has the keys g (32 / RPI) + j of its lane groups g, so that a lane's keys are neighbours.
+    char *mine = smem + wave * WAVEB;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem + (uint32_t)wave * WAVEB;
+    const uint32_t rows0 = lds0 + NST * (STAGEB + IDB);
+    const int grp = lane / PIECES;
+    // A piece of row p lies at position piece ^ f(p): reads of K touch 16 rows of one column, the transposing reads of V four
+    // rows of 32 bytes.
+    auto swz = [](int p) { return DH == 128 ? 4 * (p & 3) + ((p >> 2) & 3) : (((p >> 1) & 3) << 1) | ((p >> 3) & 1); };
+
+    for_each_pair(a, [&](int b, int hb, uint32_t t0, uint32_t nt, bool whole, int64_t slot) {
+        const int h = hb / a.rtiles, r0 = (hb - h * a.rtiles) * 16, rows = min(16, a.G - r0);
+        const int len = a.c.length(b, hb == 0 && t0 == 0 && tid == 0);
+        const int cnt = (int)nt, key0 = (int)t0 * TK + wave * WK;
+        const bf16_t *qrow = (const bf16_t *)a.q + ((int64_t)b * a.H + h * a.G + r0 + min(n16, rows - 1)) * DH;
+        bf16x8 qf[NKS];
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) qf[ks] = *(const bf16x8 *)(qrow + 32 * ks + 8 * quad);
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) asm volatile("" : "+v"(qf[ks]));       // waited for here, not among the loads below
+        f32x4 acc[NDB];
+#pragma unroll
+        for (int d = 0; d < NDB; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+        float mref = -INFINITY, lsum = 0.f;                                     // reference of the exponent (log2 domain); this lane's part of the sum
+
+        const int32_t *table = a.c.table + (int64_t)b * a.c.max_pages;
+        // rows that do not count are read from the queries, where there are numbers
+        const uint64_t safe = (uint64_t)(uintptr_t)((const bf16_t *)a.q + ((int64_t)b * a.H + h * a.G + r0) * DH);
+        // table entries of the keys of tile i (lanes 32 .. 63 as lanes 0 .. 31)
+        auto fetch_ids = [&](int i) {
+            const int s = min(key0 + i * TK + (lane & 31), len - 1);
+            lds_gather4(lds0 + NST * STAGEB + (uint32_t)(i % NST) * IDB, (uint64_t)(uintptr_t)(table + a.c.page((uint32_t)s)));
+        };
+        // the loads of tile i, whose table entries are there; returns which of its keys count
+        auto fetch = [&](int i) -> uint32_t {
+            const int s = key0 + i * TK + (lane & 31);
+            const int id = *(const __attribute__((address_space(3))) int32_t *)(uintptr_t)(lds0 + NST * STAGEB + (uint32_t)(i % NST) * IDB + lane * 4);
+            const int pg = (int)a.c.page((uint32_t)s);
+            int row = -1;
+            if (s < len) {
+                if ((uint32_t)id < (uint32_t)a.c.n_pages) row = (id * a.c.Hkv + h) * (int)a.c.page.d + (s - pg * (int)a.c.page.d);
+                else a.c.flag(MOA_DEV_BAD_PAGE);
+            }
+            if (lane < 32) *(__attribute__((address_space(3))) int32_t *)(uintptr_t)(rows0 + lane * 4) = row;
+            const uint32_t ok = (uint32_t)__ballot(row >= 0);
+            u32x4 r[NL / 4];
+#pragma unroll
+            for (int j = 0; j < NL / 4; ++j) r[j] = *(const __attribute__((address_space(3))) u32x4 *)(uintptr_t)(rows0 + (grp * NL + 4 * j) * 4);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                  // nobody reads the place any more that is filled now
+            const uint32_t at = lds0 + (uint32_t)(i % NST) * STAGEB;
+#pragma unroll
+            for (int j = 0; j < NL; ++j) {
+                const uint32_t off = 16 * ((lane % PIECES) ^ swz(RPI * j + grp));
+                const uint32_t rj = r[j / 4][j % 4];
+                const bool in = (int)rj >= 0;
+                const uint64_t far = (uint64_t)rj * ROWB;
+                lds_gather16(at + j * 1024, (in ? (uint64_t)(uintptr_t)a.c.k + far : safe) + off);
+                lds_gather16(at + HALFB + j * 1024, (in ? (uint64_t)(uintptr_t)a.c.v + far : safe) + off);
+            }
+            return ok;
+        };
+        // key of the tile that score element e (row 16 (e >> 2) + 4 quad + (e & 3) in LDS) belongs to
+        auto key_of = [&](int e) {
+            const int p = 16 * (e >> 2) + 4 * quad + (e & 3);
+            return (p % RPI) * NL + p / RPI;
+        };
+        uint32_t ok[NST];
+        if (cnt > 0) {
+#pragma unroll
+            for (int i = 0; i < NST; ++i) fetch_ids(i);
+            wait_loads<0>();
+#pragma unroll
+            for (int i = 0; i < NST; ++i) {
+                ok[i] = i < cnt ? fetch(i) : 0u;
+                fetch_ids(i + NST);
+            }
+        }
+        for (int i0 = 0; i0 < cnt; i0 += NST)
+#pragma unroll
+            for (int st = 0; st < NST; ++st) {
+                const int i = i0 + st;
+                if (i >= cnt) break;
+                if (i + NST <= cnt) wait_loads<YOUNGER>();
+                else wait_loads<0>();
+                const uint32_t kb = lds0 + st * STAGEB, vb = kb + HALFB;
+                f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {
+                        const int p = 16 * hf + n16;
+                        const bf16x8 kf = *(const __attribute__((address_space(3))) bf16x8 *)(uintptr_t)(kb + p * ROWB + 16 * ((4 * ks + quad) ^ swz(p)));
+                        s[hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[ks], s[hf], 0, 0, 0);
+                    }
+                float x[8], tm = -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * a.scale;
+                if (ok[st] != 0xffffffffu) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (!(ok[st] >> key_of(e) & 1u)) x[e] = -INFINITY;
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) tm = fmaxf(tm, x[e]);
+                if (ACC && n16 < rows) {
+                    float *raw = a.raw + (((int64_t)b * a.c.Hkv + h) * a.c.cap + key0 + i * TK) * a.G + r0 + n16;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (key0 + i * TK + key_of(e) < len) raw[key_of(e) * a.G] = x[e];
+                }
+                if (__ballot(tm > mref)) {
+                    tm = fmaxf(tm, __shfl_xor(tm, 16));
+                    tm = fmaxf(tm, __shfl_xor(tm, 32));
+                    const float mnew = fmaxf(mref, tm), corr = mnew == -INFINITY ? 1.f : fast_exp2(mref - mnew);
+                    mref = mnew;
+                    lsum *= corr;
+#pragma unroll
+                    for (int d = 0; d < NDB; ++d)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[d][e] *= corr;
+                }
+                const float ms = mref == -INFINITY ? 0.f : mref;
+                // A weight as the sum of two bf16 numbers, so that it counts with 2^-16 like in single precision: the matrix
+                // cores have nothing else to do, and one bf16 alone (2^-8) would double the result's own rounding.
+                union { uint32_t w[4]; bf16x8 v; } hi, lo;
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float p0 = fast_exp2(x[e] - ms), p1 = fast_exp2(x[e + 1] - ms);
+                    lsum += p0 + p1;
+                    hi.w[e / 2] = pack_bf16x2(p0, p1);
+                    lo.w[e / 2] = pack_bf16x2(p0 - __uint_as_float(hi.w[e / 2] << 16), p1 - __uint_as_float(hi.w[e / 2] & 0xffff0000u));
+                }
+#pragma unroll
+                for (int d = 0; d < NDB; ++d) {
+                    // transposing read: lane j of a group of 16 addresses key j >> 2 and dims 4 (j & 3) .. of the group's 16
+                    union { i16x4 h[2]; bf16x8 v; } u;
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {
+                        const int p = 16 * hf + 4 * quad + (n16 >> 2);
+                        u.h[hf] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(uintptr_t)(
+                            vb + p * ROWB + 16 * ((2 * d + ((n16 & 3) >> 1)) ^ swz(p)) + 8 * (n16 & 1)));
+                    }
+                    acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u.v, hi.v, acc[d], 0, 0, 0);
+                    acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u.v, lo.v, acc[d], 0, 0, 0);
+                }
+                if (i + NST < cnt) ok[st] = fetch(i + NST);
+                if (i + NST < cnt) fetch_ids(i + 2 * NST);
+            }
+        wait_loads<0>();
+        lsum += __shfl_xor(lsum, 16);
+        lsum += __shfl_xor(lsum, 32);
+        float *acc_s = (float *)mine;                              // the ring is free again
+        if (n16 < rows) {
+#pragma unroll
+            for (int d = 0; d < NDB; ++d) *(f32x4 *)(acc_s + n16 * DH + 16 * d + 4 * quad) = acc[d];
+            if (quad == 0) {
+                ml_s[(wave * a.HG + n16) * 2] = mref;
+                ml_s[(wave * a.HG + n16) * 2 + 1] = lsum;
+            }
+        }
+        finish<bf16_t, DH>(a, b, hb, t0, nt, whole, slot, (const float *)smem, WAVEB / 4, ml_s, fin);
     });
 }
 
@@ -361,7 +567,7 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
                 const int s = chunk * ACC_SLOTS + i * 256 + tid;
                 if (s < len)
                     for (int r = 0; r < rows; ++r)
-                        accs[i] += fast_exp2(a.raw[((int64_t)b * a.H + h * a.G + r0 + r) * a.c.cap + s] - fin[r][0]) * fin[r][1];
+                        accs[i] += fast_exp2(a.raw[(((int64_t)b * a.c.Hkv + h) * a.c.cap + s) * a.G + r0 + r] - fin[r][0]) * fin[r][1];
             }
         }
     }
@@ -377,6 +583,7 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
 
 // ---------------------------------------------------------------- host
 struct DecodePlan {
+    bool mfma;
     int HG, rtiles, runs;
     size_t part_o, part_ml, raw;       // bytes
     size_t total() const { return part_o + part_ml + raw; }
@@ -384,11 +591,18 @@ struct DecodePlan {
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-DecodePlan decode_plan(const moa_kv_cache_t &c, int H, bool accounts)
+// whether the matrix cores' form takes such a cache (and queries q, which it also reads 16 bytes at a time)
+bool takes_mfma(const moa_kv_cache_t &c, const void *q)
+{
+    return c.dtype == MOA_BF16 && (c.head_dim == 64 || c.head_dim == 128) && kv_rows16(c, {q});
+}
+
+DecodePlan decode_plan(const moa_kv_cache_t &c, int H, bool accounts, bool mfma)
 {
     DecodePlan p;
     const int G = H / c.n_kv_heads, cap = c.max_pages * c.page_size;
-    p.HG = G <= 2 ? 2 : 8;
+    p.mfma = mfma;
+    p.HG = p.mfma ? (G < 16 ? G : 16) : G <= 2 ? 2 : 8;
     p.rtiles = (G + p.HG - 1) / p.HG;
     const int64_t pairs = (int64_t)c.B * c.n_kv_heads * p.rtiles;
     // one workgroup per pair where that is a short walk, without a second launch; else four workgroups per compute unit
@@ -409,13 +623,29 @@ hipError_t launch_one(const DecodeArgs &a, int grid, hipStream_t st)
     return hipGetLastError();
 }
 
+template <int DH, bool ACC>
+hipError_t launch_mfma(const DecodeArgs &a, int grid, hipStream_t st)
+{
+    constexpr size_t lds = (size_t)WAVES * (256 / DH * (2 * WK * DH * 2 + 256) + 128);
+    static bool raised[16] = {};
+    hipError_t e = raise_lds_limit_once(raised, (const void *)k_decode_attn_mfma<DH, ACC>, lds);
+    if (e != hipSuccess) return e;
+    prof_begin(K_DECODE_ATTN_MFMA, st);
+    MOA_KLAUNCH((k_decode_attn_mfma<DH, ACC>), dim3(grid), dim3(64 * WAVES), lds, st, a);
+    prof_end(st);
+    return hipGetLastError();
+}
+
 template <typename T>
-hipError_t launch_decode(const DecodeArgs &a, hipStream_t st)
+hipError_t launch_decode(const DecodeArgs &a, bool mfma, hipStream_t st)
 {
     const int grid = a.runs ? a.runs : a.c.B * a.HB;
     constexpr int VE = 16 / sizeof(T), L1 = 64 / VE;
     hipError_t e;
-    if (a.HG == 2) e = a.c.dh <= 64 ? launch_one<T, L1, 2>(a, grid, st) : a.c.dh <= 128 ? launch_one<T, 2 * L1, 2>(a, grid, st) : launch_one<T, 4 * L1, 2>(a, grid, st);
+    if (mfma) {
+        if (a.c.dh == 128) e = a.raw ? launch_mfma<128, true>(a, grid, st) : launch_mfma<128, false>(a, grid, st);
+        else e = a.raw ? launch_mfma<64, true>(a, grid, st) : launch_mfma<64, false>(a, grid, st);
+    } else if (a.HG == 2) e = a.c.dh <= 64 ? launch_one<T, L1, 2>(a, grid, st) : a.c.dh <= 128 ? launch_one<T, 2 * L1, 2>(a, grid, st) : launch_one<T, 4 * L1, 2>(a, grid, st);
     else e = a.c.dh <= 64 ? launch_one<T, L1, 8>(a, grid, st) : a.c.dh <= 128 ? launch_one<T, 2 * L1, 8>(a, grid, st) : launch_one<T, 4 * L1, 8>(a, grid, st);
     if (e != hipSuccess || !a.runs) return e;
     const int64_t chunks = (a.c.cap + ACC_SLOTS - 1) / ACC_SLOTS;
@@ -450,8 +680,12 @@ int32_t moa_decode_attn_workspace_bytes(const moa_kv_cache_t *cache, int32_t n_q
     if (!bytes_host) return api_fail(MOA_ERR_NULL, "decode_attn_workspace_bytes: bytes_host is NULL");
     int32_t rc = check_decode(cache, n_q_heads, "decode_attn_workspace_bytes");
     if (rc) return rc;
-    const size_t without = decode_plan(*cache, n_q_heads, false).total(), with = cache->score ? decode_plan(*cache, n_q_heads, true).total() : 0;
-    *bytes_host = with > without ? with : without;
+    *bytes_host = 0;
+    for (const bool mfma : {false, takes_mfma(*cache, nullptr)})
+        for (const bool accounts : {false, cache->score != nullptr}) {
+            const size_t n = decode_plan(*cache, n_q_heads, accounts, mfma).total();
+            if (n > *bytes_host) *bytes_host = n;
+        }
     return MOA_OK;
 }
 
@@ -464,7 +698,7 @@ int32_t moa_decode_attn(const moa_kv_cache_t *cache, int32_t n_q_heads, const vo
     if (accumulate && !cache->score) return api_fail(MOA_ERR_NULL, "decode_attn: the cache keeps no accounts (score)");
     const size_t es = kv_esize(*cache);
     if (((uintptr_t)q | (uintptr_t)out) & (es - 1)) return api_fail(MOA_ERR_SHAPE, "decode_attn: q / out not aligned to their elements");
-    const DecodePlan p = decode_plan(*cache, n_q_heads, accumulate != 0);
+    const DecodePlan p = decode_plan(*cache, n_q_heads, accumulate != 0, takes_mfma(*cache, q));
     if (p.total() && (!ws || (((uintptr_t)ws) & 255) || ws_bytes < p.total()))
         return api_fail(MOA_ERR_WORKSPACE, "decode_attn: workspace NULL, misaligned or smaller than moa_decode_attn_workspace_bytes");
     DecodeArgs a = {KvDev(*cache, dev_status), q, out, n_q_heads, n_q_heads / cache->n_kv_heads, p.HG, p.rtiles, cache->n_kv_heads * p.rtiles,
@@ -472,7 +706,7 @@ int32_t moa_decode_attn(const moa_kv_cache_t *cache, int32_t n_q_heads, const vo
                     (float *)ws, (float *)((char *)ws + p.part_o), p.raw ? (float *)((char *)ws + p.part_o + p.part_ml) : nullptr};
     prof_set_site(S_DECODE);
     hipStream_t st = (hipStream_t)stream;
-    const hipError_t e = es == 2 ? launch_decode<bf16_t>(a, st) : launch_decode<float>(a, st);
+    const hipError_t e = es == 2 ? launch_decode<bf16_t>(a, p.mfma, st) : launch_decode<float>(a, false, st);
     if (e != hipSuccess) return api_fail(MOA_ERR_HIP, hipGetErrorString(e));
     return MOA_OK;
 }
