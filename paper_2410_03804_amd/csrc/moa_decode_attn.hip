@@ -48,6 +48,13 @@ struct TileList {
     {
         return b < a.c.B ? (uint32_t)(a.c.length(b, false) + TK - 1) / TK : 0u;
     }
+    __device__ __forceinline__ TileList() : total(0), per(0) {}
+    __device__ __forceinline__ void set(const DecodeArgs &a, uint32_t all)       // all: tiles of the sequences, for one KV head
+    {
+        total = all * (uint32_t)a.HB;
+        const uint32_t even = (total + a.runs - 1) / a.runs;
+        per = even > (uint32_t)a.min_run ? even : (uint32_t)a.min_run;
+    }
     __device__ __forceinline__ explicit TileList(const DecodeArgs &a) : total(0), per(0)
     {
         if (a.runs == 0) return;
@@ -56,9 +63,7 @@ struct TileList {
         for (int b = lane; b < a.c.B; b += 64) x += tiles(a, b);
 #pragma unroll
         for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
-        total = uniform(x) * (uint32_t)a.HB;
-        const uint32_t even = (total + a.runs - 1) / a.runs;
-        per = even > (uint32_t)a.min_run ? even : (uint32_t)a.min_run;
+        set(a, uniform(x));
     }
     // the sequence of tile f < total and its first tile
     __device__ __forceinline__ void find(const DecodeArgs &a, uint32_t f, int &b, uint32_t &begin, uint32_t &nt) const
@@ -486,98 +491,133 @@ __global__ __launch_bounds__(256, 1) void k_decode_attn_mfma(DecodeArgs a)
 }
 
 // ---------------------------------------------------------------- the second launch
-// Workgroups 0 .. B HB - 1 join the partial results of a pair; the others bring the accounts of 1024 slots of a (sequence, KV
-// head) up to date from its scores, now that the sums are known.  Either leaves alone what the first launch finished.
+// Workgroups 0 .. B H - 1 join the partial results of one query head; the others bring the accounts of 1024 slots of a (sequence,
+// KV head) up to date from its scores, now that the sums are known.  Either leaves alone what the first launch finished.
 constexpr int ACC_SLOTS = 1024;
 template <typename T>
 __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
 {
     __shared__ float sm[2][16][16], fin[16][2];
-    const int tid = threadIdx.x, dh = a.c.dh;
-    const TileList list(a);
-    const int nb = a.c.B * a.HB;
+    __shared__ float part[WAVES][256];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, dh = a.c.dh;
+    const int nb = a.c.B * a.H;
     const bool accounts = (int)blockIdx.x >= nb;
-    int b, hb, chunk = 0;
+    int b, h, r = 0, chunk = 0;                              // r: query head within its KV head
     if (!accounts) {
-        b = (int)blockIdx.x / a.HB;
-        hb = (int)blockIdx.x - b * a.HB;
+        b = (int)blockIdx.x / a.H;
+        h = ((int)blockIdx.x - b * a.H) / a.G;
+        r = (int)blockIdx.x - b * a.H - h * a.G;
     } else {
         const int chunks = (a.c.cap + ACC_SLOTS - 1) / ACC_SLOTS, i = (int)blockIdx.x - nb, bh = i / chunks;
         chunk = i - bh * chunks;
         b = bh / a.c.Hkv;
-        hb = (bh - b * a.c.Hkv) * a.rtiles;
+        h = bh - b * a.c.Hkv;
     }
-    const int len = a.c.length(b, !accounts && hb == 0 && tid == 0);
-    const uint32_t nt = (uint32_t)(len + TK - 1) / TK;
-    uint32_t before = 0;
-    for (int i = tid & 63; i < b; i += 64) before += list.tiles(a, i);
+    uint32_t all = 0, before = 0;
+    TileList list;
+    for (int i = lane; i < a.c.B; i += 64) {
+        const uint32_t n = list.tiles(a, i);
+        all += n;
+        before += i < b ? n : 0u;
+    }
 #pragma unroll
-    for (int d = 32; d; d >>= 1) before += __shfl_xor(before, d);
-    const uint32_t begin = uniform(before) * (uint32_t)a.HB;
-    float accs[ACC_SLOTS / 256] = {0.f, 0.f, 0.f, 0.f};      // of this thread's slots, over the row tiles
-    for (int rt = 0; rt < (accounts ? a.rtiles : 1); ++rt, ++hb) {
-        const int h = hb / a.rtiles, r0 = (hb - h * a.rtiles) * a.HG, rows = min(a.HG, a.G - r0);
-        const uint32_t f0 = begin + (uint32_t)hb * nt;
-        const uint32_t w0 = f0 / list.per, w1 = nt ? (f0 + nt - 1) / list.per : w0;
-        if (!accounts && nt == 0) {
-            for (int i = tid; i < rows * dh; i += 256) st((T *)a.out + ((int64_t)b * a.H + h * a.G + r0) * dh + i, 0.f);
+    for (int d = 32; d; d >>= 1) {
+        all += __shfl_xor(all, d);
+        before += __shfl_xor(before, d);
+    }
+    list.set(a, uniform(all));
+    const int len = a.c.length(b, !accounts && h + r == 0 && tid == 0);
+    const uint32_t nt = (uint32_t)(len + TK - 1) / TK;
+    // the runs that tiles of row tile rt of this KV head are in, and the first's place among the partial results
+    auto runs_of = [&](int rt, uint32_t &w0, uint32_t &ns, int64_t &slot0) {
+        const uint32_t hb = (uint32_t)(h * a.rtiles + rt), f0 = uniform(before) * (uint32_t)a.HB + hb * nt;
+        w0 = f0 / list.per;
+        ns = nt ? (f0 + nt - 1) / list.per - w0 + 1 : 0;
+        slot0 = (int64_t)w0 + (int64_t)b * a.HB + hb;
+    };
+    uint32_t w0, ns;
+    int64_t slot0;
+    if (!accounts) {
+        const int rt = r / a.HG, rr = r - rt * a.HG;
+        runs_of(rt, w0, ns, slot0);
+        T *out = (T *)a.out + ((int64_t)b * a.H + h * a.G + r) * dh;
+        if (ns == 0) {
+            for (int d = tid; d < dh; d += 256) st(out + d, 0.f);
             if (tid == 0) a.c.flag(MOA_DEV_EMPTY_KEYS);
-            return;
         }
-        if (accounts && chunk * ACC_SLOTS >= len) return;
-        if (w0 == w1 && (!accounts || a.rtiles == 1)) return;        // the first launch had all of it
+        if (ns <= 1) return;
+        const float *ml = a.part_ml + (slot0 * a.HG + rr) * 2, *po = a.part_o + (slot0 * a.HG + rr) * dh;
+        const int64_t ml_step = (int64_t)a.HG * 2, po_step = (int64_t)a.HG * dh;
+        float m = -INFINITY, l = 0.f;
+        for (uint32_t s = lane; s < ns; s += 64) m = fmaxf(m, ml[s * ml_step]);
+#pragma unroll
+        for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+        const float ms = m == -INFINITY ? 0.f : m;
+        for (uint32_t s = lane; s < ns; s += 64) l += ml[s * ml_step + 1] * fast_exp2(ml[s * ml_step] - ms);
+#pragma unroll
+        for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
+        if (tid == 0 && l == 0.f) a.c.flag(MOA_DEV_EMPTY_KEYS);
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        // a wavefront adds up every fourth partial result
+        float o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (uint32_t s = wave; s < ns; s += WAVES) {
+            const float w = fast_exp2(ml[s * ml_step] - ms);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i * 64 + lane < dh) o[i] = fmaf(po[s * po_step + i * 64 + lane], w, o[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[wave][i * 64 + lane] = o[i];
+        __syncthreads();
+        if (tid < dh) st(out + tid, (part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid]) * inv);
+        return;
+    }
+    if (chunk * ACC_SLOTS >= len) return;
+    float accs[ACC_SLOTS / 256] = {0.f, 0.f, 0.f, 0.f};      // of this thread's slots, over the row tiles
+    for (int rt = 0; rt < a.rtiles; ++rt) {
+        const int r0 = rt * a.HG, rows = min(a.HG, a.G - r0);
+        runs_of(rt, w0, ns, slot0);
+        if (ns == 1 && a.rtiles == 1) return;                // the first launch had all of it
         // of each row the maximum and the sum: sixteen threads a row
-        const int64_t slot0 = (int64_t)w0 + (int64_t)b * a.HB + hb, ns = (int64_t)w1 - w0 + 1;
-        const int row = tid & 15, part = tid >> 4;
+        const int row = tid & 15, p = tid >> 4;
         float m = -INFINITY, l = 0.f;
         if (row < rows)
-            for (int64_t s = part; s < ns; s += 16) m = fmaxf(m, a.part_ml[((slot0 + s) * a.HG + row) * 2]);
+            for (uint32_t s = p; s < ns; s += 16) m = fmaxf(m, a.part_ml[((slot0 + s) * a.HG + row) * 2]);
         __syncthreads();
-        sm[0][row][part] = m;
+        sm[0][row][p] = m;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 16; ++i) m = fmaxf(m, sm[0][row][i]);
         const float ms = m == -INFINITY ? 0.f : m;
         if (row < rows)
-            for (int64_t s = part; s < ns; s += 16) {
+            for (uint32_t s = p; s < ns; s += 16) {
                 const float *ml = a.part_ml + ((slot0 + s) * a.HG + row) * 2;
                 l += ml[1] * fast_exp2(ml[0] - ms);
             }
-        sm[1][row][part] = l;
+        sm[1][row][p] = l;
         __syncthreads();
-        if (part == 0) {
+        if (p == 0) {
             l = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) l += sm[1][row][i];
             fin[row][0] = ms;
             fin[row][1] = l == 0.f ? 0.f : 1.f / l;
-            if (!accounts && row < rows && l == 0.f) a.c.flag(MOA_DEV_EMPTY_KEYS);
         }
         __syncthreads();
-        if (!accounts) {
-            for (int i = tid; i < rows * dh; i += 256) {
-                const int r = i / dh, d = i - r * dh;
-                float o = 0.f;
-                for (int64_t s = 0; s < ns; ++s) o += a.part_o[((slot0 + s) * a.HG + r) * dh + d] * fast_exp2(a.part_ml[((slot0 + s) * a.HG + r) * 2] - fin[r][0]);
-                st((T *)a.out + ((int64_t)b * a.H + h * a.G + r0 + r) * dh + d, o * fin[r][1]);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < ACC_SLOTS / 256; ++i) {
-                const int s = chunk * ACC_SLOTS + i * 256 + tid;
-                if (s < len)
-                    for (int r = 0; r < rows; ++r)
-                        accs[i] += fast_exp2(a.raw[(((int64_t)b * a.c.Hkv + h) * a.c.cap + s) * a.G + r0 + r] - fin[r][0]) * fin[r][1];
-            }
-        }
-    }
-    if (accounts) {
-        const int h = hb / a.rtiles - 1;                     // (the loop left hb one past the head's last row tile)
 #pragma unroll
         for (int i = 0; i < ACC_SLOTS / 256; ++i) {
             const int s = chunk * ACC_SLOTS + i * 256 + tid;
-            if (s < len) a.c.score[((int64_t)b * a.c.Hkv + h) * a.c.cap + s] += accs[i];
+            if (s < len) {
+                const float *raw = a.raw + (((int64_t)b * a.c.Hkv + h) * a.c.cap + s) * a.G + r0;
+                for (int q = 0; q < rows; ++q) accs[i] += fast_exp2(raw[q] - fin[q][0]) * fin[q][1];
+            }
         }
+    }
+#pragma unroll
+    for (int i = 0; i < ACC_SLOTS / 256; ++i) {
+        const int s = chunk * ACC_SLOTS + i * 256 + tid;
+        if (s < len) a.c.score[((int64_t)b * a.c.Hkv + h) * a.c.cap + s] += accs[i];
     }
 }
 
@@ -605,12 +645,26 @@ DecodePlan decode_plan(const moa_kv_cache_t &c, int H, bool accounts, bool mfma)
     p.HG = p.mfma ? (G < 16 ? G : 16) : G <= 2 ? 2 : 8;
     p.rtiles = (G + p.HG - 1) / p.HG;
     const int64_t pairs = (int64_t)c.B * c.n_kv_heads * p.rtiles;
-    // one workgroup per pair where that is a short walk, without a second launch; else four workgroups per compute unit
-    p.runs = cap <= 4 * TK && !(accounts && p.rtiles > 1) ? 0 : 1024;
+    // One workgroup per pair where that is a short walk, without a second launch.  Else a run per compute unit, of which one
+    // workgroup fills the LDS; shorter runs only start more often (8 x 32768 keys: 181 us with 256, 184 with 1024; 4 x 4097:
+    // 17.5 and 27.9).
+    p.runs = cap <= 512 && !(accounts && p.rtiles > 1) ? 0 : 256;
     p.part_o = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * c.head_dim * 4) : 0;
     p.part_ml = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * 2 * 4) : 0;
     p.raw = accounts ? align256((size_t)c.B * H * cap * 4) : 0;
     return p;
+}
+
+// enough for either form, and for accounts where the cache keeps them
+size_t workspace_bytes(const moa_kv_cache_t &c, int H)
+{
+    size_t most = 0;
+    for (const bool mfma : {false, takes_mfma(c, nullptr)})
+        for (const bool accounts : {false, c.score != nullptr}) {
+            const size_t n = decode_plan(c, H, accounts, mfma).total();
+            if (n > most) most = n;
+        }
+    return most;
 }
 
 template <typename T, int LPR, int HG>
@@ -650,7 +704,7 @@ hipError_t launch_decode(const DecodeArgs &a, bool mfma, hipStream_t st)
     if (e != hipSuccess || !a.runs) return e;
     const int64_t chunks = (a.c.cap + ACC_SLOTS - 1) / ACC_SLOTS;
     prof_begin(K_DECODE_JOIN, st);
-    MOA_KLAUNCH(k_decode_join<T>, dim3((unsigned)(a.c.B * a.HB + (a.raw ? a.c.B * a.c.Hkv * chunks : 0))), dim3(256), 0, st, a);
+    MOA_KLAUNCH(k_decode_join<T>, dim3((unsigned)(a.c.B * a.H + (a.raw ? a.c.B * a.c.Hkv * chunks : 0))), dim3(256), 0, st, a);
     prof_end(st);
     return hipGetLastError();
 }
@@ -680,12 +734,7 @@ int32_t moa_decode_attn_workspace_bytes(const moa_kv_cache_t *cache, int32_t n_q
     if (!bytes_host) return api_fail(MOA_ERR_NULL, "decode_attn_workspace_bytes: bytes_host is NULL");
     int32_t rc = check_decode(cache, n_q_heads, "decode_attn_workspace_bytes");
     if (rc) return rc;
-    *bytes_host = 0;
-    for (const bool mfma : {false, takes_mfma(*cache, nullptr)})
-        for (const bool accounts : {false, cache->score != nullptr}) {
-            const size_t n = decode_plan(*cache, n_q_heads, accounts, mfma).total();
-            if (n > *bytes_host) *bytes_host = n;
-        }
+    *bytes_host = workspace_bytes(*cache, n_q_heads);
     return MOA_OK;
 }
 
@@ -699,10 +748,11 @@ int32_t moa_decode_attn(const moa_kv_cache_t *cache, int32_t n_q_heads, const vo
     const size_t es = kv_esize(*cache);
     if (((uintptr_t)q | (uintptr_t)out) & (es - 1)) return api_fail(MOA_ERR_SHAPE, "decode_attn: q / out not aligned to their elements");
     const DecodePlan p = decode_plan(*cache, n_q_heads, accumulate != 0, takes_mfma(*cache, q));
-    if (p.total() && (!ws || (((uintptr_t)ws) & 255) || ws_bytes < p.total()))
+    const size_t need = workspace_bytes(*cache, n_q_heads);
+    if (need && (!ws || (((uintptr_t)ws) & 255) || ws_bytes < need))
         return api_fail(MOA_ERR_WORKSPACE, "decode_attn: workspace NULL, misaligned or smaller than moa_decode_attn_workspace_bytes");
     DecodeArgs a = {KvDev(*cache, dev_status), q, out, n_q_heads, n_q_heads / cache->n_kv_heads, p.HG, p.rtiles, cache->n_kv_heads * p.rtiles,
-                    p.runs, 2, kv_rows16(*cache, {}) ? 1 : 0, 1.4426950408889634f / sqrtf((float)cache->head_dim),
+                    p.runs, 1, kv_rows16(*cache, {}) ? 1 : 0, 1.4426950408889634f / sqrtf((float)cache->head_dim),
                     (float *)ws, (float *)((char *)ws + p.part_o), p.raw ? (float *)((char *)ws + p.part_o + p.part_ml) : nullptr};
     prof_set_site(S_DECODE);
     hipStream_t st = (hipStream_t)stream;

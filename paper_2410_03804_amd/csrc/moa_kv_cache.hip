@@ -36,7 +36,8 @@ struct AppendArgs {
     KvDev c;
     const char *k_new, *v_new;       // [B, Hkv, M, dh]
     const int32_t *path, *n_new;     // [B, M], [B]; may be NULL
-    int M, units;                    // units of T per row
+    int M;
+    FastDiv units;                   // units of T per row
 };
 
 // rows that sequence b gets: those asked for, within M and the room there is
@@ -54,19 +55,21 @@ __device__ __forceinline__ int append_count(const AppendArgs &a, int b, int held
     return n;
 }
 
-// One workgroup (LAST) or gridDim.x of them per sequence.  Only where it is one may it move the sequence's length on itself.
-template <typename T, bool LAST>
-__global__ __launch_bounds__(256) void k_kv_append(AppendArgs a)
+// ONE: a workgroup per sequence, which may then also move its length on.  Else gridDim.x of them per sequence and KV head.
+template <typename T, int THREADS, bool ONE>
+__global__ __launch_bounds__(THREADS) void k_kv_append(AppendArgs a)
 {
-    const int b = blockIdx.y;
-    const bool first = blockIdx.x == 0 && threadIdx.x == 0;
+    const int b = blockIdx.z, units = (int)a.units.d;
+    const bool first = blockIdx.x + blockIdx.y == 0 && threadIdx.x == 0;
     const int held = a.c.length(b, first), n = append_count(a, b, held, first);
     const int seen = a.c.seen ? a.c.seen[b] : 0;
-    const int64_t work = (int64_t)n * a.c.Hkv * a.units;
-    for (int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x; w < work; w += (int64_t)gridDim.x * 256) {
-        const int u = (int)(w % a.units);
-        const int hi = (int)(w / a.units), h = hi % a.c.Hkv, i = hi / a.c.Hkv;
-        int src = i;
+    const int h0 = ONE ? 0 : blockIdx.y, h1 = ONE ? a.c.Hkv : h0 + 1;
+    // item: a unit of a row of K and the same of V; the rows of a head one after the other, as they come
+    const uint32_t per_head = (uint32_t)n * units, work = per_head * (uint32_t)(h1 - h0);
+    for (uint32_t w = blockIdx.x * THREADS + threadIdx.x; w < work; w += gridDim.x * THREADS) {
+        const uint32_t hh = ONE ? w / per_head : 0u, in = w - hh * per_head, i = a.units(in), u = in - i * units;
+        const int h = h0 + (int)hh;
+        int src = (int)i;
         if (a.path) {
             src = a.path[(int64_t)b * a.M + i];
             if ((uint32_t)src >= (uint32_t)a.M) {
@@ -74,19 +77,20 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a)
                 src = src < 0 ? 0 : a.M - 1;
             }
         }
-        const int row = a.c.row(b, h, held + i);
-        const int64_t from = (((int64_t)b * a.c.Hkv + h) * a.M + src) * a.units + u;
+        const int row = a.c.row(b, h, held + (int)i);
+        const int64_t from = (((int64_t)b * a.c.Hkv + h) * a.M + src) * units + u;
+        const T kx = ((const T *)a.k_new)[from], vx = ((const T *)a.v_new)[from];
         if (row >= 0) {
-            ((T *)a.c.k)[(int64_t)row * a.units + u] = ((const T *)a.k_new)[from];
-            ((T *)a.c.v)[(int64_t)row * a.units + u] = ((const T *)a.v_new)[from];
+            ((T *)a.c.k)[(int64_t)row * units + u] = kx;
+            ((T *)a.c.v)[(int64_t)row * units + u] = vx;
         } else a.c.flag(MOA_DEV_BAD_PAGE);
         if (u == 0) {
             const int64_t slot = ((int64_t)b * a.c.Hkv + h) * a.c.cap + held + i;
-            if (a.c.pos) a.c.pos[slot] = seen + i;
+            if (a.c.pos) a.c.pos[slot] = seen + (int)i;
             if (a.c.score) a.c.score[slot] = 0.f;
         }
     }
-    if (LAST) {
+    if (ONE) {
         __syncthreads();                     // every thread has read the length
         if (threadIdx.x == 0) {
             a.c.len[b] = held + n;
@@ -107,14 +111,17 @@ __global__ __launch_bounds__(256) void k_kv_append_len(AppendArgs a)
 template <typename T>
 hipError_t launch_append(const AppendArgs &a, hipStream_t st)
 {
-    const int64_t work = (int64_t)a.M * a.c.Hkv * a.units;
-    const bool one = work <= 8192;
-    const int64_t blocks = one ? 1 : (work + 1023) / 1024 < 1024 ? (work + 1023) / 1024 : 1024;
+    const int64_t per_head = (int64_t)a.M * a.units.d, work = per_head * a.c.Hkv;
     prof_begin(K_KV_APPEND, st);
-    if (one) MOA_KLAUNCH((k_kv_append<T, true>), dim3(1, a.c.B), dim3(256), 0, st, a);
-    else MOA_KLAUNCH((k_kv_append<T, false>), dim3((unsigned)blocks, a.c.B), dim3(256), 0, st, a);
+    // One workgroup per sequence saves the second launch; up to eight items a thread that is the shorter way.
+    if (work <= 1024) MOA_KLAUNCH((k_kv_append<T, 256, true>), dim3(1, 1, a.c.B), dim3(256), 0, st, a);
+    else if (work <= 8192) MOA_KLAUNCH((k_kv_append<T, 1024, true>), dim3(1, 1, a.c.B), dim3(1024), 0, st, a);
+    else {
+        const int64_t blocks = (per_head + 1023) / 1024;
+        MOA_KLAUNCH((k_kv_append<T, 256, false>), dim3((unsigned)(blocks < 1024 ? blocks : 1024), a.c.Hkv, a.c.B), dim3(256), 0, st, a);
+    }
     prof_end(st);
-    if (!one) {
+    if (work > 8192) {
         prof_begin(K_KV_APPEND_LEN, st);
         MOA_KLAUNCH(k_kv_append_len, dim3((a.c.B + 255) / 256), dim3(256), 0, st, a);
         prof_end(st);
@@ -123,15 +130,16 @@ hipError_t launch_append(const AppendArgs &a, hipStream_t st)
 }
 
 // ---------------------------------------------------------------- evict
-constexpr int EV_T = 1024, EV_W = EV_T / 64, EV_BITS = 11, EV_BINS = 1 << EV_BITS;
+constexpr int EV_T = 1024, EV_BITS = 11, EV_BINS = 1 << EV_BITS, EV_KEYS = 32768;
 
 struct EvictArgs {
     KvDev c;
     int budget, recent;
     int moves;                // room for moves per (sequence, KV head)
+    int keys;                 // that LDS holds: a multiple of 64 per wavefront
     int32_t *count;           // [B, Hkv]
     int32_t *dst, *src;       // [B, Hkv, moves]
-    int units;
+    FastDiv units;
 };
 
 // The order in which slots stay: the newest tokens' first, then by weight (ordered as its float is; NaN last).
@@ -143,132 +151,222 @@ __device__ __forceinline__ uint32_t stay_key(float w, bool newest)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// inclusive sums over the workgroup's threads; s: EV_W words of LDS
-__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t *s)
+// inclusive sums over the wavefront's lanes by moves inside the vector unit: within rows of 16, then across them
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_from(uint32_t x)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
-    __syncthreads();
-    if (lane == 63) s[wave] = x;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) x += s[w];
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x)
+{
+    x += dpp_from<0x111, 0xf>(x);     // row_shr 1, 2, 4, 8: from the lane so many below, 0 where there is none
+    x += dpp_from<0x112, 0xf>(x);
+    x += dpp_from<0x114, 0xf>(x);
+    x += dpp_from<0x118, 0xf>(x);
+    x += dpp_from<0x142, 0xa>(x);     // row_bcast 15: lane 15 of the row before, to rows 1 and 3
+    x += dpp_from<0x143, 0xc>(x);     // row_bcast 31: lane 31, to rows 2 and 3
     return x;
 }
 
-// One workgroup per (sequence, KV head).  The key of the last slot that stays is found digit by digit from histograms (11, 11
-// and 10 bits); slots with a larger key stay, and of those with an equal one the lowest.  Each wavefront then lists what its
-// stretch of slots frees below the budget and what stays beyond it; the i-th of either are one move.
+// the sum of s[0 .. n): n <= 16
+__device__ __forceinline__ uint32_t sum_before(const uint32_t *s, int n)
+{
+    uint32_t x = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) x += w < n ? s[w] : 0u;
+    return x;
+}
+
+__device__ __forceinline__ uint32_t lanes_below(uint64_t mask)
+{
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
+}
+
+// One workgroup per (sequence, KV head).  Every wavefront has a stretch of the slots, whose keys it keeps in LDS (where there are
+// more than that holds, those behind are read again whenever they are wanted).  The key of the last slot that stays is found
+// digit by digit from histograms (11, 11 and 10 bits; the newest, whose key is the largest there is, are only counted); slots
+// with a larger key stay, and of those with an equal one the lowest, which only matters in the one wavefront where the equal
+// ones that stay end.  Each wavefront then lists what its stretch frees below the budget and what stays beyond it; the i-th of
+// either are one move.
 __global__ __launch_bounds__(EV_T) void k_kv_evict_select(EvictArgs a)
 {
+    constexpr int NW = EV_T / 64, U = 4, UL = 8;         // rounds of 64 slots at a time: from LDS, from memory
+    static_assert(NW == 16 && EV_BINS == 2 * EV_T, "sum_before; two digits a thread");
+    constexpr uint32_t NEWEST = 0xffffffffu;
     __shared__ uint32_t hist[EV_BINS];
-    __shared__ uint32_t sums[EV_W], chosen[2], per_wave[3][EV_W];
-    const int bh = blockIdx.x, b = bh / a.c.Hkv, h = bh - b * a.c.Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ uint32_t sums[NW], chosen[2], per_wave[3][NW];
+    extern __shared__ uint32_t keys[];         // a.keys of them
+    const int bh = blockIdx.x, b = bh / a.c.Hkv, h = bh - b * a.c.Hkv, tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = a.c.length(b, h == 0 && tid == 0);
     if (n <= a.budget) {
         if (tid == 0) a.count[bh] = 0;
         return;
     }
+    for (int i = tid; i < EV_BINS; i += EV_T) hist[i] = 0;
+    __syncthreads();
     const float *score = a.c.score + (int64_t)bh * a.c.cap;
     const int32_t *pos = a.c.pos + (int64_t)bh * a.c.cap;
     const int64_t oldest = (int64_t)a.c.seen[b] - a.recent;
-    auto key = [&](int s) { return stay_key(score[s], pos[s] >= oldest); };
-
-    uint32_t want = (uint32_t)a.budget, prefix = 0, known = 0;        // `want` slots are still to be found among keys that begin with prefix
+    const int seg = ((n + NW - 1) / NW + 63) / 64 * 64, s0 = wave * seg, s1 = min(s0 + seg, n), rounds = s1 > s0 ? (s1 - s0 + 63) / 64 : 0;
+    const int room = a.keys / NW, here = min(rounds, room / 64);
+    uint32_t *const mine = keys + wave * room;
+    auto tally = [&](uint32_t d) {
+        // sixty-four equal accounts would wait for each other at one address
+        const uint32_t d0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)d);
+        const uint64_t all = __ballot(true);
+        if (__ballot(d == d0) == all) {
+            if (lanes_below(all) == 0) atomicAdd(&hist[d0], (uint32_t)__popcll(all));
+        } else atomicAdd(&hist[d], 1u);
+    };
+    uint32_t newest = 0;
+#pragma unroll 1
+    for (int j = 0; j < rounds; j += UL) {
+        float w[UL];
+        int32_t p[UL];
 #pragma unroll
-    for (int pass = 0; pass < 3; ++pass) {
-        const int bits = pass == 2 ? 10 : EV_BITS, shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-        for (int i = tid; i < EV_BINS; i += EV_T) hist[i] = 0;
-        __syncthreads();
-        for (int s = tid; s < n; s += EV_T) {
-            const uint32_t x = key(s);
-            if ((x & known) == prefix) atomicAdd(&hist[(x >> shift) & ((1u << bits) - 1)], 1u);
+        for (int q = 0; q < UL; ++q) {
+            const int s = min(s0 + 64 * (j + q) + lane, s1 - 1);
+            w[q] = score[s];
+            p[q] = pos[s];
         }
-        __syncthreads();
-        // from the largest digit down; thread t has the two digits 2 t, 2 t + 1 from the top
-        const int hi = EV_BINS - 1 - 2 * tid;
-        const uint32_t c0 = hist[hi], c1 = hist[hi - 1];
-        const uint32_t upto = block_scan(c0 + c1, sums), before = upto - c0 - c1;
-        if (before < want && want <= upto) {
-            const bool second = want > before + c0;
-            chosen[0] = (uint32_t)(second ? hi - 1 : hi);
-            chosen[1] = want - before - (second ? c0 : 0u);
+#pragma unroll
+        for (int q = 0; q < UL; ++q) {
+            const bool in = s0 + 64 * (j + q) + lane < s1;
+            const uint32_t x = stay_key(w[q], p[q] >= oldest);
+            if (j + q < here) mine[64 * (j + q) + lane] = x;
+            newest += __popcll(__ballot(in && x == NEWEST));
+            if (in && x != NEWEST) tally(x >> 21);
         }
-        __syncthreads();
-        prefix |= chosen[0] << shift;
-        known |= ((1u << bits) - 1) << shift;
-        want = chosen[1];
-        __syncthreads();
     }
-    const uint32_t last = prefix, ties = want;          // of the slots whose key is `last` the lowest `ties` stay
-
-    const int seg = ((n + EV_W - 1) / EV_W + 63) / 64 * 64, s0 = wave * seg, s1 = min(s0 + seg, n);
-    const uint64_t below = lane ? ~0ull >> (64 - lane) : 0ull;
-    uint32_t eq = 0;
-    for (int s = s0; s < s1; s += 64) eq += __popcll(__ballot(s + lane < s1 && key(s + lane) == last));
-    if (lane == 0) per_wave[0][wave] = eq;
-    __syncthreads();
-    uint32_t eq0 = 0;
-    for (int w = 0; w < wave; ++w) eq0 += per_wave[0][w];
-    uint32_t holes = 0, movers = 0;
-    // out: NULL while counting
-    auto walk = [&](int32_t *dst, int32_t *src) {
-        uint32_t e = eq0;
-        holes = movers = 0;
-        for (int s = s0; s < s1; s += 64) {
-            const int slot = s + lane;
-            const bool in = slot < s1;
-            const uint32_t x = in ? key(slot) : 0u;
-            const uint64_t same = __ballot(in && x == last);
-            const bool stays = in && (x > last || (x == last && e + __popcll(same & below) < ties));
-            e += __popcll(same);
-            const bool hole = in && !stays && slot < a.budget, mover = stays && slot >= a.budget;
-            const uint64_t bh_ = __ballot(hole), bm = __ballot(mover);
-            if (dst) {
-                if (hole) dst[holes + __popcll(bh_ & below)] = slot;
-                if (mover) src[movers + __popcll(bm & below)] = slot;
+    // f(first slot, this lane's key, whether it has one) for every round of 64 slots
+    auto each = [&](auto f) {
+#pragma unroll 1
+        for (int j = 0; j < rounds; j += U) {
+            uint32_t x[U];
+#pragma unroll
+            for (int q = 0; q < U; ++q) {
+                const int s = s0 + 64 * (j + q) + lane;
+                x[q] = 0;
+                if (j + q < here) x[q] = mine[64 * (j + q) + lane];
+                else if (s < s1) x[q] = stay_key(score[s], pos[s] >= oldest);
             }
-            holes += __popcll(bh_);
-            movers += __popcll(bm);
+#pragma unroll
+            for (int q = 0; q < U; ++q) f(s0 + 64 * (j + q), x[q], s0 + 64 * (j + q) + lane < s1);
         }
     };
-    walk(nullptr, nullptr);
+
+    if (lane == 0) per_wave[0][wave] = newest;
+    __syncthreads();
+    newest = sum_before(per_wave[0], NW);
+    uint32_t last = NEWEST, ties = (uint32_t)a.budget;                // of the slots whose key is `last` the lowest `ties` stay
+    if (newest < ties) {
+        uint32_t want = ties - newest, prefix = 0;                    // `want` slots are still to be found among keys that begin with prefix
+        int shift = 21;
+#pragma unroll 1
+        for (;;) {
+            // from the largest digit down; thread t has the digits 2 t and 2 t + 1, counted from the top
+            const int top = EV_BINS - 1 - 2 * tid;
+            const uint32_t c0 = hist[top], c1 = hist[top - 1];
+            hist[top] = hist[top - 1] = 0;
+            uint32_t upto = wave_scan(c0 + c1);
+            if (lane == 63) sums[wave] = upto;
+            __syncthreads();
+            upto += sum_before(sums, wave);
+            const uint32_t before = upto - c0 - c1;
+            if (before < want && want <= upto) {
+                const bool second = want > before + c0;
+                chosen[0] = (uint32_t)(second ? top - 1 : top);
+                chosen[1] = want - before - (second ? c0 : 0u);
+            }
+            __syncthreads();
+            prefix |= chosen[0] << shift;
+            want = chosen[1];
+            if (shift == 0) break;
+            const int down = shift, bits = shift == 21 ? EV_BITS : 10;
+            shift -= bits;
+            each([&](int, uint32_t x, bool in) {
+                if (in && x != NEWEST && x >> down == prefix >> down) tally((x >> shift) & ((1u << bits) - 1));
+            });
+            __syncthreads();
+        }
+        last = prefix;
+        ties = want;
+    }
+
+    // of this stretch, below the budget (0) and beyond it (1): keys above the last one, and equal to it
+    uint32_t more[2] = {0, 0}, same[2] = {0, 0};
+    each([&](int s, uint32_t x, bool in) {
+        const bool low = s + lane < a.budget;
+        const uint64_t gt = __ballot(in && x > last), eq = __ballot(in && x == last), lows = __ballot(low);
+        more[0] += __popcll(gt & lows);
+        more[1] += __popcll(gt & ~lows);
+        same[0] += __popcll(eq & lows);
+        same[1] += __popcll(eq & ~lows);
+    });
+    if (lane == 0) per_wave[1][wave] = same[0] + same[1];
+    __syncthreads();
+    // those of the equal ones that stay are the stretch's first
+    const uint32_t eq0 = sum_before(per_wave[1], wave), left = eq0 < ties ? ties - eq0 : 0u;
+    const uint32_t stay_low = min(same[0], left), stay_high = min(same[1], left - stay_low);
+    const uint32_t holes = (uint32_t)max(min(s1, a.budget) - s0, 0) - more[0] - stay_low, movers = more[1] + stay_high;
     if (lane == 0) {
-        per_wave[1][wave] = holes;
+        per_wave[0][wave] = holes;
         per_wave[2][wave] = movers;
     }
     __syncthreads();
-    uint32_t h0 = 0, m0 = 0;
-    for (int w = 0; w < wave; ++w) {
-        h0 += per_wave[1][w];
-        m0 += per_wave[2][w];
-    }
-    const int64_t at = (int64_t)bh * a.moves;
-    walk(a.dst + at + h0, a.src + at + m0);
+    const uint32_t h0 = sum_before(per_wave[0], wave);
+    int32_t *dst = a.dst + (int64_t)bh * a.moves + h0, *src = a.src + (int64_t)bh * a.moves + sum_before(per_wave[2], wave);
+    uint32_t e = 0;
+    each([&](int s, uint32_t x, bool in) {
+        const bool low = s + lane < a.budget;
+        const uint64_t eq = __ballot(in && x == last);
+        const bool stays = in && (x > last || (x == last && e + lanes_below(eq) < left));
+        e += __popcll(eq);
+        const uint64_t hole = __ballot(in && low && !stays), mover = __ballot(!low && stays);
+        if (hole >> lane & 1) dst[lanes_below(hole)] = s + lane;
+        if (mover >> lane & 1) src[lanes_below(mover)] = s + lane;
+        dst += __popcll(hole);
+        src += __popcll(mover);
+    });
     if (tid == EV_T - 1) a.count[bh] = (int32_t)(h0 + holes);
 }
 
 template <typename T>
 __global__ __launch_bounds__(256) void k_kv_evict_move(EvictArgs a)
 {
-    const int bh = blockIdx.y, b = bh / a.c.Hkv, h = bh - b * a.c.Hkv;
+    constexpr int U = 4;                  // items in flight per thread
+    const int bh = blockIdx.y, b = bh / a.c.Hkv, h = bh - b * a.c.Hkv, units = (int)a.units.d;
     const int n = a.count[bh];
     const int64_t at = (int64_t)bh * a.moves, acc = (int64_t)bh * a.c.cap;
-    const int64_t work = (int64_t)n * a.units;
-    for (int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x; w < work; w += (int64_t)gridDim.x * 256) {
-        const int i = (int)(w / a.units), u = (int)(w - (int64_t)i * a.units);
-        const int d = a.dst[at + i], s = a.src[at + i], rd = a.c.row(b, h, d), rs = a.c.row(b, h, s);
-        if (rd >= 0 && rs >= 0) {
-            ((T *)a.c.k)[(int64_t)rd * a.units + u] = ((T *)a.c.k)[(int64_t)rs * a.units + u];
-            ((T *)a.c.v)[(int64_t)rd * a.units + u] = ((T *)a.c.v)[(int64_t)rs * a.units + u];
-        } else a.c.flag(MOA_DEV_BAD_PAGE);
-        if (u == 0) {
-            a.c.pos[acc + d] = a.c.pos[acc + s];
-            a.c.score[acc + d] = a.c.score[acc + s];
+    const uint32_t work = (uint32_t)n * units, step = gridDim.x * 256;
+    T *const k = (T *)a.c.k, *const v = (T *)a.c.v;
+    for (uint32_t w0 = blockIdx.x * 256 + threadIdx.x; w0 < work; w0 += U * step) {
+        int64_t to[U];
+        T kx[U], vx[U];
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+            const uint32_t w = w0 + q * step;
+            to[q] = -1;
+            if (w >= work) continue;
+            const uint32_t i = a.units(w), u = w - i * units;
+            const int d = a.dst[at + i], s = a.src[at + i], rd = a.c.row(b, h, d), rs = a.c.row(b, h, s);
+            if (rd >= 0 && rs >= 0) {
+                to[q] = (int64_t)rd * units + u;
+                kx[q] = k[(int64_t)rs * units + u];
+                vx[q] = v[(int64_t)rs * units + u];
+            } else a.c.flag(MOA_DEV_BAD_PAGE);
+            if (u == 0) {
+                a.c.pos[acc + d] = a.c.pos[acc + s];
+                a.c.score[acc + d] = a.c.score[acc + s];
+            }
         }
+#pragma unroll
+        for (int q = 0; q < U; ++q)
+            if (to[q] >= 0) {
+                k[to[q]] = kx[q];
+                v[to[q]] = vx[q];
+            }
     }
     // nobody in this launch reads the lengths
     if (h == 0 && blockIdx.x == 0 && threadIdx.x == 0 && a.c.len[b] > a.budget) a.c.len[b] = a.budget;
@@ -278,10 +376,13 @@ template <typename T>
 hipError_t launch_evict(const EvictArgs &a, hipStream_t st)
 {
     const int bh = a.c.B * a.c.Hkv;
+    static bool raised[16] = {};
+    hipError_t e = raise_lds_limit_once(raised, (const void *)k_kv_evict_select, EV_KEYS * 4);
+    if (e != hipSuccess) return e;
     prof_begin(K_KV_EVICT_SELECT, st);
-    MOA_KLAUNCH(k_kv_evict_select, dim3(bh), dim3(EV_T), 0, st, a);
+    MOA_KLAUNCH(k_kv_evict_select, dim3(bh), dim3(EV_T), (size_t)a.keys * 4, st, a);
     prof_end(st);
-    const int64_t work = (int64_t)a.moves * a.units, blocks = (work + 1023) / 1024;
+    const int64_t work = (int64_t)a.moves * a.units.d, blocks = (work + 1023) / 1024;
     prof_begin(K_KV_EVICT_MOVE, st);
     MOA_KLAUNCH(k_kv_evict_move<T>, dim3((unsigned)(blocks < 64 ? blocks : 64), bh), dim3(256), 0, st, a);
     prof_end(st);
@@ -308,13 +409,13 @@ int32_t moa_kv_append(const moa_kv_cache_t *cache, const void *k_new, const void
     if (rc) return rc;
     if (!k_new || !v_new) return api_fail(MOA_ERR_NULL, "kv_append: k_new / v_new is NULL");
     if (M < 1 || M > (1 << 24)) return api_fail(MOA_ERR_SHAPE, "kv_append: M outside [1, 2^24]");
-    if ((int64_t)cache->n_kv_heads * M > INT32_MAX) return api_fail(MOA_ERR_SHAPE, "kv_append: more than 2^31 - 1 rows per sequence");
-    if (cache->B > 65535) return api_fail(MOA_ERR_SHAPE, "kv_append: more than 65535 sequences");
+    if ((int64_t)cache->head_dim * M > INT32_MAX) return api_fail(MOA_ERR_SHAPE, "kv_append: M * head_dim above 2^31 - 1");
+    if (cache->B > 65535 || cache->n_kv_heads > 65535) return api_fail(MOA_ERR_SHAPE, "kv_append: more than 65535 sequences or KV heads");
     const size_t es = kv_esize(*cache);
     if (((uintptr_t)k_new | (uintptr_t)v_new) & (es - 1)) return api_fail(MOA_ERR_SHAPE, "kv_append: k_new / v_new not aligned to their elements");
     const bool wide = kv_rows16(*cache, {k_new, v_new});
     AppendArgs a = {KvDev(*cache, dev_status), (const char *)k_new, (const char *)v_new, path, n_new, M,
-                    (int)(wide ? cache->head_dim * es / 16 : cache->head_dim)};
+                    FastDiv((uint32_t)(wide ? cache->head_dim * es / 16 : cache->head_dim))};
     prof_set_site(S_KV_CACHE);
     hipStream_t st = (hipStream_t)stream;
     const hipError_t e = wide ? launch_append<u32x4>(a, st) : es == 2 ? launch_append<uint16_t>(a, st) : launch_append<uint32_t>(a, st);
@@ -343,6 +444,8 @@ int32_t moa_kv_evict(const moa_kv_cache_t *cache, int32_t budget, int32_t recent
     if (!cache->pos || !cache->score) return api_fail(MOA_ERR_NULL, "kv_evict: the cache keeps no positions (pos, seen) or no accounts (score)");
     if (budget < 1 || recent < 0 || recent > budget) return api_fail(MOA_ERR_RANGE, "kv_evict: 1 <= budget and 0 <= recent <= budget");
     if ((int64_t)cache->B * cache->n_kv_heads > 65535) return api_fail(MOA_ERR_SHAPE, "kv_evict: more than 65535 pairs of sequence and KV head");
+    if ((int64_t)evict_moves(*cache, budget) * cache->head_dim > (1 << 30))
+        return api_fail(MOA_ERR_SHAPE, "kv_evict: min(budget, capacity - budget) * head_dim above 2^30");
     (void)moa_kv_evict_workspace_bytes(cache, budget, &need);
     if (need == 0) return MOA_OK;                              // no sequence can hold more than the budget
     if (!ws || (((uintptr_t)ws) & 255) || ws_bytes < need)
@@ -351,9 +454,10 @@ int32_t moa_kv_evict(const moa_kv_cache_t *cache, int32_t budget, int32_t recent
     const bool wide = kv_rows16(*cache, {});
     const int64_t bh = (int64_t)cache->B * cache->n_kv_heads;
     const int moves = evict_moves(*cache, budget);
+    const int cap = cache->max_pages * cache->page_size, keys = cap < EV_KEYS ? (cap + EV_T - 1) / EV_T * EV_T : EV_KEYS;
     int32_t *w = (int32_t *)ws;
-    EvictArgs a = {KvDev(*cache, dev_status), budget, recent, moves, w, w + bh, w + bh + bh * moves,
-                   (int)(wide ? cache->head_dim * es / 16 : cache->head_dim)};
+    EvictArgs a = {KvDev(*cache, dev_status), budget, recent, moves, keys, w, w + bh, w + bh + bh * moves,
+                   FastDiv((uint32_t)(wide ? cache->head_dim * es / 16 : cache->head_dim))};
     prof_set_site(S_KV_CACHE);
     hipStream_t st = (hipStream_t)stream;
     const hipError_t e = wide ? launch_evict<u32x4>(a, st) : es == 2 ? launch_evict<uint16_t>(a, st) : launch_evict<uint32_t>(a, st);

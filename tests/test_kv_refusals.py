@@ -56,7 +56,7 @@ def test_every_call_refuses_such_a_cache(kw, status):
 
 def test_append_arguments():
     assert append(cache(), k=None) == NULL and append(cache(), v=None) == NULL
-    assert append(cache(), M=0) == SHAPE and append(cache(), M=(1 << 24) + 1) == SHAPE and append(cache(n_kv_heads=1024), M=1 << 24) == SHAPE
+    assert append(cache(), M=0) == SHAPE and append(cache(), M=(1 << 24) + 1) == SHAPE and append(cache(head_dim=256), M=1 << 24) == SHAPE
     assert append(cache(), k=FAKE + 1) == SHAPE
     assert append(cache(B=70000, n_kv_heads=1)) == SHAPE
 
