@@ -310,7 +310,7 @@ int32_t moa_lm_head_argmax(int32_t dtype, const void *x, int32_t R, int32_t d, c
  * cache [B, Hkv, P_cap, dh] as moa_tree_verify_attn and the others read it is one of these too: n_pages = B, page_size = P_cap,
  * max_pages = 1, table[b] = b, len = prefix_len.
  *   k, v  [n_pages, Hkv, page_size, dh] in `dtype` (keys as they are to be attended: rotated, if they are);
- *   table [B, max_pages]: entries behind the last slot in use are not read.  Two sequences may share a page that neither
+ *   table [B, max_pages]: what stands behind the last slot in use does not matter.  Two sequences may share a page that neither
  *         call below writes to: the append writes slots len[b] .., the eviction any slot below len[b];
  *   len   [B], within the capacity cap = max_pages * page_size (clamped, MOA_DEV_BAD_LENGTH);
  *   pos   [B, Hkv, cap] the position of the token in each slot and seen [B] the tokens ever appended (both or neither);

@@ -190,7 +190,8 @@ __device__ __forceinline__ float sum_over_lanes(float x)
 template <typename T, int LPR, int HG>
 __global__ __launch_bounds__(256) void k_decode_attn(DecodeArgs a)
 {
-    constexpr int VE = 16 / sizeof(T), KPW = 64 / LPR, U = 4;
+    constexpr int VE = 16 / sizeof(T), KPW = 64 / LPR, U = KPW < 8 ? 4 : 2;
+    static_assert(WK % (KPW * U) == 0, "rounds of a tile");
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     float *acc_s = (float *)smem, *ml_s = acc_s + WAVES * HG * a.c.dh, *fin = ml_s + WAVES * HG * 2;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane % LPR, grp = lane / LPR, dh = a.c.dh;
@@ -210,65 +211,73 @@ __global__ __launch_bounds__(256) void k_decode_attn(DecodeArgs a)
             m[r] = -INFINITY;
             l[r] = 0.f;
         }
-        auto load = [&](const char *pool, int row, float (&x)[VE]) {
+        auto load = [&](const char *pool, int row, u32x4 &x) {
             const T *p = (const T *)pool + (int64_t)row * dh + e0;
-            union { u32x4 v; T t[VE]; } u;
-            u.v = u32x4{0u, 0u, 0u, 0u};
+            x = u32x4{0u, 0u, 0u, 0u};
             if (row >= 0 && ne > 0) {
-                if (a.wide) u.v = *(const u32x4 *)p;
-                else
-                    for (int e = 0; e < ne; ++e) u.t[e] = p[e];
+                if (a.wide) x = *(const u32x4 *)p;
+                else {
+                    union { u32x4 v; T t[VE]; } u;
+                    u.v = x;
+#pragma unroll
+                    for (int e = 0; e < VE; ++e)
+                        if (e < ne) u.t[e] = p[e];
+                    x = u.v;
+                }
+            }
+        };
+        auto value = [](const u32x4 &x, int e) {
+            return sizeof(T) == 4 ? __uint_as_float(x[e]) : __uint_as_float(e & 1 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16);
+        };
+#pragma unroll 1
+        for (uint32_t t = t0 * (WK / (KPW * U)); t < (t0 + nt) * (WK / (KPW * U)); ++t) {
+            const int base = (int)(t / (WK / (KPW * U))) * TK + wave * WK + (int)(t % (WK / (KPW * U))) * KPW * U + grp;
+            int slots[U], row[U];
+            u32x4 k[U], v[U];
+            float s[U][HG];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                // (the table is read for any slot: what is there only counts for those in use)
+                slots[u] = base + u * KPW;
+                row[u] = a.c.row(b, h, min(slots[u], a.c.cap - 1));
+                if (slots[u] >= len) row[u] = -1;
+                else if (row[u] < 0) a.c.flag(MOA_DEV_BAD_PAGE);
             }
 #pragma unroll
-            for (int e = 0; e < VE; ++e) x[e] = ld(&u.t[e]);
-        };
-        for (uint32_t t = t0; t < t0 + nt; ++t)
-            for (int s0 = 0; s0 < WK; s0 += KPW * U) {
-                int slots[U], row[U];
-                float x[U][VE], s[U][HG];
+            for (int u = 0; u < U; ++u) load(a.c.k, row[u], k[u]);
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    slots[u] = (int)t * TK + wave * WK + s0 + u * KPW + grp;
-                    row[u] = -1;
-                    if (slots[u] < len) {
-                        row[u] = a.c.row(b, h, slots[u]);
-                        if (row[u] < 0) a.c.flag(MOA_DEV_BAD_PAGE);
-                    }
-                    load(a.c.k, row[u], x[u]);
-                }
+            for (int u = 0; u < U; ++u) load(a.c.v, row[u], v[u]);
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int r = 0; r < HG; ++r) {
-                        float d = 0.f;
-#pragma unroll
-                        for (int e = 0; e < VE; ++e) d = fmaf(qf[r][e], x[u][e], d);
-                        d = sum_over_lanes<LPR>(d);
-                        s[u][r] = row[u] >= 0 ? d : -INFINITY;
-                        if (a.raw && c == 0 && slots[u] < len && r < rows)
-                            a.raw[(((int64_t)b * a.c.Hkv + h) * a.c.cap + slots[u]) * a.G + r0 + r] = s[u][r];
-                    }
-#pragma unroll
-                for (int u = 0; u < U; ++u) load(a.c.v, row[u], x[u]);
+            for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int r = 0; r < HG; ++r) {
-                    float mn = m[r];
+                    float d = 0.f;
 #pragma unroll
-                    for (int u = 0; u < U; ++u) mn = fmaxf(mn, s[u][r]);
-                    const float ms = mn == -INFINITY ? 0.f : mn, corr = fast_exp2(m[r] - ms);
-                    m[r] = mn;
-                    l[r] *= corr;
+                    for (int e = 0; e < VE; ++e) d = fmaf(qf[r][e], value(k[u], e), d);
+                    d = sum_over_lanes<LPR>(d);
+                    s[u][r] = row[u] >= 0 ? d : -INFINITY;
+                    if (a.raw && c == 0 && slots[u] < len && r < rows)
+                        a.raw[(((int64_t)b * a.c.Hkv + h) * a.c.cap + slots[u]) * a.G + r0 + r] = s[u][r];
+                }
 #pragma unroll
-                    for (int e = 0; e < VE; ++e) acc[r][e] *= corr;
+            for (int r = 0; r < HG; ++r) {
+                float mn = m[r];
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        const float p = fast_exp2(s[u][r] - ms);
-                        l[r] += p;
+                for (int u = 0; u < U; ++u) mn = fmaxf(mn, s[u][r]);
+                const float ms = mn == -INFINITY ? 0.f : mn, corr = fast_exp2(m[r] - ms);
+                m[r] = mn;
+                l[r] *= corr;
 #pragma unroll
-                        for (int e = 0; e < VE; ++e) acc[r][e] = fmaf(p, x[u][e], acc[r][e]);
-                    }
+                for (int e = 0; e < VE; ++e) acc[r][e] *= corr;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const float p = fast_exp2(s[u][r] - ms);
+                    l[r] += p;
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) acc[r][e] = fmaf(p, value(v[u], e), acc[r][e]);
                 }
             }
+        }
         // the lane groups' parts of a head, then one per wavefront into LDS
 #pragma unroll
         for (int r = 0; r < HG; ++r) {
@@ -366,8 +375,8 @@ __global__ __launch_bounds__(256, 1) void k_decode_attn_mfma(DecodeArgs a)
             const int pg = (int)a.c.page((uint32_t)s);
             int row = -1;
             if (s < len) {
-                if ((uint32_t)id < (uint32_t)a.c.n_pages) row = (id * a.c.Hkv + h) * (int)a.c.page.d + (s - pg * (int)a.c.page.d);
-                else a.c.flag(MOA_DEV_BAD_PAGE);
+                row = a.c.row_in(id, pg, h, s);
+                if (row < 0) a.c.flag(MOA_DEV_BAD_PAGE);
             }
             if (lane < 32) *(__attribute__((address_space(3))) int32_t *)(uintptr_t)(rows0 + lane * 4) = row;
             const uint32_t ok = (uint32_t)__ballot(row >= 0);
@@ -648,7 +657,7 @@ DecodePlan decode_plan(const moa_kv_cache_t &c, int H, bool accounts, bool mfma)
     // One workgroup per pair where that is a short walk, without a second launch.  Else a run per compute unit, of which one
     // workgroup fills the LDS; shorter runs only start more often (8 x 32768 keys: 181 us with 256, 184 with 1024; 4 x 4097:
     // 17.5 and 27.9).
-    p.runs = cap <= 512 && !(accounts && p.rtiles > 1) ? 0 : 256;
+    p.runs = cap <= 512 && !(accounts && p.rtiles > 1) ? 0 : p.mfma ? 256 : 1024;
     p.part_o = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * c.head_dim * 4) : 0;
     p.part_ml = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * 2 * 4) : 0;
     p.raw = accounts ? align256((size_t)c.B * H * cap * 4) : 0;

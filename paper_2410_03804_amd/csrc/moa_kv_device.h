@@ -38,7 +38,12 @@ struct KvDev {
     // fit 31 bits: check_kv_cache.)
     __host__ __device__ __forceinline__ int row(int b, int h, int slot) const
     {
-        const int pg = (int)page((uint32_t)slot), id = table[(int64_t)b * max_pages + pg];
+        const int pg = (int)page((uint32_t)slot);
+        return row_in(table[(int64_t)b * max_pages + pg], pg, h, slot);
+    }
+    // the same where the entry of the slot's page pg is at hand
+    __host__ __device__ __forceinline__ int row_in(int id, int pg, int h, int slot) const
+    {
         return (uint32_t)id < (uint32_t)n_pages ? (id * Hkv + h) * (int)page.d + (slot - pg * (int)page.d) : -1;
     }
     __device__ __forceinline__ void flag(int bit) const
