@@ -21,7 +21,6 @@ struct DecodeArgs {
     void *out;                    // [B, H, dh]
     int H, G, HG, rtiles, HB;     // query heads, per KV head; of these in a tile; tiles per KV head; Hkv * rtiles
     int runs;                     // workgroups the tiles are dealt to; 0: one workgroup per pair
-    int min_run;                  // tiles of a run, at least
     int wide;                     // rows can be read 16 bytes at a time
     float scale;                  // log2(e) / sqrt(dh)
     float *part_o;                // [runs + B HB][HG][dh]
@@ -29,58 +28,41 @@ struct DecodeArgs {
     float *raw;                   // [B, Hkv, cap, G] scores, where accounts are kept; else NULL
 };
 
-__device__ __forceinline__ uint32_t wave_scan(uint32_t x, int lane)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
-    return x;
-}
-
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+__device__ __forceinline__ uint32_t from_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
+__device__ __forceinline__ uint32_t tiles_of(int len) { return (uint32_t)(len + TK - 1) / TK; }
 
 // Where the tiles of the sequences lie in the list of all tiles: every wavefront works this out for itself.
 struct TileList {
     uint32_t total, per;          // tiles in all, of a run
-    __device__ __forceinline__ uint32_t tiles(const DecodeArgs &a, int b) const
-    {
-        return b < a.c.B ? (uint32_t)(a.c.length(b, false) + TK - 1) / TK : 0u;
-    }
-    __device__ __forceinline__ TileList() : total(0), per(0) {}
     __device__ __forceinline__ void set(const DecodeArgs &a, uint32_t all)       // all: tiles of the sequences, for one KV head
     {
         total = all * (uint32_t)a.HB;
-        const uint32_t even = (total + a.runs - 1) / a.runs;
-        per = even > (uint32_t)a.min_run ? even : (uint32_t)a.min_run;
+        per = max((total + a.runs - 1) / a.runs, 1u);
     }
-    __device__ __forceinline__ explicit TileList(const DecodeArgs &a) : total(0), per(0)
-    {
-        if (a.runs == 0) return;
-        const int lane = threadIdx.x & 63;
-        uint32_t x = 0;
-        for (int b = lane; b < a.c.B; b += 64) x += tiles(a, b);
-#pragma unroll
-        for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
-        set(a, uniform(x));
-    }
-    // the sequence of tile f < total and its first tile
-    __device__ __forceinline__ void find(const DecodeArgs &a, uint32_t f, int &b, uint32_t &begin, uint32_t &nt) const
+    // the sequence of the first tile of run w (if it has one), its length and its first tile
+    __device__ __forceinline__ bool find(const DecodeArgs &a, uint32_t w, int &b, int &len, uint32_t &begin)
     {
         const int lane = threadIdx.x & 63;
+        int mine = lane < a.c.B ? a.c.length(lane, false) : 0;
+        uint32_t upto = wave_scan(tiles_of(mine)), all = from_lane(upto, 63);
+        for (int i = lane + 64; i < (a.c.B + 63) / 64 * 64; i += 64) all += from_lane(wave_scan(i < a.c.B ? tiles_of(a.c.length(i, false)) : 0u), 63);
+        set(a, all);
+        const uint32_t f = w * per;
+        if (f >= total) return false;
         uint32_t base = 0;
         for (int b0 = 0;; b0 += 64) {
-            const uint32_t mine = tiles(a, b0 + lane), upto = base + wave_scan(mine, lane);
-            const uint64_t past = __ballot(f < upto * (uint32_t)a.HB);
-            if (past || b0 + 64 >= a.c.B) {
-                const int at = past ? __ffsll((unsigned long long)past) - 1 : 63;
+            const uint64_t past = __ballot(f < (base + upto) * (uint32_t)a.HB);
+            if (past) {
+                const int at = __ffsll((unsigned long long)past) - 1;
                 b = b0 + at;
-                nt = uniform(__shfl(mine, at));
-                begin = (uniform(__shfl(upto, at)) - nt) * (uint32_t)a.HB;
-                return;
+                len = (int)from_lane((uint32_t)mine, at);
+                begin = (base + from_lane(upto, at) - tiles_of(len)) * (uint32_t)a.HB;
+                return true;
             }
-            base = uniform(__shfl(upto, 63));
+            base += from_lane(upto, 63);
+            mine = b0 + 64 + lane < a.c.B ? a.c.length(b0 + 64 + lane, false) : 0;
+            upto = wave_scan(tiles_of(mine));
         }
     }
 };
@@ -88,7 +70,7 @@ struct TileList {
 // ---------------------------------------------------------------- what either kernel does with a run's result
 // (DH: the head_dim, 0 where it is not known here.)  LDS: acc [HG][dh] of each wavefront, `stride` floats apart, and ml [WAVES][HG][2].
 template <typename T, int DH>
-__device__ __forceinline__ void finish(const DecodeArgs &a, int b, int hb, uint32_t t0, uint32_t nt, bool whole, int64_t slot, const float *acc,
+__device__ __forceinline__ void finish(const DecodeArgs &a, int b, int len, int hb, bool whole, int64_t slot, const float *acc,
                                        int stride, const float *ml, float *fin)
 {
     const int tid = threadIdx.x, dh = DH ? DH : a.c.dh, h = hb / a.rtiles, rt = hb - h * a.rtiles;
@@ -122,8 +104,7 @@ __device__ __forceinline__ void finish(const DecodeArgs &a, int b, int hb, uint3
     }
     // A pair's accounts are one workgroup's to change only where it has all its keys and all its query heads.
     if (a.raw && whole && a.rtiles == 1) {
-        const int n = min((int)((t0 + nt) * TK), a.c.length(b, false));
-        for (int s = (int)t0 * TK + tid; s < n; s += 64 * WAVES) {
+        for (int s = tid; s < len; s += 64 * WAVES) {
             float p = 0.f;
             const float *raw = a.raw + (((int64_t)b * a.c.Hkv + h) * a.c.cap + s) * a.G;
             for (int r = 0; r < rows; ++r) p += fast_exp2(raw[r] - fin[r * 2]) * fin[r * 2 + 1];
@@ -133,42 +114,41 @@ __device__ __forceinline__ void finish(const DecodeArgs &a, int b, int hb, uint3
     __syncthreads();
 }
 
-// The runs of a workgroup: each of the pairs that its tiles belong to, with process(b, hb, first tile, tiles, all of them, partial slot).
+// The run of a workgroup: each of the pairs that its tiles belong to, with process(b, length, hb, first tile, tiles, whether these are
+// all of them, partial slot).
 template <typename F>
 __device__ __forceinline__ void for_each_pair(const DecodeArgs &a, const F &process)
 {
-    int b;
-    uint32_t f, end, begin, nt, hb, t, cnt;
+    int b, len;
+    uint32_t f = 0, end = 0, begin = 0, hb, t = 0, cnt;
     const bool one = a.runs == 0;
-    const TileList list(a);
     if (one) {
         b = (int)blockIdx.x / a.HB;
         hb = blockIdx.x - (uint32_t)b * a.HB;
-        cnt = nt = uniform(list.tiles(a, b));
-        f = end = begin = t = 0;
-        if (hb == 0 && threadIdx.x == 0) (void)a.c.length(b, true);
+        len = (int)uniform((uint32_t)a.c.length(b, hb == 0 && threadIdx.x == 0));
+        cnt = tiles_of(len);
     } else {
+        TileList list;
+        if (!list.find(a, blockIdx.x, b, len, begin)) return;
         f = blockIdx.x * list.per;
         end = min(f + list.per, list.total);
-        if (f >= end) return;
-        list.find(a, f, b, begin, nt);
     }
     for (;;) {
+        const uint32_t nt = tiles_of(len);
         if (!one) {
             const uint32_t in = f - begin;
             hb = in / nt;
             t = in - hb * nt;
             cnt = min(nt - t, end - f);
+            if (hb == 0 && t == 0 && threadIdx.x == 0) (void)a.c.length(b, true);
         }
-        process(b, (int)hb, t, cnt, cnt == nt, (int64_t)blockIdx.x + (int64_t)b * a.HB + hb);
+        process(b, len, (int)hb, t, cnt, cnt == nt, (int64_t)blockIdx.x + (int64_t)b * a.HB + hb);
         f += cnt;
         if (one || f >= end) return;
         if (f == begin + nt * (uint32_t)a.HB) {
             begin = f;
-            do {
-                ++b;
-                nt = uniform(list.tiles(a, b));
-            } while (nt == 0);                              // (f < total: there is one)
+            do len = (int)uniform((uint32_t)a.c.length(++b, false));
+            while (len == 0);                               // (f < total: there is one)
         }
     }
 }
@@ -196,9 +176,8 @@ __global__ __launch_bounds__(256) void k_decode_attn(DecodeArgs a)
     float *acc_s = (float *)smem, *ml_s = acc_s + WAVES * HG * a.c.dh, *fin = ml_s + WAVES * HG * 2;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane % LPR, grp = lane / LPR, dh = a.c.dh;
     const int e0 = c * VE, ne = min(max(dh - e0, 0), VE);
-    for_each_pair(a, [&](int b, int hb, uint32_t t0, uint32_t nt, bool whole, int64_t slot) {
+    for_each_pair(a, [&](int b, int len, int hb, uint32_t t0, uint32_t nt, bool whole, int64_t slot) {
         const int h = hb / a.rtiles, r0 = (hb - h * a.rtiles) * HG, rows = min(HG, a.G - r0);
-        const int len = a.c.length(b, hb == 0 && t0 == 0 && tid == 0);
         float qf[HG][VE], acc[HG][VE], m[HG], l[HG];
 #pragma unroll
         for (int r = 0; r < HG; ++r) {
@@ -300,11 +279,11 @@ __global__ __launch_bounds__(256) void k_decode_attn(DecodeArgs a)
                 ml_s[(wave * HG + r) * 2 + 1] = l[r];
             }
         }
-        finish<T, 0>(a, b, hb, t0, nt, whole, slot, acc_s, HG * dh, ml_s, fin);
+        finish<T, 0>(a, b, len, hb, whole, slot, acc_s, HG * dh, ml_s, fin);
     });
 }
 
-// ---------------------------------------------------------------- on the matrix cores: bf16, head_dim 64 or 128
+// ---------------------------------------------------------------- on the matrix cores: bf16, head_dim a multiple of 8 up to 128
 // 64 lanes x 16 (4) bytes, each from an address of its own, to 1 KB (256 bytes) of LDS at `lds`.  (As lds_dma16 in
 // moa_gemm_device.h, but a pool of pages takes 64-bit addresses; the s_nop stands between the write of m0 and its use.)
 __device__ __forceinline__ void lds_gather16(uint32_t lds, uint64_t at)
@@ -321,38 +300,94 @@ __device__ __forceinline__ void wait_loads()
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
+// what rows that do not count are read from
+__device__ const u32x4 zero_row[16] = {};
+
 // Sixteen query heads of a KV head are the columns of a tile: S^T = K Q^T, O^T += V^T P^T.  Every wavefront walks its own 32
-// keys of each tile of the run, with a ring of its own in LDS, so that there is no barrier before the run's end; what a tile
-// needs is loaded NST tiles ahead straight into LDS, its table entries another NST before that.
-template <int DH, bool ACC>
-__global__ __launch_bounds__(256, 1) void k_decode_attn_mfma(DecodeArgs a)
+// keys of each tile of the run, with LDS of its own for NST tiles, so that there is no barrier before the run's end.  Keys and
+// values go straight into LDS: a tile's keys take the place of those NST tiles before as soon as these have been used, its
+// values likewise, and its table entries come another NST tiles before that.  Two workgroups share a compute unit, so that one
+// loads while the other begins or ends a run.
+// DH: head_dim as it lies in LDS; the rows in the pool may be shorter (PAD, a multiple of 8): their last pieces are then zeros.
+template <int DH, bool PAD, bool ACC>
+__global__ __launch_bounds__(256, 2) void k_decode_attn_mfma(DecodeArgs a)
 {
     constexpr int ROWB = DH * 2, PIECES = ROWB / 16, RPI = 64 / PIECES, NL = WK / RPI;   // bytes and 16-byte pieces of a row; rows of a load, loads of K (or V)
-    constexpr int NST = 256 / DH, NKS = DH / 32, NDB = DH / 16;
+    constexpr int NST = 128 / DH, NKS = DH / 32, NDB = DH / 16;
     constexpr uint32_t HALFB = WK * ROWB, STAGEB = 2 * HALFB, IDB = 256, WAVEB = NST * (STAGEB + IDB) + 128;
-    constexpr int YOUNGER = (NST - 1) * (2 * NL + 1);            // loads issued behind those of the current tile
+    constexpr int PERTILE = 2 * NL + 1;                          // loads of a tile: keys, table entries for NST tiles later, values
+    constexpr int BEHIND_K = (NST - 1) * PERTILE + NL, BEHIND_V = (NST - 1) * PERTILE + NL + 1;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     __shared__ float ml_s[WAVES * 16 * 2], fin[16 * 2];
     const int tid = threadIdx.x, lane = tid & 63, n16 = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int dh = PAD ? a.c.dh : DH;
     // [stages: K rows, V rows][table entries][row numbers] of this wavefront.  Rows lie in LDS in the order in which the loads
     // bring them: load j has the keys g (32 / RPI) + j of its lane groups g, so that a lane's keys are neighbours.
     char *mine = smem + wave * WAVEB;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem + (uint32_t)wave * WAVEB;
-    const uint32_t rows0 = lds0 + NST * (STAGEB + IDB);
+    const uint32_t ids0 = lds0 + NST * STAGEB, rows0 = ids0 + NST * IDB;
     const int grp = lane / PIECES;
     // A piece of row p lies at position piece ^ f(p): reads of K touch 16 rows of one column, the transposing reads of V four
     // rows of 32 bytes.
     auto swz = [](int p) { return DH == 128 ? 4 * (p & 3) + ((p >> 2) & 3) : (((p >> 1) & 3) << 1) | ((p >> 3) & 1); };
 
-    for_each_pair(a, [&](int b, int hb, uint32_t t0, uint32_t nt, bool whole, int64_t slot) {
+    for_each_pair(a, [&](int b, int len, int hb, uint32_t t0, uint32_t nt, bool whole, int64_t slot) {
         const int h = hb / a.rtiles, r0 = (hb - h * a.rtiles) * 16, rows = min(16, a.G - r0);
-        const int len = a.c.length(b, hb == 0 && t0 == 0 && tid == 0);
         const int cnt = (int)nt, key0 = (int)t0 * TK + wave * WK;
-        const bf16_t *qrow = (const bf16_t *)a.q + ((int64_t)b * a.H + h * a.G + r0 + min(n16, rows - 1)) * DH;
+        const int32_t *table = a.c.table + (int64_t)b * a.c.max_pages;
+        const bf16_t *q0 = (const bf16_t *)a.q + ((int64_t)b * a.H + h * a.G + r0) * dh;
+        const uint64_t zeros = (uint64_t)(uintptr_t)zero_row;
+        // table entries of the keys of tile i (lanes 32 .. 63 as lanes 0 .. 31)
+        auto fetch_ids = [&](int i) {
+            const int s = min(key0 + i * TK + (lane & 31), len - 1);
+            lds_gather4(ids0 + (uint32_t)(i % NST) * IDB, (uint64_t)(uintptr_t)(table + a.c.page((uint32_t)s)));
+        };
+        u32x4 row[NL / 4];                                  // rows of the pool that this lane reads of the tile that is being fetched
+        // from the table entries of tile i, which are there; returns which of its keys count
+        auto find_rows = [&](int i) -> uint32_t {
+            const int s = key0 + i * TK + (lane & 31);
+            const int id = *(const __attribute__((address_space(3))) int32_t *)(uintptr_t)(ids0 + (uint32_t)(i % NST) * IDB + lane * 4);
+            int r = -1;
+            if (s < len) {
+                r = a.c.row_in(id, (int)a.c.page((uint32_t)s), h, s);
+                if (r < 0) a.c.flag(MOA_DEV_BAD_PAGE);
+            }
+            if (lane < 32) *(__attribute__((address_space(3))) int32_t *)(uintptr_t)(rows0 + lane * 4) = r;
+            const uint32_t ok = (uint32_t)__ballot(r >= 0);
+#pragma unroll
+            for (int j = 0; j < NL / 4; ++j) row[j] = *(const __attribute__((address_space(3))) u32x4 *)(uintptr_t)(rows0 + (grp * NL + 4 * j) * 4);
+            return ok;
+        };
+        auto fetch = [&](const char *pool, uint32_t at) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                  // nobody reads the place any more that is filled now
+#pragma unroll
+            for (int j = 0; j < NL; ++j) {
+                const int piece = (lane % PIECES) ^ swz(RPI * j + grp);
+                const uint32_t r = row[j / 4][j % 4];
+                const bool in = (int)r >= 0 && (!PAD || 8 * piece < dh);
+                const uint64_t from = in ? (uint64_t)(uintptr_t)pool + (uint64_t)r * (uint32_t)(2 * dh) + 16 * piece : zeros + 16 * piece;
+                lds_gather16(at + j * 1024, from);
+            }
+        };
+        // key of the tile that score element e (row 16 (e >> 2) + 4 quad + (e & 3) in LDS) belongs to
+        auto key_of = [&](int e) {
+            const int p = 16 * (e >> 2) + 4 * quad + (e & 3);
+            return (p % RPI) * NL + p / RPI;
+        };
+        if (cnt > 0) {
+#pragma unroll
+            for (int i = 0; i < NST; ++i) fetch_ids(i);
+        }
         bf16x8 qf[NKS];
 #pragma unroll
-        for (int ks = 0; ks < NKS; ++ks) qf[ks] = *(const bf16x8 *)(qrow + 32 * ks + 8 * quad);
+        for (int ks = 0; ks < NKS; ++ks) {
+            const int d = 32 * ks + 8 * quad;
+            union { u32x4 u; bf16x8 v; } x;
+            x.u = u32x4{0u, 0u, 0u, 0u};
+            if (!PAD || d < dh) x.u = *(const u32x4 *)(q0 + min(n16, rows - 1) * dh + d);
+            qf[ks] = x.v;
+        }
 #pragma unroll
         for (int ks = 0; ks < NKS; ++ks) asm volatile("" : "+v"(qf[ks]));       // waited for here, not among the loads below
         f32x4 acc[NDB];
@@ -360,56 +395,18 @@ __global__ __launch_bounds__(256, 1) void k_decode_attn_mfma(DecodeArgs a)
         for (int d = 0; d < NDB; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
         float mref = -INFINITY, lsum = 0.f;                                     // reference of the exponent (log2 domain); this lane's part of the sum
 
-        const int32_t *table = a.c.table + (int64_t)b * a.c.max_pages;
-        // rows that do not count are read from the queries, where there are numbers
-        const uint64_t safe = (uint64_t)(uintptr_t)((const bf16_t *)a.q + ((int64_t)b * a.H + h * a.G + r0) * DH);
-        // table entries of the keys of tile i (lanes 32 .. 63 as lanes 0 .. 31)
-        auto fetch_ids = [&](int i) {
-            const int s = min(key0 + i * TK + (lane & 31), len - 1);
-            lds_gather4(lds0 + NST * STAGEB + (uint32_t)(i % NST) * IDB, (uint64_t)(uintptr_t)(table + a.c.page((uint32_t)s)));
-        };
-        // the loads of tile i, whose table entries are there; returns which of its keys count
-        auto fetch = [&](int i) -> uint32_t {
-            const int s = key0 + i * TK + (lane & 31);
-            const int id = *(const __attribute__((address_space(3))) int32_t *)(uintptr_t)(lds0 + NST * STAGEB + (uint32_t)(i % NST) * IDB + lane * 4);
-            const int pg = (int)a.c.page((uint32_t)s);
-            int row = -1;
-            if (s < len) {
-                row = a.c.row_in(id, pg, h, s);
-                if (row < 0) a.c.flag(MOA_DEV_BAD_PAGE);
-            }
-            if (lane < 32) *(__attribute__((address_space(3))) int32_t *)(uintptr_t)(rows0 + lane * 4) = row;
-            const uint32_t ok = (uint32_t)__ballot(row >= 0);
-            u32x4 r[NL / 4];
-#pragma unroll
-            for (int j = 0; j < NL / 4; ++j) r[j] = *(const __attribute__((address_space(3))) u32x4 *)(uintptr_t)(rows0 + (grp * NL + 4 * j) * 4);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                  // nobody reads the place any more that is filled now
-            const uint32_t at = lds0 + (uint32_t)(i % NST) * STAGEB;
-#pragma unroll
-            for (int j = 0; j < NL; ++j) {
-                const uint32_t off = 16 * ((lane % PIECES) ^ swz(RPI * j + grp));
-                const uint32_t rj = r[j / 4][j % 4];
-                const bool in = (int)rj >= 0;
-                const uint64_t far = (uint64_t)rj * ROWB;
-                lds_gather16(at + j * 1024, (in ? (uint64_t)(uintptr_t)a.c.k + far : safe) + off);
-                lds_gather16(at + HALFB + j * 1024, (in ? (uint64_t)(uintptr_t)a.c.v + far : safe) + off);
-            }
-            return ok;
-        };
-        // key of the tile that score element e (row 16 (e >> 2) + 4 quad + (e & 3) in LDS) belongs to
-        auto key_of = [&](int e) {
-            const int p = 16 * (e >> 2) + 4 * quad + (e & 3);
-            return (p % RPI) * NL + p / RPI;
-        };
         uint32_t ok[NST];
         if (cnt > 0) {
-#pragma unroll
-            for (int i = 0; i < NST; ++i) fetch_ids(i);
             wait_loads<0>();
 #pragma unroll
             for (int i = 0; i < NST; ++i) {
-                ok[i] = i < cnt ? fetch(i) : 0u;
-                fetch_ids(i + NST);
+                ok[i] = 0;
+                if (i < cnt) {
+                    ok[i] = find_rows(i);
+                    fetch(a.c.k, lds0 + i * STAGEB);
+                    fetch_ids(i + NST);
+                    fetch(a.c.v, lds0 + i * STAGEB + HALFB);
+                }
             }
         }
         for (int i0 = 0; i0 < cnt; i0 += NST)
@@ -417,9 +414,10 @@ __global__ __launch_bounds__(256, 1) void k_decode_attn_mfma(DecodeArgs a)
             for (int st = 0; st < NST; ++st) {
                 const int i = i0 + st;
                 if (i >= cnt) break;
-                if (i + NST <= cnt) wait_loads<YOUNGER>();
+                const uint32_t kb = lds0 + st * STAGEB, vb = kb + HALFB, count = ok[st];
+                const bool next = i + NST < cnt;
+                if (i + NST <= cnt) wait_loads<BEHIND_K>();
                 else wait_loads<0>();
-                const uint32_t kb = lds0 + st * STAGEB, vb = kb + HALFB;
                 f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
                 for (int ks = 0; ks < NKS; ++ks)
@@ -432,19 +430,24 @@ __global__ __launch_bounds__(256, 1) void k_decode_attn_mfma(DecodeArgs a)
                 float x[8], tm = -INFINITY;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * a.scale;
-                if (ok[st] != 0xffffffffu) {
+                if (count != 0xffffffffu) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        if (!(ok[st] >> key_of(e) & 1u)) x[e] = -INFINITY;
+                        if (!(count >> key_of(e) & 1u)) x[e] = -INFINITY;
                 }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) tm = fmaxf(tm, x[e]);
-                if (ACC && n16 < rows) {
+                if (ACC && n16 < rows) {                          // (in front of the loads, so that nobody waits for these with the stores)
                     float *raw = a.raw + (((int64_t)b * a.c.Hkv + h) * a.c.cap + key0 + i * TK) * a.G + r0 + n16;
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         if (key0 + i * TK + key_of(e) < len) raw[key_of(e) * a.G] = x[e];
                 }
+                if (next) {
+                    ok[st] = find_rows(i + NST);
+                    fetch(a.c.k, kb);
+                    fetch_ids(i + 2 * NST);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) tm = fmaxf(tm, x[e]);
                 if (__ballot(tm > mref)) {
                     tm = fmaxf(tm, __shfl_xor(tm, 16));
                     tm = fmaxf(tm, __shfl_xor(tm, 32));
@@ -467,6 +470,8 @@ __global__ __launch_bounds__(256, 1) void k_decode_attn_mfma(DecodeArgs a)
                     hi.w[e / 2] = pack_bf16x2(p0, p1);
                     lo.w[e / 2] = pack_bf16x2(p0 - __uint_as_float(hi.w[e / 2] << 16), p1 - __uint_as_float(hi.w[e / 2] & 0xffff0000u));
                 }
+                if (next) wait_loads<BEHIND_V>();
+                else wait_loads<0>();
 #pragma unroll
                 for (int d = 0; d < NDB; ++d) {
                     // transposing read: lane j of a group of 16 addresses key j >> 2 and dims 4 (j & 3) .. of the group's 16
@@ -480,22 +485,22 @@ __global__ __launch_bounds__(256, 1) void k_decode_attn_mfma(DecodeArgs a)
                     acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u.v, hi.v, acc[d], 0, 0, 0);
                     acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u.v, lo.v, acc[d], 0, 0, 0);
                 }
-                if (i + NST < cnt) ok[st] = fetch(i + NST);
-                if (i + NST < cnt) fetch_ids(i + 2 * NST);
+                if (next) fetch(a.c.v, vb);
             }
         wait_loads<0>();
         lsum += __shfl_xor(lsum, 16);
         lsum += __shfl_xor(lsum, 32);
-        float *acc_s = (float *)mine;                              // the ring is free again
+        float *acc_s = (float *)mine;                              // the stages are free again
         if (n16 < rows) {
 #pragma unroll
-            for (int d = 0; d < NDB; ++d) *(f32x4 *)(acc_s + n16 * DH + 16 * d + 4 * quad) = acc[d];
+            for (int d = 0; d < NDB; ++d)
+                if (!PAD || 16 * d + 4 * quad < dh) *(f32x4 *)(acc_s + n16 * dh + 16 * d + 4 * quad) = acc[d];
             if (quad == 0) {
                 ml_s[(wave * a.HG + n16) * 2] = mref;
                 ml_s[(wave * a.HG + n16) * 2 + 1] = lsum;
             }
         }
-        finish<bf16_t, DH>(a, b, hb, t0, nt, whole, slot, (const float *)smem, WAVEB / 4, ml_s, fin);
+        finish<bf16_t, PAD ? 0 : DH>(a, b, len, hb, whole, slot, (const float *)smem, WAVEB / 4, ml_s, fin);
     });
 }
 
@@ -507,8 +512,8 @@ template <typename T>
 __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
 {
     __shared__ float sm[2][16][16], fin[16][2];
-    __shared__ float part[WAVES][256];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, dh = a.c.dh;
+    __shared__ __attribute__((aligned(16))) float part[1024];
+    const int tid = threadIdx.x, lane = tid & 63, dh = a.c.dh;
     const int nb = a.c.B * a.H;
     const bool accounts = (int)blockIdx.x >= nb;
     int b, h, r = 0, chunk = 0;                              // r: query head within its KV head
@@ -523,23 +528,18 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
         h = bh - b * a.c.Hkv;
     }
     uint32_t all = 0, before = 0;
+    for (int b0 = 0; b0 < a.c.B; b0 += 64) {
+        const uint32_t upto = wave_scan(b0 + lane < a.c.B ? tiles_of(a.c.length(b0 + lane, false)) : 0u);
+        if (b > b0) before = all + from_lane(upto, min(b - b0, 64) - 1);
+        all += from_lane(upto, 63);
+    }
     TileList list;
-    for (int i = lane; i < a.c.B; i += 64) {
-        const uint32_t n = list.tiles(a, i);
-        all += n;
-        before += i < b ? n : 0u;
-    }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) {
-        all += __shfl_xor(all, d);
-        before += __shfl_xor(before, d);
-    }
-    list.set(a, uniform(all));
+    list.set(a, all);
     const int len = a.c.length(b, !accounts && h + r == 0 && tid == 0);
-    const uint32_t nt = (uint32_t)(len + TK - 1) / TK;
+    const uint32_t nt = tiles_of(len);
     // the runs that tiles of row tile rt of this KV head are in, and the first's place among the partial results
     auto runs_of = [&](int rt, uint32_t &w0, uint32_t &ns, int64_t &slot0) {
-        const uint32_t hb = (uint32_t)(h * a.rtiles + rt), f0 = uniform(before) * (uint32_t)a.HB + hb * nt;
+        const uint32_t hb = (uint32_t)(h * a.rtiles + rt), f0 = before * (uint32_t)a.HB + hb * nt;
         w0 = f0 / list.per;
         ns = nt ? (f0 + nt - 1) / list.per - w0 + 1 : 0;
         slot0 = (int64_t)w0 + (int64_t)b * a.HB + hb;
@@ -567,19 +567,33 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
         for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
         if (tid == 0 && l == 0.f) a.c.flag(MOA_DEV_EMPTY_KEYS);
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        // a wavefront adds up every fourth partial result
+        // each group of `lanes` threads adds up every so many-th partial result, four elements a thread
+        const int lanes = dh <= 64 ? 16 : dh <= 128 ? 32 : 64, c = tid & (lanes - 1), groups = 256 / lanes, d0 = 4 * c;
         float o[4] = {0.f, 0.f, 0.f, 0.f};
+        if ((dh & 3) == 0 && d0 < dh) {
 #pragma unroll 4
-        for (uint32_t s = wave; s < ns; s += WAVES) {
-            const float w = fast_exp2(ml[s * ml_step] - ms);
+            for (uint32_t s = tid / lanes; s < ns; s += groups) {
+                const float w = fast_exp2(ml[s * ml_step] - ms);
+                const f32x4 x = *(const f32x4 *)(po + s * po_step + d0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i * 64 + lane < dh) o[i] = fmaf(po[s * po_step + i * 64 + lane], w, o[i]);
+                for (int i = 0; i < 4; ++i) o[i] = fmaf(x[i], w, o[i]);
+            }
+        } else {
+#pragma unroll 1
+            for (uint32_t s = tid / lanes; s < ns; s += groups) {
+                const float w = fast_exp2(ml[s * ml_step] - ms);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (d0 + i < dh) o[i] = fmaf(po[s * po_step + d0 + i], w, o[i]);
+            }
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) part[wave][i * 64 + lane] = o[i];
+        *(f32x4 *)(part + 4 * tid) = f32x4{o[0], o[1], o[2], o[3]};
         __syncthreads();
-        if (tid < dh) st(out + tid, (part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid]) * inv);
+        if (tid < dh) {
+            float x = 0.f;
+            for (int g = 0; g < groups; ++g) x += part[g * 4 * lanes + tid];
+            st(out + tid, x * inv);
+        }
         return;
     }
     if (chunk * ACC_SLOTS >= len) return;
@@ -643,7 +657,7 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 // whether the matrix cores' form takes such a cache (and queries q, which it also reads 16 bytes at a time)
 bool takes_mfma(const moa_kv_cache_t &c, const void *q)
 {
-    return c.dtype == MOA_BF16 && (c.head_dim == 64 || c.head_dim == 128) && kv_rows16(c, {q});
+    return c.dtype == MOA_BF16 && c.head_dim <= 128 && kv_rows16(c, {q});
 }
 
 DecodePlan decode_plan(const moa_kv_cache_t &c, int H, bool accounts, bool mfma)
@@ -651,13 +665,13 @@ DecodePlan decode_plan(const moa_kv_cache_t &c, int H, bool accounts, bool mfma)
     DecodePlan p;
     const int G = H / c.n_kv_heads, cap = c.max_pages * c.page_size;
     p.mfma = mfma;
-    p.HG = p.mfma ? (G < 16 ? G : 16) : G <= 2 ? 2 : 8;
+    p.HG = p.mfma ? (G < 16 ? G : 16) : G <= 2 ? 2 : G <= 4 ? 4 : 8;
     p.rtiles = (G + p.HG - 1) / p.HG;
     const int64_t pairs = (int64_t)c.B * c.n_kv_heads * p.rtiles;
     // One workgroup per pair where that is a short walk, without a second launch.  Else a run per compute unit, of which one
     // workgroup fills the LDS; shorter runs only start more often (8 x 32768 keys: 181 us with 256, 184 with 1024; 4 x 4097:
     // 17.5 and 27.9).
-    p.runs = cap <= 512 && !(accounts && p.rtiles > 1) ? 0 : p.mfma ? 256 : 1024;
+    p.runs = cap <= 512 && !(accounts && p.rtiles > 1) ? 0 : p.mfma ? 512 : 1024;
     p.part_o = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * c.head_dim * 4) : 0;
     p.part_ml = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * 2 * 4) : 0;
     p.raw = accounts ? align256((size_t)c.B * H * cap * 4) : 0;
@@ -686,30 +700,40 @@ hipError_t launch_one(const DecodeArgs &a, int grid, hipStream_t st)
     return hipGetLastError();
 }
 
-template <int DH, bool ACC>
+template <int DH, bool PAD, bool ACC>
 hipError_t launch_mfma(const DecodeArgs &a, int grid, hipStream_t st)
 {
-    constexpr size_t lds = (size_t)WAVES * (256 / DH * (2 * WK * DH * 2 + 256) + 128);
+    constexpr size_t lds = (size_t)WAVES * (128 / DH * (2 * WK * DH * 2 + 256) + 128);
     static bool raised[16] = {};
-    hipError_t e = raise_lds_limit_once(raised, (const void *)k_decode_attn_mfma<DH, ACC>, lds);
+    hipError_t e = raise_lds_limit_once(raised, (const void *)k_decode_attn_mfma<DH, PAD, ACC>, lds);
     if (e != hipSuccess) return e;
     prof_begin(K_DECODE_ATTN_MFMA, st);
-    MOA_KLAUNCH((k_decode_attn_mfma<DH, ACC>), dim3(grid), dim3(64 * WAVES), lds, st, a);
+    MOA_KLAUNCH((k_decode_attn_mfma<DH, PAD, ACC>), dim3(grid), dim3(64 * WAVES), lds, st, a);
     prof_end(st);
     return hipGetLastError();
+}
+
+template <int DH>
+hipError_t launch_mfma(const DecodeArgs &a, int grid, hipStream_t st)
+{
+    if (a.c.dh == DH) return a.raw ? launch_mfma<DH, false, true>(a, grid, st) : launch_mfma<DH, false, false>(a, grid, st);
+    return a.raw ? launch_mfma<DH, true, true>(a, grid, st) : launch_mfma<DH, true, false>(a, grid, st);
+}
+
+template <typename T, int HG>
+hipError_t launch_rows(const DecodeArgs &a, int grid, hipStream_t st)
+{
+    constexpr int L1 = 4 * sizeof(T);            // lanes of a row of 64 elements
+    return a.c.dh <= 64 ? launch_one<T, L1, HG>(a, grid, st) : a.c.dh <= 128 ? launch_one<T, 2 * L1, HG>(a, grid, st) : launch_one<T, 4 * L1, HG>(a, grid, st);
 }
 
 template <typename T>
 hipError_t launch_decode(const DecodeArgs &a, bool mfma, hipStream_t st)
 {
     const int grid = a.runs ? a.runs : a.c.B * a.HB;
-    constexpr int VE = 16 / sizeof(T), L1 = 64 / VE;
     hipError_t e;
-    if (mfma) {
-        if (a.c.dh == 128) e = a.raw ? launch_mfma<128, true>(a, grid, st) : launch_mfma<128, false>(a, grid, st);
-        else e = a.raw ? launch_mfma<64, true>(a, grid, st) : launch_mfma<64, false>(a, grid, st);
-    } else if (a.HG == 2) e = a.c.dh <= 64 ? launch_one<T, L1, 2>(a, grid, st) : a.c.dh <= 128 ? launch_one<T, 2 * L1, 2>(a, grid, st) : launch_one<T, 4 * L1, 2>(a, grid, st);
-    else e = a.c.dh <= 64 ? launch_one<T, L1, 8>(a, grid, st) : a.c.dh <= 128 ? launch_one<T, 2 * L1, 8>(a, grid, st) : launch_one<T, 4 * L1, 8>(a, grid, st);
+    if (mfma) e = a.c.dh <= 64 ? launch_mfma<64>(a, grid, st) : launch_mfma<128>(a, grid, st);
+    else e = a.HG == 2 ? launch_rows<T, 2>(a, grid, st) : a.HG == 4 ? launch_rows<T, 4>(a, grid, st) : launch_rows<T, 8>(a, grid, st);
     if (e != hipSuccess || !a.runs) return e;
     const int64_t chunks = (a.c.cap + ACC_SLOTS - 1) / ACC_SLOTS;
     prof_begin(K_DECODE_JOIN, st);
@@ -761,7 +785,7 @@ int32_t moa_decode_attn(const moa_kv_cache_t *cache, int32_t n_q_heads, const vo
     if (need && (!ws || (((uintptr_t)ws) & 255) || ws_bytes < need))
         return api_fail(MOA_ERR_WORKSPACE, "decode_attn: workspace NULL, misaligned or smaller than moa_decode_attn_workspace_bytes");
     DecodeArgs a = {KvDev(*cache, dev_status), q, out, n_q_heads, n_q_heads / cache->n_kv_heads, p.HG, p.rtiles, cache->n_kv_heads * p.rtiles,
-                    p.runs, 1, kv_rows16(*cache, {}) ? 1 : 0, 1.4426950408889634f / sqrtf((float)cache->head_dim),
+                    p.runs, kv_rows16(*cache, {}) ? 1 : 0, 1.4426950408889634f / sqrtf((float)cache->head_dim),
                     (float *)ws, (float *)((char *)ws + p.part_o), p.raw ? (float *)((char *)ws + p.part_o + p.part_ml) : nullptr};
     prof_set_site(S_DECODE);
     hipStream_t st = (hipStream_t)stream;

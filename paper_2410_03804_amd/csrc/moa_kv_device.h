@@ -60,6 +60,23 @@ struct KvDev {
     }
 };
 
+// inclusive sums over the wavefront's lanes by moves inside the vector unit: within rows of 16, then across them
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_from(uint32_t x)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x)
+{
+    x += dpp_from<0x111, 0xf>(x);     // row_shr 1, 2, 4, 8: from the lane so many below, 0 where there is none
+    x += dpp_from<0x112, 0xf>(x);
+    x += dpp_from<0x114, 0xf>(x);
+    x += dpp_from<0x118, 0xf>(x);
+    x += dpp_from<0x142, 0xa>(x);     // row_bcast 15: lane 15 of the row before, to rows 1 and 3
+    x += dpp_from<0x143, 0xc>(x);     // row_bcast 31: lane 31, to rows 2 and 3
+    return x;
+}
+
 // the description's own consistency; `who` for the message
 int32_t check_kv_cache(const moa_kv_cache_t *c, const char *who);
 

@@ -12,6 +12,7 @@ HEADS = {
     "tiny": (4, 2, 64, "f32"), "8b": (32, 8, 128, "bf16"), "mha64": (8, 8, 64, "bf16"), "g8": (16, 2, 128, "bf16"),
     "g20": (20, 1, 128, "bf16"), "g32": (64, 2, 64, "bf16"), "g9f": (9, 1, 128, "f32"), "d80": (6, 2, 80, "bf16"),
     "d33f": (5, 5, 33, "f32"), "d33": (3, 1, 33, "bf16"), "d256f": (2, 1, 256, "f32"), "d256": (8, 2, 256, "bf16"), "d1": (2, 2, 1, "f32"),
+    "d8": (4, 1, 8, "bf16"), "d72": (8, 2, 72, "bf16"), "d96": (12, 2, 96, "bf16"), "d120": (7, 1, 120, "bf16"), "d56": (4, 4, 56, "bf16"), "g3f": (6, 2, 100, "f32"),
 }
 LENS = {
     "one": [1], "few": [5, 1, 17], "edges": [127, 128, 129, 31, 33], "edges512": [511, 512, 513], "ragged": [1000, 3, 0, 2500, 64],
@@ -137,6 +138,21 @@ def test_peaked_and_far_scores(heads):
     q = queries(c, 12, scale=8.0)
     want, tol, _, _ = decode_reference(c, q)
     check(run(c, q), want, tol, f"peaked {heads}")
+
+
+@pytest.mark.parametrize("heads", ["8b", "tiny", "mha64", "d96", "d72"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_query_that_is_no_number_stays_with_its_head(heads, bad):
+    c = Cache(HEADS[heads], [700, 37, 0], 16, seed=16)
+    q = queries(c, 16)
+    want, tol, _, _ = decode_reference(c, q)
+    heads_hit = torch.zeros(c.H, dtype=torch.bool)
+    heads_hit[0] = heads_hit[c.H - 1] = True
+    q[:, heads_hit.cuda(), 0] = bad
+    out = run(c, q)
+    check(out[:, (~heads_hit).cuda()], want[:, (~heads_hit).numpy()], tol[:, (~heads_hit).numpy()], "the other heads")
+    assert not torch.isfinite(out[:2, heads_hit.cuda()]).any()
+    assert (out[2] == 0).all()
 
 
 @pytest.mark.parametrize("heads", ["8b", "tiny"])
