@@ -21,7 +21,6 @@ struct DecodeArgs {
     void *out;                    // [B, H, dh]
     int H, G, HG, rtiles, HB;     // query heads, per KV head; of these in a tile; tiles per KV head; Hkv * rtiles
     int runs;                     // workgroups the tiles are dealt to; 0: one workgroup per pair
-    int wide;                     // rows can be read 16 bytes at a time
     float scale;                  // log2(e) / sqrt(dh)
     float *part_o;                // [runs + B HB][HG][dh]
     float *part_ml;               // [runs + B HB][HG][2]
@@ -167,8 +166,9 @@ __device__ __forceinline__ float sum_over_lanes(float x)
 }
 
 // A row of keys or values is spread over LPR lanes, VE = 16 bytes' worth of elements each; 64 / LPR keys at a time.
-template <typename T, int LPR, int HG>
-__global__ __launch_bounds__(256) void k_decode_attn(DecodeArgs a)
+// WIDE: rows can be read 16 bytes at a time.
+template <typename T, int LPR, int HG, bool WIDE>
+__global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : HG == 8 && sizeof(T) == 2 ? 1 : 2) void k_decode_attn(DecodeArgs a)
 {
     constexpr int VE = 16 / sizeof(T), KPW = 64 / LPR, U = KPW < 8 ? 4 : 2;
     static_assert(WK % (KPW * U) == 0, "rounds of a tile");
@@ -193,35 +193,40 @@ __global__ __launch_bounds__(256) void k_decode_attn(DecodeArgs a)
         auto load = [&](const char *pool, int row, u32x4 &x) {
             const T *p = (const T *)pool + (int64_t)row * dh + e0;
             x = u32x4{0u, 0u, 0u, 0u};
-            if (row >= 0 && ne > 0) {
-                if (a.wide) x = *(const u32x4 *)p;
-                else {
-                    union { u32x4 v; T t[VE]; } u;
-                    u.v = x;
+            if (row < 0 || ne == 0) return;
+            if (WIDE) x = *(const u32x4 *)p;
+            else
 #pragma unroll
-                    for (int e = 0; e < VE; ++e)
-                        if (e < ne) u.t[e] = p[e];
-                    x = u.v;
+                for (int e = 0; e < VE; ++e) {
+                    const uint32_t one = e < ne ? sizeof(T) == 4 ? ((const uint32_t *)p)[e] : ((const uint16_t *)p)[e] : 0u;
+                    if (sizeof(T) == 4) x[e] = one;
+                    else x[e / 2] |= one << 16 * (e & 1);
                 }
-            }
         };
         auto value = [](const u32x4 &x, int e) {
             return sizeof(T) == 4 ? __uint_as_float(x[e]) : __uint_as_float(e & 1 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16);
         };
+        // rounds of KPW U keys of this wavefront; the rows of one are looked up while the one before is computed
+        constexpr int RT = WK / (KPW * U);
+        int row_next[U];
+        auto slot_of = [&](uint32_t t, int u) { return (int)(t / RT) * TK + wave * WK + (int)(t % RT) * KPW * U + u * KPW + grp; };
+        auto look_up = [&](uint32_t t) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) row_next[u] = a.c.row(b, h, min(slot_of(t, u), a.c.cap - 1));   // (what is there only counts below len)
+        };
+        look_up(t0 * RT);
 #pragma unroll 1
-        for (uint32_t t = t0 * (WK / (KPW * U)); t < (t0 + nt) * (WK / (KPW * U)); ++t) {
-            const int base = (int)(t / (WK / (KPW * U))) * TK + wave * WK + (int)(t % (WK / (KPW * U))) * KPW * U + grp;
+        for (uint32_t t = t0 * RT; t < (t0 + nt) * RT; ++t) {
             int slots[U], row[U];
             u32x4 k[U], v[U];
             float s[U][HG];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                // (the table is read for any slot: what is there only counts for those in use)
-                slots[u] = base + u * KPW;
-                row[u] = a.c.row(b, h, min(slots[u], a.c.cap - 1));
-                if (slots[u] >= len) row[u] = -1;
-                else if (row[u] < 0) a.c.flag(MOA_DEV_BAD_PAGE);
+                slots[u] = slot_of(t, u);
+                row[u] = slots[u] < len ? row_next[u] : -1;
+                if (slots[u] < len && row[u] < 0) a.c.flag(MOA_DEV_BAD_PAGE);
             }
+            look_up(t + 1);
 #pragma unroll
             for (int u = 0; u < U; ++u) load(a.c.k, row[u], k[u]);
 #pragma unroll
@@ -307,7 +312,8 @@ __device__ const u32x4 zero_row[16] = {};
 // keys of each tile of the run, with LDS of its own for NST tiles, so that there is no barrier before the run's end.  Keys and
 // values go straight into LDS: a tile's keys take the place of those NST tiles before as soon as these have been used, its
 // values likewise, and its table entries come another NST tiles before that.  Two workgroups share a compute unit, so that one
-// loads while the other begins or ends a run.
+// loads while the other begins or ends a run.  (Rings of two tiles and one workgroup a compute unit: 8 x 32768 keys 181 us against
+// 180, 64 ragged sequences up to 8192 207 against 192, 96 of up to 100 16.7 against 11.1.)
 // DH: head_dim as it lies in LDS; the rows in the pool may be shorter (PAD, a multiple of 8): their last pieces are then zeros.
 template <int DH, bool PAD, bool ACC>
 __global__ __launch_bounds__(256, 2) void k_decode_attn_mfma(DecodeArgs a)
@@ -646,7 +652,7 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
 
 // ---------------------------------------------------------------- host
 struct DecodePlan {
-    bool mfma;
+    bool mfma, wide;
     int HG, rtiles, runs;
     size_t part_o, part_ml, raw;       // bytes
     size_t total() const { return part_o + part_ml + raw; }
@@ -665,7 +671,8 @@ DecodePlan decode_plan(const moa_kv_cache_t &c, int H, bool accounts, bool mfma)
     DecodePlan p;
     const int G = H / c.n_kv_heads, cap = c.max_pages * c.page_size;
     p.mfma = mfma;
-    p.HG = p.mfma ? (G < 16 ? G : 16) : G <= 2 ? 2 : G <= 4 ? 4 : 8;
+    p.wide = kv_rows16(c, {});
+    p.HG = p.mfma ? (G < 16 ? G : 16) : G <= 2 || !p.wide ? 2 : G <= 4 ? 4 : 8;
     p.rtiles = (G + p.HG - 1) / p.HG;
     const int64_t pairs = (int64_t)c.B * c.n_kv_heads * p.rtiles;
     // One workgroup per pair where that is a short walk, without a second launch.  Else a run per compute unit, of which one
@@ -690,12 +697,12 @@ size_t workspace_bytes(const moa_kv_cache_t &c, int H)
     return most;
 }
 
-template <typename T, int LPR, int HG>
+template <typename T, int LPR, int HG, bool WIDE>
 hipError_t launch_one(const DecodeArgs &a, int grid, hipStream_t st)
 {
     const size_t lds = ((size_t)WAVES * HG * (a.c.dh + 2) + HG * 2) * 4;
     prof_begin(K_DECODE_ATTN, st);
-    MOA_KLAUNCH((k_decode_attn<T, LPR, HG>), dim3(grid), dim3(64 * WAVES), lds, st, a);
+    MOA_KLAUNCH((k_decode_attn<T, LPR, HG, WIDE>), dim3(grid), dim3(64 * WAVES), lds, st, a);
     prof_end(st);
     return hipGetLastError();
 }
@@ -720,20 +727,21 @@ hipError_t launch_mfma(const DecodeArgs &a, int grid, hipStream_t st)
     return a.raw ? launch_mfma<DH, true, true>(a, grid, st) : launch_mfma<DH, true, false>(a, grid, st);
 }
 
-template <typename T, int HG>
+template <typename T, int HG, bool WIDE>
 hipError_t launch_rows(const DecodeArgs &a, int grid, hipStream_t st)
 {
     constexpr int L1 = 4 * sizeof(T);            // lanes of a row of 64 elements
-    return a.c.dh <= 64 ? launch_one<T, L1, HG>(a, grid, st) : a.c.dh <= 128 ? launch_one<T, 2 * L1, HG>(a, grid, st) : launch_one<T, 4 * L1, HG>(a, grid, st);
+    return a.c.dh <= 64 ? launch_one<T, L1, HG, WIDE>(a, grid, st) : a.c.dh <= 128 ? launch_one<T, 2 * L1, HG, WIDE>(a, grid, st) : launch_one<T, 4 * L1, HG, WIDE>(a, grid, st);
 }
 
 template <typename T>
-hipError_t launch_decode(const DecodeArgs &a, bool mfma, hipStream_t st)
+hipError_t launch_decode(const DecodeArgs &a, bool mfma, bool wide, hipStream_t st)
 {
     const int grid = a.runs ? a.runs : a.c.B * a.HB;
     hipError_t e;
     if (mfma) e = a.c.dh <= 64 ? launch_mfma<64>(a, grid, st) : launch_mfma<128>(a, grid, st);
-    else e = a.HG == 2 ? launch_rows<T, 2>(a, grid, st) : a.HG == 4 ? launch_rows<T, 4>(a, grid, st) : launch_rows<T, 8>(a, grid, st);
+    else if (!wide) e = launch_rows<T, 2, false>(a, grid, st);
+    else e = a.HG == 2 ? launch_rows<T, 2, true>(a, grid, st) : a.HG == 4 ? launch_rows<T, 4, true>(a, grid, st) : launch_rows<T, 8, true>(a, grid, st);
     if (e != hipSuccess || !a.runs) return e;
     const int64_t chunks = (a.c.cap + ACC_SLOTS - 1) / ACC_SLOTS;
     prof_begin(K_DECODE_JOIN, st);
@@ -785,11 +793,11 @@ int32_t moa_decode_attn(const moa_kv_cache_t *cache, int32_t n_q_heads, const vo
     if (need && (!ws || (((uintptr_t)ws) & 255) || ws_bytes < need))
         return api_fail(MOA_ERR_WORKSPACE, "decode_attn: workspace NULL, misaligned or smaller than moa_decode_attn_workspace_bytes");
     DecodeArgs a = {KvDev(*cache, dev_status), q, out, n_q_heads, n_q_heads / cache->n_kv_heads, p.HG, p.rtiles, cache->n_kv_heads * p.rtiles,
-                    p.runs, kv_rows16(*cache, {}) ? 1 : 0, 1.4426950408889634f / sqrtf((float)cache->head_dim),
+                    p.runs, 1.4426950408889634f / sqrtf((float)cache->head_dim),
                     (float *)ws, (float *)((char *)ws + p.part_o), p.raw ? (float *)((char *)ws + p.part_o + p.part_ml) : nullptr};
     prof_set_site(S_DECODE);
     hipStream_t st = (hipStream_t)stream;
-    const hipError_t e = es == 2 ? launch_decode<bf16_t>(a, p.mfma, st) : launch_decode<float>(a, false, st);
+    const hipError_t e = es == 2 ? launch_decode<bf16_t>(a, p.mfma, p.wide, st) : launch_decode<float>(a, false, p.wide, st);
     if (e != hipSuccess) return api_fail(MOA_ERR_HIP, hipGetErrorString(e));
     return MOA_OK;
 }
