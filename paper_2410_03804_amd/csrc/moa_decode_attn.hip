@@ -31,6 +31,32 @@ __device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__bui
 __device__ __forceinline__ uint32_t from_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
 __device__ __forceinline__ uint32_t tiles_of(int len) { return (uint32_t)(len + TK - 1) / TK; }
 
+// f(x of this lane, x of the lane 16 (32) away), by exchanges inside the vector unit; f commutes
+template <typename F>
+__device__ __forceinline__ float with_lane16(float x, const F &f)
+{
+    const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return f(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+template <typename F>
+__device__ __forceinline__ float with_lane32(float x, const F &f)
+{
+    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return f(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+// over the lanes that differ in bits FROM .. 5 of their number only (FROM = 0: over all)
+template <int FROM, typename F>
+__device__ __forceinline__ float over_lanes(float x, const F &f)
+{
+    if (FROM <= 0) x = f(x, dpp_move_f32<0xB1>(x));      // quad_perm [1, 0, 3, 2]
+    if (FROM <= 1) x = f(x, dpp_move_f32<0x4E>(x));      // quad_perm [2, 3, 0, 1]
+    if (FROM <= 2) x = f(x, dpp_move_f32<0x141>(x));     // row_half_mirror: by now quads are uniform
+    if (FROM <= 3) x = f(x, FROM == 3 ? dpp_move_f32<0x128>(x) : dpp_move_f32<0x140>(x));   // row_ror 8; row_mirror where halves of rows are uniform
+    if (FROM <= 4) x = with_lane16(x, f);
+    return FROM <= 5 ? with_lane32(x, f) : x;
+}
+__device__ __forceinline__ float add(float x, float y) { return x + y; }
+
 // Where the tiles of the sequences lie in the list of all tiles: every wavefront works this out for itself.
 struct TileList {
     uint32_t total, per;          // tiles in all, of a run
@@ -75,32 +101,32 @@ __device__ __forceinline__ void finish(const DecodeArgs &a, int b, int len, int 
     const int tid = threadIdx.x, dh = DH ? DH : a.c.dh, h = hb / a.rtiles, rt = hb - h * a.rtiles;
     const int r0 = rt * a.HG, rows = min(a.HG, a.G - r0);
     __syncthreads();
-    if (tid < rows) {
-        float m = -INFINITY, l = 0.f;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) m = fmaxf(m, ml[(w * a.HG + tid) * 2]);
-        const float ms = m == -INFINITY ? 0.f : m;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) l += ml[(w * a.HG + tid) * 2 + 1] * fast_exp2(ml[(w * a.HG + tid) * 2] - ms);
-        fin[tid * 2] = ms;
-        fin[tid * 2 + 1] = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-        // (a pair with several row tiles has its accounts changed by the second launch in any case)
-        if (!whole || (a.raw && a.rtiles > 1)) {
-            a.part_ml[(slot * a.HG + tid) * 2] = m;
-            a.part_ml[(slot * a.HG + tid) * 2 + 1] = l;
-        }
-        if (whole && l == 0.f) a.c.flag(MOA_DEV_EMPTY_KEYS);
-    }
-    __syncthreads();
     for (int i = tid; i < rows * dh; i += 64 * WAVES) {
         const int r = i / dh, d = i - r * dh;
-        float o = 0.f;
+        float mw[WAVES], m = -INFINITY, l = 0.f, o = 0.f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) o += acc[w * stride + i] * fast_exp2(ml[(w * a.HG + r) * 2] - fin[r * 2]);
-        o *= fin[r * 2 + 1];
-        if (whole) st((T *)a.out + ((int64_t)b * a.H + h * a.G + r0 + r) * dh + d, o);
+        for (int w = 0; w < WAVES; ++w) m = fmaxf(m, mw[w] = ml[(w * a.HG + r) * 2]);
+        const float ms = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float c = fast_exp2(mw[w] - ms);
+            l = fmaf(ml[(w * a.HG + r) * 2 + 1], c, l);
+            o = fmaf(acc[w * stride + i], c, o);
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        if (whole) st((T *)a.out + ((int64_t)b * a.H + h * a.G + r0 + r) * dh + d, o * inv);
         else a.part_o[(slot * a.HG + r) * dh + d] = o;
+        if (d != 0) continue;
+        // (a pair with several row tiles has its accounts changed by the second launch in any case)
+        if (!whole || (a.raw && a.rtiles > 1)) {
+            a.part_ml[(slot * a.HG + r) * 2] = m;
+            a.part_ml[(slot * a.HG + r) * 2 + 1] = l;
+        }
+        if (whole && l == 0.f) a.c.flag(MOA_DEV_EMPTY_KEYS);
+        fin[r * 2] = ms;
+        fin[r * 2 + 1] = inv;
     }
+    __syncthreads();
     // A pair's accounts are one workgroup's to change only where it has all its keys and all its query heads.
     if (a.raw && whole && a.rtiles == 1) {
         for (int s = tid; s < len; s += 64 * WAVES) {
@@ -160,8 +186,8 @@ __device__ __forceinline__ float sum_over_lanes(float x)
     x += dpp_move_f32<0x4E>(x);     // quad_perm [2, 3, 0, 1]
     x += dpp_move_f32<0x141>(x);    // row_half_mirror
     if (LPR >= 16) x += dpp_move_f32<0x140>(x);    // row_mirror
-    if (LPR >= 32) x += __shfl_xor(x, 16);
-    if (LPR >= 64) x += __shfl_xor(x, 32);
+    if (LPR >= 32) x = with_lane16(x, add);
+    if (LPR >= 64) x = with_lane32(x, add);
     return x;
 }
 
@@ -209,14 +235,14 @@ __global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : HG == 8 && siz
         // rounds of KPW U keys of this wavefront; the rows of one are looked up while the one before is computed
         constexpr int RT = WK / (KPW * U);
         int row_next[U];
-        auto slot_of = [&](uint32_t t, int u) { return (int)(t / RT) * TK + wave * WK + (int)(t % RT) * KPW * U + u * KPW + grp; };
+        auto slot_of = [&](uint32_t t, int u) { return (int)(t * WAVES + wave) * KPW * U + u * KPW + grp; };
         auto look_up = [&](uint32_t t) {
 #pragma unroll
             for (int u = 0; u < U; ++u) row_next[u] = a.c.row(b, h, min(slot_of(t, u), a.c.cap - 1));   // (what is there only counts below len)
         };
         look_up(t0 * RT);
 #pragma unroll 1
-        for (uint32_t t = t0 * RT; t < (t0 + nt) * RT; ++t) {
+        for (uint32_t t = t0 * RT; t < (t0 + nt) * RT && slot_of(t, 0) - grp < len; ++t) {
             int slots[U], row[U];
             u32x4 k[U], v[U];
             float s[U][HG];
@@ -265,18 +291,12 @@ __global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : HG == 8 && siz
         // the lane groups' parts of a head, then one per wavefront into LDS
 #pragma unroll
         for (int r = 0; r < HG; ++r) {
-            float mn = m[r];
-#pragma unroll
-            for (int d = LPR; d < 64; d <<= 1) mn = fmaxf(mn, __shfl_xor(mn, d));
-            const float ms = mn == -INFINITY ? 0.f : mn, corr = fast_exp2(m[r] - ms);
-            l[r] *= corr;
-#pragma unroll
-            for (int d = LPR; d < 64; d <<= 1) l[r] += __shfl_xor(l[r], d);
+            constexpr int FROM = LPR == 8 ? 3 : LPR == 16 ? 4 : LPR == 32 ? 5 : 6;
+            const float mn = over_lanes<FROM>(m[r], fmaxf), ms = mn == -INFINITY ? 0.f : mn, corr = fast_exp2(m[r] - ms);
+            l[r] = over_lanes<FROM>(l[r] * corr, add);
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
-                float o = acc[r][e] * corr;
-#pragma unroll
-                for (int d = LPR; d < 64; d <<= 1) o += __shfl_xor(o, d);
+                const float o = over_lanes<FROM>(acc[r][e] * corr, add);
                 if (grp == 0 && e < ne) acc_s[(wave * HG + r) * dh + e0 + e] = o;
             }
             if (lane == 0) {
@@ -455,8 +475,7 @@ __global__ __launch_bounds__(256, 2) void k_decode_attn_mfma(DecodeArgs a)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) tm = fmaxf(tm, x[e]);
                 if (__ballot(tm > mref)) {
-                    tm = fmaxf(tm, __shfl_xor(tm, 16));
-                    tm = fmaxf(tm, __shfl_xor(tm, 32));
+                    tm = over_lanes<4>(tm, fmaxf);
                     const float mnew = fmaxf(mref, tm), corr = mnew == -INFINITY ? 1.f : fast_exp2(mref - mnew);
                     mref = mnew;
                     lsum *= corr;
@@ -494,8 +513,7 @@ __global__ __launch_bounds__(256, 2) void k_decode_attn_mfma(DecodeArgs a)
                 if (next) fetch(a.c.v, vb);
             }
         wait_loads<0>();
-        lsum += __shfl_xor(lsum, 16);
-        lsum += __shfl_xor(lsum, 32);
+        lsum = over_lanes<4>(lsum, add);
         float *acc_s = (float *)mine;                              // the stages are free again
         if (n16 < rows) {
 #pragma unroll
@@ -563,37 +581,49 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
         if (ns <= 1) return;
         const float *ml = a.part_ml + (slot0 * a.HG + rr) * 2, *po = a.part_o + (slot0 * a.HG + rr) * dh;
         const int64_t ml_step = (int64_t)a.HG * 2, po_step = (int64_t)a.HG * dh;
+        // each group of `lanes` threads adds up every so many-th partial result, four elements a thread; the first ones are loaded
+        // while the sums are still unknown
+        const int lanes = dh <= 64 ? 16 : dh <= 128 ? 32 : 64, c = tid & (lanes - 1), groups = 256 / lanes, d0 = 4 * c, g0 = tid / lanes;
+        auto load = [&](uint32_t s) {
+            f32x4 x = {0.f, 0.f, 0.f, 0.f};
+            if (s < ns && d0 < dh) {
+                if ((dh & 3) == 0) x = *(const f32x4 *)(po + s * po_step + d0);
+                else
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (d0 + i < dh) x[i] = po[s * po_step + d0 + i];
+            }
+            return x;
+        };
+        constexpr int U = 4;
+        f32x4 x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = load(g0 + u * groups);
         float m = -INFINITY, l = 0.f;
         for (uint32_t s = lane; s < ns; s += 64) m = fmaxf(m, ml[s * ml_step]);
-#pragma unroll
-        for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+        m = over_lanes<0>(m, fmaxf);
         const float ms = m == -INFINITY ? 0.f : m;
         for (uint32_t s = lane; s < ns; s += 64) l += ml[s * ml_step + 1] * fast_exp2(ml[s * ml_step] - ms);
-#pragma unroll
-        for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
+        l = over_lanes<0>(l, add);
         if (tid == 0 && l == 0.f) a.c.flag(MOA_DEV_EMPTY_KEYS);
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        // each group of `lanes` threads adds up every so many-th partial result, four elements a thread
-        const int lanes = dh <= 64 ? 16 : dh <= 128 ? 32 : 64, c = tid & (lanes - 1), groups = 256 / lanes, d0 = 4 * c;
-        float o[4] = {0.f, 0.f, 0.f, 0.f};
-        if ((dh & 3) == 0 && d0 < dh) {
-#pragma unroll 4
-            for (uint32_t s = tid / lanes; s < ns; s += groups) {
-                const float w = fast_exp2(ml[s * ml_step] - ms);
-                const f32x4 x = *(const f32x4 *)(po + s * po_step + d0);
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        for (uint32_t s = g0; s < ns; s += U * groups) {
+            f32x4 y[U];
+            float w[U];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = fmaf(x[i], w, o[i]);
+            for (int u = 0; u < U; ++u) {
+                const uint32_t su = s + u * groups;
+                w[u] = su < ns ? fast_exp2(ml[su * ml_step] - ms) : 0.f;
+                y[u] = x[u];
+                x[u] = load(su + U * groups);
             }
-        } else {
-#pragma unroll 1
-            for (uint32_t s = tid / lanes; s < ns; s += groups) {
-                const float w = fast_exp2(ml[s * ml_step] - ms);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (d0 + i < dh) o[i] = fmaf(po[s * po_step + d0 + i], w, o[i]);
-            }
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = fmaf(y[u][i], w[u], o[i]);
         }
-        *(f32x4 *)(part + 4 * tid) = f32x4{o[0], o[1], o[2], o[3]};
+        *(f32x4 *)(part + 4 * tid) = o;
         __syncthreads();
         if (tid < dh) {
             float x = 0.f;
