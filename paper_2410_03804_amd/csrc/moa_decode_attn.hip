@@ -24,7 +24,8 @@ struct DecodeArgs {
     float scale;                  // log2(e) / sqrt(dh)
     float *part_o;                // [runs + B HB][HG][dh]
     float *part_ml;               // [runs + B HB][HG][2]
-    float *raw;                   // [B, Hkv, cap, G] scores, where accounts are kept; else NULL
+    int cap32;                    // the capacity in whole blocks of 32 slots
+    float *raw;                   // [B, HB, cap32, HG] scores, where accounts are kept; else NULL
 };
 
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
@@ -131,7 +132,7 @@ __device__ __forceinline__ void finish(const DecodeArgs &a, int b, int len, int 
     if (a.raw && whole && a.rtiles == 1) {
         for (int s = tid; s < len; s += 64 * WAVES) {
             float p = 0.f;
-            const float *raw = a.raw + (((int64_t)b * a.c.Hkv + h) * a.c.cap + s) * a.G;
+            const float *raw = a.raw + (((int64_t)b * a.HB + hb) * a.cap32 + s) * a.HG;
             for (int r = 0; r < rows; ++r) p += fast_exp2(raw[r] - fin[r * 2]) * fin[r * 2 + 1];
             a.c.score[((int64_t)b * a.c.Hkv + h) * a.c.cap + s] += p;
         }
@@ -267,7 +268,7 @@ __global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : HG == 8 && siz
                     d = sum_over_lanes<LPR>(d);
                     s[u][r] = row[u] >= 0 ? d : -INFINITY;
                     if (a.raw && c == 0 && slots[u] < len && r < rows)
-                        a.raw[(((int64_t)b * a.c.Hkv + h) * a.c.cap + slots[u]) * a.G + r0 + r] = s[u][r];
+                        a.raw[(((int64_t)b * a.HB + hb) * a.cap32 + slots[u]) * HG + r] = s[u][r];
                 }
 #pragma unroll
             for (int r = 0; r < HG; ++r) {
@@ -325,6 +326,8 @@ __device__ __forceinline__ void wait_loads()
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
+constexpr uint32_t RAWB = WK * 16 * 4;        // a tile's scores
+
 // what rows that do not count are read from
 __device__ const u32x4 zero_row[16] = {};
 
@@ -340,7 +343,7 @@ __global__ __launch_bounds__(256, 2) void k_decode_attn_mfma(DecodeArgs a)
 {
     constexpr int ROWB = DH * 2, PIECES = ROWB / 16, RPI = 64 / PIECES, NL = WK / RPI;   // bytes and 16-byte pieces of a row; rows of a load, loads of K (or V)
     constexpr int NST = 128 / DH, NKS = DH / 32, NDB = DH / 16;
-    constexpr uint32_t HALFB = WK * ROWB, STAGEB = 2 * HALFB, IDB = 256, WAVEB = NST * (STAGEB + IDB) + 128;
+    constexpr uint32_t HALFB = WK * ROWB, STAGEB = 2 * HALFB, IDB = 256, WAVEB = NST * (STAGEB + IDB) + 128 + (ACC ? RAWB : 0);
     constexpr int PERTILE = 2 * NL + 1;                          // loads of a tile: keys, table entries for NST tiles later, values
     constexpr int BEHIND_K = (NST - 1) * PERTILE + NL, BEHIND_V = (NST - 1) * PERTILE + NL + 1;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -348,11 +351,11 @@ __global__ __launch_bounds__(256, 2) void k_decode_attn_mfma(DecodeArgs a)
     const int tid = threadIdx.x, lane = tid & 63, n16 = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int dh = PAD ? a.c.dh : DH;
-    // [stages: K rows, V rows][table entries][row numbers] of this wavefront.  Rows lie in LDS in the order in which the loads
+    // [stages: K rows, V rows][table entries][row numbers][scores] of this wavefront.  Rows lie in LDS in the order in which the loads
     // bring them: load j has the keys g (32 / RPI) + j of its lane groups g, so that a lane's keys are neighbours.
     char *mine = smem + wave * WAVEB;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem + (uint32_t)wave * WAVEB;
-    const uint32_t ids0 = lds0 + NST * STAGEB, rows0 = ids0 + NST * IDB;
+    const uint32_t ids0 = lds0 + NST * STAGEB, rows0 = ids0 + NST * IDB, raw0 = rows0 + 128;
     const int grp = lane / PIECES;
     // A piece of row p lies at position piece ^ f(p): reads of K touch 16 rows of one column, the transposing reads of V four
     // rows of 32 bytes.
@@ -461,11 +464,15 @@ __global__ __launch_bounds__(256, 2) void k_decode_attn_mfma(DecodeArgs a)
                     for (int e = 0; e < 8; ++e)
                         if (!(count >> key_of(e) & 1u)) x[e] = -INFINITY;
                 }
-                if (ACC && n16 < rows) {                          // (in front of the loads, so that nobody waits for these with the stores)
-                    float *raw = a.raw + (((int64_t)b * a.c.Hkv + h) * a.c.cap + key0 + i * TK) * a.G + r0 + n16;
+                if (ACC && key0 + i * TK < len) {                 // (in front of the loads, so that nobody waits for these with the stores)
+                    // through LDS, where a tile's scores lie as they do in memory
+                    if (n16 < rows) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (key0 + i * TK + key_of(e) < len) raw[key_of(e) * a.G] = x[e];
+                        for (int e = 0; e < 8; ++e) *(__attribute__((address_space(3))) float *)(uintptr_t)(raw0 + (key_of(e) * a.HG + n16) * 4) = x[e];
+                    }
+                    float *raw = a.raw + (((int64_t)b * a.HB + hb) * a.cap32 + key0 + i * TK) * a.HG;
+                    for (int at = 4 * lane; at < WK * a.HG; at += 256)
+                        *(u32x4 *)(raw + at) = *(const __attribute__((address_space(3))) u32x4 *)(uintptr_t)(raw0 + at * 4);
                 }
                 if (next) {
                     ok[st] = find_rows(i + NST);
@@ -529,9 +536,9 @@ __global__ __launch_bounds__(256, 2) void k_decode_attn_mfma(DecodeArgs a)
 }
 
 // ---------------------------------------------------------------- the second launch
-// Workgroups 0 .. B H - 1 join the partial results of one query head; the others bring the accounts of 1024 slots of a (sequence,
+// Workgroups 0 .. B H - 1 join the partial results of one query head; the others bring the accounts of 256 slots of a (sequence,
 // KV head) up to date from its scores, now that the sums are known.  Either leaves alone what the first launch finished.
-constexpr int ACC_SLOTS = 1024;
+constexpr int ACC_SLOTS = 256;
 template <typename T>
 __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
 {
@@ -550,6 +557,26 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
         chunk = i - bh * chunks;
         b = bh / a.c.Hkv;
         h = bh - b * a.c.Hkv;
+    }
+    // this thread's account and scores, while the lengths are on their way (where there are several row tiles, those of the first)
+    const int mine = chunk * ACC_SLOTS + tid;
+    float score = 0.f, weight = 0.f, raw[16];
+    auto load_raw = [&](int rt) {
+        const float *p = a.raw + ((((int64_t)b * a.HB + h * a.rtiles + rt)) * a.cap32 + mine) * a.HG;
+        if ((a.HG & 3) == 0) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (4 * q < a.HG) *(f32x4 *)(raw + 4 * q) = *(const f32x4 *)(p + 4 * q);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+                if (q < a.HG) raw[q] = p[q];
+        }
+    };
+    float *const account = a.c.score + ((int64_t)b * a.c.Hkv + h) * a.c.cap + mine;
+    if (accounts && mine < a.c.cap) {
+        score = *account;
+        load_raw(0);
     }
     uint32_t all = 0, before = 0;
     for (int b0 = 0; b0 < a.c.B; b0 += 64) {
@@ -633,7 +660,6 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
         return;
     }
     if (chunk * ACC_SLOTS >= len) return;
-    float accs[ACC_SLOTS / 256] = {0.f, 0.f, 0.f, 0.f};      // of this thread's slots, over the row tiles
     for (int rt = 0; rt < a.rtiles; ++rt) {
         const int r0 = rt * a.HG, rows = min(a.HG, a.G - r0);
         runs_of(rt, w0, ns, slot0);
@@ -664,26 +690,20 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
             fin[row][1] = l == 0.f ? 0.f : 1.f / l;
         }
         __syncthreads();
+        if (mine < len) {
+            if (rt > 0) load_raw(rt);
 #pragma unroll
-        for (int i = 0; i < ACC_SLOTS / 256; ++i) {
-            const int s = chunk * ACC_SLOTS + i * 256 + tid;
-            if (s < len) {
-                const float *raw = a.raw + (((int64_t)b * a.c.Hkv + h) * a.c.cap + s) * a.G + r0;
-                for (int q = 0; q < rows; ++q) accs[i] += fast_exp2(raw[q] - fin[q][0]) * fin[q][1];
-            }
+            for (int q = 0; q < 16; ++q)
+                if (q < rows) weight += fast_exp2(raw[q] - fin[q][0]) * fin[q][1];
         }
     }
-#pragma unroll
-    for (int i = 0; i < ACC_SLOTS / 256; ++i) {
-        const int s = chunk * ACC_SLOTS + i * 256 + tid;
-        if (s < len) a.c.score[((int64_t)b * a.c.Hkv + h) * a.c.cap + s] += accs[i];
-    }
+    if (mine < len) *account = score + weight;
 }
 
 // ---------------------------------------------------------------- host
 struct DecodePlan {
     bool mfma, wide;
-    int HG, rtiles, runs;
+    int HG, rtiles, runs, cap32;
     size_t part_o, part_ml, raw;       // bytes
     size_t total() const { return part_o + part_ml + raw; }
 };
@@ -711,7 +731,8 @@ DecodePlan decode_plan(const moa_kv_cache_t &c, int H, bool accounts, bool mfma)
     p.runs = cap <= 512 && !(accounts && p.rtiles > 1) ? 0 : p.mfma ? 512 : 1024;
     p.part_o = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * c.head_dim * 4) : 0;
     p.part_ml = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * 2 * 4) : 0;
-    p.raw = accounts ? align256((size_t)c.B * H * cap * 4) : 0;
+    p.cap32 = (cap + 31) & ~31;
+    p.raw = accounts ? align256((size_t)pairs * p.cap32 * p.HG * 4) : 0;
     return p;
 }
 
@@ -740,7 +761,7 @@ hipError_t launch_one(const DecodeArgs &a, int grid, hipStream_t st)
 template <int DH, bool PAD, bool ACC>
 hipError_t launch_mfma(const DecodeArgs &a, int grid, hipStream_t st)
 {
-    constexpr size_t lds = (size_t)WAVES * (128 / DH * (2 * WK * DH * 2 + 256) + 128);
+    constexpr size_t lds = (size_t)WAVES * (128 / DH * (2 * WK * DH * 2 + 256) + 128 + (ACC ? RAWB : 0));
     static bool raised[16] = {};
     hipError_t e = raise_lds_limit_once(raised, (const void *)k_decode_attn_mfma<DH, PAD, ACC>, lds);
     if (e != hipSuccess) return e;
@@ -824,7 +845,7 @@ int32_t moa_decode_attn(const moa_kv_cache_t *cache, int32_t n_q_heads, const vo
         return api_fail(MOA_ERR_WORKSPACE, "decode_attn: workspace NULL, misaligned or smaller than moa_decode_attn_workspace_bytes");
     DecodeArgs a = {KvDev(*cache, dev_status), q, out, n_q_heads, n_q_heads / cache->n_kv_heads, p.HG, p.rtiles, cache->n_kv_heads * p.rtiles,
                     p.runs, 1.4426950408889634f / sqrtf((float)cache->head_dim),
-                    (float *)ws, (float *)((char *)ws + p.part_o), p.raw ? (float *)((char *)ws + p.part_o + p.part_ml) : nullptr};
+                    (float *)ws, (float *)((char *)ws + p.part_o), p.cap32, p.raw ? (float *)((char *)ws + p.part_o + p.part_ml) : nullptr};
     prof_set_site(S_DECODE);
     hipStream_t st = (hipStream_t)stream;
     const hipError_t e = es == 2 ? launch_decode<bf16_t>(a, p.mfma, p.wide, st) : launch_decode<float>(a, false, p.wide, st);
