@@ -20,7 +20,7 @@ struct DecodeArgs {
     const void *q;                // [B, H, dh]
     void *out;                    // [B, H, dh]
     int H, G, HG, rtiles, HB;     // query heads, per KV head; of these in a tile; tiles per KV head; Hkv * rtiles
-    int runs;                     // workgroups the tiles are dealt to; 0: one workgroup per pair
+    int runs, runs_log2;          // workgroups the tiles are dealt to, a power of two; 0: one workgroup per pair
     float scale;                  // log2(e) / sqrt(dh)
     float *part_o;                // [runs + B HB][HG][dh]
     float *part_ml;               // [runs + B HB][HG][2]
@@ -64,7 +64,7 @@ struct TileList {
     __device__ __forceinline__ void set(const DecodeArgs &a, uint32_t all)       // all: tiles of the sequences, for one KV head
     {
         total = all * (uint32_t)a.HB;
-        per = max((total + a.runs - 1) / a.runs, 1u);
+        per = max((total + a.runs - 1) >> a.runs_log2, 1u);
     }
     // the sequence of the first tile of run w (if it has one), its length and its first tile
     __device__ __forceinline__ bool find(const DecodeArgs &a, uint32_t w, int &b, int &len, uint32_t &begin)
@@ -464,7 +464,9 @@ __global__ __launch_bounds__(256, 2) void k_decode_attn_mfma(DecodeArgs a)
                     for (int e = 0; e < 8; ++e)
                         if (!(count >> key_of(e) & 1u)) x[e] = -INFINITY;
                 }
-                if (ACC && key0 + i * TK < len) {                 // (in front of the loads, so that nobody waits for these with the stores)
+                // (in front of the next loads, so that nobody waits for these with the stores.  The stores are most of what accounts
+                // cost: 8 x 8192 keys, 8 query heads per KV head, 49.5 us without, 59.5 with, 52 with all but the stores.)
+                if (ACC && key0 + i * TK < len) {
                     // through LDS, where a tile's scores lie as they do in memory
                     if (n16 < rows) {
 #pragma unroll
@@ -844,7 +846,7 @@ int32_t moa_decode_attn(const moa_kv_cache_t *cache, int32_t n_q_heads, const vo
     if (need && (!ws || (((uintptr_t)ws) & 255) || ws_bytes < need))
         return api_fail(MOA_ERR_WORKSPACE, "decode_attn: workspace NULL, misaligned or smaller than moa_decode_attn_workspace_bytes");
     DecodeArgs a = {KvDev(*cache, dev_status), q, out, n_q_heads, n_q_heads / cache->n_kv_heads, p.HG, p.rtiles, cache->n_kv_heads * p.rtiles,
-                    p.runs, 1.4426950408889634f / sqrtf((float)cache->head_dim),
+                    p.runs, p.runs ? 31 - __builtin_clz((unsigned)p.runs) : 0, 1.4426950408889634f / sqrtf((float)cache->head_dim),
                     (float *)ws, (float *)((char *)ws + p.part_o), p.cap32, p.raw ? (float *)((char *)ws + p.part_o + p.part_ml) : nullptr};
     prof_set_site(S_DECODE);
     hipStream_t st = (hipStream_t)stream;
