@@ -151,13 +151,14 @@ __device__ __forceinline__ uint32_t stay_key(float w, bool newest)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// the sum of s[0 .. n): n <= 16
-__device__ __forceinline__ uint32_t sum_before(const uint32_t *s, int n)
+// one number of each of the 16 wavefronts: their sum over the ones before this one, and over all
+struct Before { uint32_t mine, all; };
+__device__ __forceinline__ Before sum_before(const uint32_t *s, int wave)
 {
-    uint32_t x = 0;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) x += w < n ? s[w] : 0u;
-    return x;
+    const int lane = threadIdx.x & 63;
+    const uint32_t upto = wave_scan(lane < 16 ? s[lane] : 0u);
+    const uint32_t mine = (uint32_t)__builtin_amdgcn_readlane((int)upto, wave ? wave - 1 : 0);
+    return {wave ? mine : 0u, (uint32_t)__builtin_amdgcn_readlane((int)upto, 15)};
 }
 
 __device__ __forceinline__ uint32_t lanes_below(uint64_t mask)
@@ -171,12 +172,15 @@ __device__ __forceinline__ uint32_t lanes_below(uint64_t mask)
 // with a larger key stay, and of those with an equal one the lowest, which only matters in the one wavefront where the equal
 // ones that stay end.  Each wavefront then lists what its stretch frees below the budget and what stays beyond it; the i-th of
 // either are one move.
+// What bounds it is instructions, all of them on the one compute unit that has the pair, and a pass over 8 bytes a slot that it loads
+// alone.  64 pairs of up to 16384 slots: 34 us with keys in registers and every pass unrolled (33 KB of code, fetched for one
+// pass), 35 with loops but sums by shuffles, 19.9 now; 128 pairs of 2112 9.6 us.
 __global__ __launch_bounds__(EV_T) void k_kv_evict_select(EvictArgs a)
 {
     constexpr int NW = EV_T / 64, U = 4, UL = 8;         // rounds of 64 slots at a time: from LDS, from memory
     static_assert(NW == 16 && EV_BINS == 2 * EV_T, "sum_before; two digits a thread");
     constexpr uint32_t NEWEST = 0xffffffffu;
-    __shared__ uint32_t hist[EV_BINS];
+    __shared__ __attribute__((aligned(8))) uint32_t hist[EV_BINS];
     __shared__ uint32_t sums[NW], chosen[2], per_wave[3][NW];
     extern __shared__ uint32_t keys[];         // a.keys of them
     const int bh = blockIdx.x, b = bh / a.c.Hkv, h = bh - b * a.c.Hkv, tid = threadIdx.x, lane = tid & 63;
@@ -241,7 +245,7 @@ __global__ __launch_bounds__(EV_T) void k_kv_evict_select(EvictArgs a)
 
     if (lane == 0) per_wave[0][wave] = newest;
     __syncthreads();
-    newest = sum_before(per_wave[0], NW);
+    newest = sum_before(per_wave[0], wave).all;
     uint32_t last = NEWEST, ties = (uint32_t)a.budget;                // of the slots whose key is `last` the lowest `ties` stay
     if (newest < ties) {
         uint32_t want = ties - newest, prefix = 0;                    // `want` slots are still to be found among keys that begin with prefix
@@ -250,12 +254,13 @@ __global__ __launch_bounds__(EV_T) void k_kv_evict_select(EvictArgs a)
         for (;;) {
             // from the largest digit down; thread t has the digits 2 t and 2 t + 1, counted from the top
             const int top = EV_BINS - 1 - 2 * tid;
-            const uint32_t c0 = hist[top], c1 = hist[top - 1];
-            hist[top] = hist[top - 1] = 0;
+            u32x2 *const pair = (u32x2 *)(hist + top - 1);
+            const uint32_t c0 = (*pair)[1], c1 = (*pair)[0];
+            *pair = u32x2{0u, 0u};
             uint32_t upto = wave_scan(c0 + c1);
             if (lane == 63) sums[wave] = upto;
             __syncthreads();
-            upto += sum_before(sums, wave);
+            upto += sum_before(sums, wave).mine;
             const uint32_t before = upto - c0 - c1;
             if (before < want && want <= upto) {
                 const bool second = want > before + c0;
@@ -290,7 +295,7 @@ __global__ __launch_bounds__(EV_T) void k_kv_evict_select(EvictArgs a)
     if (lane == 0) per_wave[1][wave] = same[0] + same[1];
     __syncthreads();
     // those of the equal ones that stay are the stretch's first
-    const uint32_t eq0 = sum_before(per_wave[1], wave), left = eq0 < ties ? ties - eq0 : 0u;
+    const uint32_t eq0 = sum_before(per_wave[1], wave).mine, left = eq0 < ties ? ties - eq0 : 0u;
     const uint32_t stay_low = min(same[0], left), stay_high = min(same[1], left - stay_low);
     const uint32_t holes = (uint32_t)max(min(s1, a.budget) - s0, 0) - more[0] - stay_low, movers = more[1] + stay_high;
     if (lane == 0) {
@@ -298,19 +303,26 @@ __global__ __launch_bounds__(EV_T) void k_kv_evict_select(EvictArgs a)
         per_wave[2][wave] = movers;
     }
     __syncthreads();
-    const uint32_t h0 = sum_before(per_wave[0], wave);
-    int32_t *dst = a.dst + (int64_t)bh * a.moves + h0, *src = a.src + (int64_t)bh * a.moves + sum_before(per_wave[2], wave);
+    const uint32_t h0 = sum_before(per_wave[0], wave).mine;
+    int32_t *dst = a.dst + (int64_t)bh * a.moves + h0, *src = a.src + (int64_t)bh * a.moves + sum_before(per_wave[2], wave).mine;
     uint32_t e = 0;
     each([&](int s, uint32_t x, bool in) {
         const bool low = s + lane < a.budget;
         const uint64_t eq = __ballot(in && x == last);
         const bool stays = in && (x > last || (x == last && e + lanes_below(eq) < left));
         e += __popcll(eq);
-        const uint64_t hole = __ballot(in && low && !stays), mover = __ballot(!low && stays);
-        if (hole >> lane & 1) dst[lanes_below(hole)] = s + lane;
-        if (mover >> lane & 1) src[lanes_below(mover)] = s + lane;
-        dst += __popcll(hole);
-        src += __popcll(mover);
+        if (s < a.budget) {
+            const bool is = in && low && !stays;
+            const uint64_t hole = __ballot(is);
+            if (is) dst[lanes_below(hole)] = s + lane;
+            dst += __popcll(hole);
+        }
+        if (s + 63 >= a.budget) {
+            const bool is = !low && stays;
+            const uint64_t mover = __ballot(is);
+            if (is) src[lanes_below(mover)] = s + lane;
+            src += __popcll(mover);
+        }
     });
     if (tid == EV_T - 1) a.count[bh] = (int32_t)(h0 + holes);
 }
