@@ -316,7 +316,9 @@ int32_t moa_lm_head_argmax(int32_t dtype, const void *x, int32_t R, int32_t d, c
  *   pos   [B, Hkv, cap] the position of the token in each slot and seen [B] the tokens ever appended (both or neither);
  *   score [B, Hkv, cap] the attention weight each slot has received (or NULL).
  * moa_kv_evict needs pos, seen and score.  All of it belongs to the caller and is only described here.  Limits: head_dim <= 256,
- * cap <= 2^30, n_pages * Hkv * page_size < 2^31, B * Hkv <= 2^20, B * n_q_heads * ceil(cap / 128) <= 2^30.
+ * cap <= 2^30, n_pages * Hkv * page_size < 2^31, B * Hkv <= 2^20; for the attention B * n_q_heads <= 2^20 and B * n_q_heads *
+ * ceil(cap / 128) <= 2^30, for the append B, Hkv <= 65535, M <= 2^24 and M * head_dim < 2^31, for the eviction B * Hkv <= 65535 and
+ * min(budget, cap - budget) * head_dim <= 2^30 (MOA_ERR_SHAPE beyond).
  *
  * moa_kv_append puts rows into the cache (the append of moa_ca_kv_append for keys and values that are there already; with
  *   path / n_path of moa_tree_accept it commits the accepted nodes of a verified tree, Alg. 1):

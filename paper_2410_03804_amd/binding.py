@@ -471,7 +471,7 @@ class KVCache:
     """moa_kv_cache_t: a KV cache in pages.  k, v [n_pages, Hkv, page_size, dh]; table [B, max_pages], len [B], optionally pos
     [B, Hkv, max_pages * page_size] with seen [B], score [B, Hkv, max_pages * page_size] (fp32; all others int32).  The tensors
     are checked here, once, and kept alive; their contents belong to the caller.  A contiguous cache [B, Hkv, P_cap, dh] is
-    KVCache(k, v, torch.arange(B)[:, None], prefix_len)."""
+    KVCache(k, v, torch.arange(B)[:, None], prefix_len).  Calls on it are made with its device as the current one."""
 
     def __init__(self, k, v, table, len, pos=None, seen=None, score=None):
         n_pages, Hkv, page_size, dh = k.shape
@@ -481,32 +481,44 @@ class KVCache:
         if k.dtype not in (torch.float32, torch.bfloat16):
             raise ValueError(f"k: dtype {k.dtype}, expected float32 or bfloat16")
         i32, slots = torch.int32, B * Hkv * max_pages * page_size
-        for t in (v, table, len, pos, seen, score):
-            if t is not None and t.device != k.device:
-                raise ValueError("the cache's tensors must be on one device")
+        self._index = k.get_device()
+        t = self._tensor
         self._c = _KvCache(F32 if k.dtype == torch.float32 else BF16, Hkv, dh, B, n_pages, page_size, max_pages,
-                           _dev(k, k.dtype, 0, "k"), _dev(v, k.dtype, 0, "v"), _dev(table, i32, 0, "table"), _dev(len, i32, B, "len"),
-                           _dev(pos, i32, slots, "pos"), _dev(seen, i32, B, "seen"), _dev(score, torch.float32, slots, "score"))
+                           t(k, k.dtype, 0, "k"), t(v, k.dtype, 0, "v"), t(table, i32, 0, "table"), t(len, i32, B, "len"),
+                           t(pos, i32, slots, "pos"), t(seen, i32, B, "seen"), t(score, torch.float32, slots, "score"))
         self._ref = C.byref(self._c)
+        self._dtype, self._dims = k.dtype, (B, Hkv, dh)
         self.k, self.v, self.table, self.len, self.pos, self.seen, self.score = k, v, table, len, pos, seen, score
 
-    def _tensor(self, t, numel, name, dtype=None):
-        if t is not None and t.device != self.k.device:
+    def _tensor(self, t, dtype, numel, name):
+        if t is not None and t.get_device() != self._index and t.is_cuda:
             raise ValueError(f"{name}: must be on the cache's device")
-        return _dev(t, self.k.dtype if dtype is None else dtype, numel, name)
+        return _dev(t, dtype, numel, name)
+
+    def _ws(self, ws):
+        if ws is not None and ws.get_device() != self._index and ws.is_cuda:
+            raise ValueError("ws: must be on the cache's device")
+        return _ws(ws)
+
+    def _stream(self, stream):
+        if torch._C._cuda_getDevice() != self._index or (stream is not None and stream.device_index != self._index):
+            raise ValueError("the cache's device must be the current one, and the stream's")
+        return torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream.cuda_stream
 
 
 def kv_append(cache: KVCache, k_new, v_new, path=None, n_new=None, dev_status=None, stream=None):
     """Rows path[b][:n_new[b]] (without path the first n_new[b], without n_new all) of k_new / v_new [B, Hkv, M, dh] go into the
     slots behind the cache's len[b]; len and seen grow."""
-    c, i32 = cache._c, torch.int32
-    if k_new.shape != v_new.shape or len(k_new.shape) != 4 or k_new.shape[:2] != (c.B, c.n_kv_heads) or k_new.shape[3] != c.head_dim:
+    shape = k_new.shape
+    B, Hkv, dh = cache._dims
+    if len(shape) != 4 or shape[0] != B or shape[1] != Hkv or shape[3] != dh or v_new.shape != shape:
         raise ValueError("k_new and v_new: must be [B, Hkv, M, dh] of the cache")
-    M = k_new.shape[2]
-    n = c.B * c.n_kv_heads * M * c.head_dim
-    _check(_lib.moa_kv_append(cache._ref, cache._tensor(k_new, n, "k_new"), cache._tensor(v_new, n, "v_new"), M,
-                              cache._tensor(path, c.B * M, "path", i32), cache._tensor(n_new, c.B, "n_new", i32),
-                              cache._tensor(dev_status, 1, "dev_status", i32), _stream(stream)))
+    M, t, dt, i32 = shape[2], cache._tensor, cache._dtype, torch.int32
+    n = B * Hkv * M * dh
+    rc = _lib.moa_kv_append(cache._ref, t(k_new, dt, n, "k_new"), t(v_new, dt, n, "v_new"), M, t(path, i32, B * M, "path"),
+                            t(n_new, i32, B, "n_new"), t(dev_status, i32, 1, "dev_status"), cache._stream(stream))
+    if rc:
+        _check(rc)
 
 
 def decode_attn_workspace_bytes(cache: KVCache, n_q_heads: int) -> int:
@@ -517,14 +529,17 @@ def decode_attn_workspace_bytes(cache: KVCache, n_q_heads: int) -> int:
 
 def decode_attn(cache: KVCache, q, out, ws, accumulate=False, dev_status=None, stream=None):
     """Attention of one new token per sequence (q, out [B, H, dh]) over the cache; with accumulate the weights are added to its score."""
-    c = cache._c
-    if len(q.shape) != 3 or q.shape[0] != c.B or q.shape[2] != c.head_dim:
+    shape = q.shape
+    B, _, dh = cache._dims
+    if len(shape) != 3 or shape[0] != B or shape[2] != dh:
         raise ValueError("q: must be [B, H, dh] of the cache")
-    H = q.shape[1]
-    n = c.B * H * c.head_dim
-    wsp, wsb = _ws(ws)
-    _check(_lib.moa_decode_attn(cache._ref, H, cache._tensor(q, n, "q"), cache._tensor(out, n, "out"), 1 if accumulate else 0,
-                                cache._tensor(dev_status, 1, "dev_status", torch.int32), wsp, wsb, _stream(stream)))
+    H, t, dt = shape[1], cache._tensor, cache._dtype
+    n = B * H * dh
+    wsp, wsb = cache._ws(ws)
+    rc = _lib.moa_decode_attn(cache._ref, H, t(q, dt, n, "q"), t(out, dt, n, "out"), 1 if accumulate else 0,
+                              t(dev_status, torch.int32, 1, "dev_status"), wsp, wsb, cache._stream(stream))
+    if rc:
+        _check(rc)
 
 
 def kv_evict_workspace_bytes(cache: KVCache, budget: int) -> int:
@@ -535,9 +550,11 @@ def kv_evict_workspace_bytes(cache: KVCache, budget: int) -> int:
 
 def kv_evict(cache: KVCache, budget: int, recent: int, ws, dev_status=None, stream=None):
     """Sequences of more than `budget` slots are cut down to it: the `recent` newest tokens and those with the largest score stay."""
-    wsp, wsb = _ws(ws)
-    _check(_lib.moa_kv_evict(cache._ref, int(budget), int(recent), cache._tensor(dev_status, 1, "dev_status", torch.int32),
-                             wsp, wsb, _stream(stream)))
+    wsp, wsb = cache._ws(ws)
+    rc = _lib.moa_kv_evict(cache._ref, int(budget), int(recent), cache._tensor(dev_status, torch.int32, 1, "dev_status"), wsp, wsb,
+                           cache._stream(stream))
+    if rc:
+        _check(rc)
 
 
 def msg_pack_tree(tok, parent, msg, dev_status=None, stream=None):

@@ -84,6 +84,44 @@ static void single_entry_points()
     EXPECT(rc == MOA_ERR_WORKSPACE);            // more scratch than the fixed array holds
 }
 
+// the cache of pages: descriptions and arguments that are refused, and calls that get through every host check
+static void kv_cache()
+{
+    moa_kv_cache_t c = {MOA_BF16, 8, 128, 4, 1000, 16, 100, fake(1), fake(2), (const int32_t *)fake(3), (int32_t *)fake(4),
+                        (int32_t *)fake(5), (int32_t *)fake(6), (float *)fake(7)};
+    size_t n = 0, m = 0;
+    for (const int dtype : {MOA_BF16, MOA_F32})
+        for (const int dh : {1, 33, 64, 80, 128, 256})
+            for (const int H : {8, 16, 32, 64, 160})
+                for (const int page : {1, 7, 16, 4096}) {
+                    moa_kv_cache_t d = c;
+                    d.dtype = dtype;
+                    d.head_dim = dh;
+                    d.page_size = page;
+                    EXPECT(moa_decode_attn_workspace_bytes(&d, H, &n) == MOA_OK && n > 0);
+                    for (const int accumulate : {0, 1}) {
+                        const int32_t rc = moa_decode_attn(&d, H, fake(8), fake(9), accumulate, (int32_t *)fake(10), fake(11), n, nullptr);
+                        EXPECT(rc == MOA_ERR_HIP || rc == MOA_OK);
+                    }
+                    EXPECT(moa_decode_attn(&d, H, fake(8), fake(9), 0, nullptr, fake(11), n - 1, nullptr) == MOA_ERR_WORKSPACE);
+                    for (const int M : {1, 60, 5000}) {
+                        const int32_t rc = moa_kv_append(&d, fake(12), fake(13), M, nullptr, nullptr, nullptr, nullptr);
+                        EXPECT(rc == MOA_ERR_HIP || rc == MOA_OK);
+                    }
+                    EXPECT(moa_kv_evict_workspace_bytes(&d, 60, &m) == MOA_OK && m > 0);
+                    const int32_t rc = moa_kv_evict(&d, 60, 60, nullptr, fake(14), m, nullptr);
+                    EXPECT(rc == MOA_ERR_HIP || rc == MOA_OK);
+                }
+    EXPECT(moa_decode_attn(&c, 12, fake(8), fake(9), 0, nullptr, fake(11), 1 << 30, nullptr) == MOA_ERR_SHAPE);
+    EXPECT(moa_kv_evict(&c, 60, 61, nullptr, fake(14), 1 << 30, nullptr) == MOA_ERR_RANGE);
+    c.max_pages = 1 << 30;
+    EXPECT(moa_kv_append(&c, fake(12), fake(13), 1, nullptr, nullptr, nullptr, nullptr) == MOA_ERR_SHAPE);
+    c.max_pages = 100;
+    c.seen = nullptr;
+    EXPECT(moa_kv_append(&c, fake(12), fake(13), 1, nullptr, nullptr, nullptr, nullptr) == MOA_ERR_NULL);
+    EXPECT(moa_kv_append(nullptr, fake(12), fake(13), 1, nullptr, nullptr, nullptr, nullptr) == MOA_ERR_NULL);
+}
+
 // a whole step with fake device pointers: the checks-only pass over every stage, under each schedule and regime
 static void whole_step(int dtype, int B, int M, int P_cap, int64_t T_lsa, int layers, int schedule, bool with_sa, bool folded, bool packed,
                        bool tiny_ws)
@@ -159,6 +197,7 @@ int main()
 {
     workspace_and_shapes();
     single_entry_points();
+    kv_cache();
     for (int schedule = MOA_SCHED_GROUPED; schedule <= MOA_SCHED_SEQUENTIAL; ++schedule) {
         whole_step(MOA_BF16, 1, 60, 1084, 60, 1, schedule, false, true, true, false);       // the headline step
         whole_step(MOA_BF16, 1, 60, 1084, 60, 3, schedule, true, false, false, false);      // Self-Attention layer in front, more layers

@@ -551,11 +551,13 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
     const bool accounts = (int)blockIdx.x >= nb;
     int b, h, r = 0, chunk = 0;                              // r: query head within its KV head
     if (!accounts) {
+        if (blockIdx.y) return;
         b = (int)blockIdx.x / a.H;
         h = ((int)blockIdx.x - b * a.H) / a.G;
         r = (int)blockIdx.x - b * a.H - h * a.G;
     } else {
-        const int chunks = (a.c.cap + ACC_SLOTS - 1) / ACC_SLOTS, i = (int)blockIdx.x - nb, bh = i / chunks;
+        const int chunks = (a.c.cap + ACC_SLOTS - 1) / ACC_SLOTS, i = (int)(blockIdx.x + blockIdx.y * (gridDim.x - nb)) - nb, bh = i / chunks;
+        if (bh >= a.c.B * a.c.Hkv) return;
         chunk = i - bh * chunks;
         b = bh / a.c.Hkv;
         h = bh - b * a.c.Hkv;
@@ -796,9 +798,11 @@ hipError_t launch_decode(const DecodeArgs &a, bool mfma, bool wide, hipStream_t 
     else if (!wide) e = launch_rows<T, 2, false>(a, grid, st);
     else e = a.HG == 2 ? launch_rows<T, 2, true>(a, grid, st) : a.HG == 4 ? launch_rows<T, 4, true>(a, grid, st) : launch_rows<T, 8, true>(a, grid, st);
     if (e != hipSuccess || !a.runs) return e;
-    const int64_t chunks = (a.c.cap + ACC_SLOTS - 1) / ACC_SLOTS;
+    // (a dimension of a launch has less than 2^32 threads)
+    const int64_t accounts = a.raw ? (int64_t)a.c.B * a.c.Hkv * ((a.c.cap + ACC_SLOTS - 1) / ACC_SLOTS) : 0;
+    const int64_t wide_x = accounts < (1 << 20) ? accounts : 1 << 20, y = accounts > wide_x ? (accounts + wide_x - 1) / wide_x : 1;
     prof_begin(K_DECODE_JOIN, st);
-    MOA_KLAUNCH(k_decode_join<T>, dim3((unsigned)(a.c.B * a.H + (a.raw ? a.c.B * a.c.Hkv * chunks : 0))), dim3(256), 0, st, a);
+    MOA_KLAUNCH(k_decode_join<T>, dim3((unsigned)(a.c.B * a.H + wide_x), (unsigned)y), dim3(256), 0, st, a);
     prof_end(st);
     return hipGetLastError();
 }

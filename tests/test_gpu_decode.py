@@ -12,7 +12,7 @@ HEADS = {
     "tiny": (4, 2, 64, "f32"), "8b": (32, 8, 128, "bf16"), "mha64": (8, 8, 64, "bf16"), "g8": (16, 2, 128, "bf16"),
     "g20": (20, 1, 128, "bf16"), "g32": (64, 2, 64, "bf16"), "g9f": (9, 1, 128, "f32"), "d80": (6, 2, 80, "bf16"),
     "d33f": (5, 5, 33, "f32"), "d33": (3, 1, 33, "bf16"), "d256f": (2, 1, 256, "f32"), "d256": (8, 2, 256, "bf16"), "d1": (2, 2, 1, "f32"),
-    "d8": (4, 1, 8, "bf16"), "d72": (8, 2, 72, "bf16"), "d96": (12, 2, 96, "bf16"), "d120": (7, 1, 120, "bf16"), "d56": (4, 4, 56, "bf16"), "g3f": (6, 2, 100, "f32"),
+    "g16": (16, 1, 128, "bf16"), "g9": (9, 1, 64, "bf16"), "d8": (4, 1, 8, "bf16"), "d72": (8, 2, 72, "bf16"), "d96": (12, 2, 96, "bf16"), "d120": (7, 1, 120, "bf16"), "d56": (4, 4, 56, "bf16"), "g3f": (6, 2, 100, "f32"),
 }
 LENS = {
     "one": [1], "few": [5, 1, 17], "edges": [127, 128, 129, 31, 33], "edges512": [511, 512, 513], "ragged": [1000, 3, 0, 2500, 64],
@@ -77,7 +77,7 @@ def test_many_sequences(heads):
 
 
 @pytest.mark.parametrize("lens", [[1], [300, 0, 17], [2100, 1, 0, 640], [129]])
-@pytest.mark.parametrize("heads", ["8b", "tiny", "g20", "g32", "g9f", "d80", "mha64"])
+@pytest.mark.parametrize("heads", ["8b", "tiny", "g20", "g32", "g9f", "d80", "mha64", "g16", "g9", "d33", "d72"])
 def test_accounts(heads, lens):
     c = Cache(HEADS[heads], lens, 16, seed=7, accounts=True)
     q = queries(c, 7)
@@ -170,6 +170,24 @@ def test_same_bits_again_and_on_another_stream(heads):
     moa.decode_attn(k, q, out, ws, stream=s)
     s.synchronize()
     assert torch.equal(out, first)
+
+
+def test_more_blocks_of_accounts_than_a_launch_is_wide():
+    """Room for 2^28 slots, a few in use: blocks of 256 accounts in two rows of the second launch."""
+    B, Hkv, dh, ps = 1, 1, 8, 16
+    cap = 256 * ((1 << 20) + 5)
+    c = Cache((1, Hkv, dh, "f32"), [70], ps, seed=17)
+    table = torch.full((B, cap // ps), -1, dtype=torch.int32, device="cuda")
+    table[:, :c.mp] = c.t_table
+    score = torch.zeros(B, Hkv, cap, device="cuda")
+    cache = moa.KVCache(c.k, c.v, table, c.t_len, score=score)
+    q = queries(c, 17)
+    want, tol, weight, wtol = decode_reference(c, q)
+    out = torch.zeros_like(q)
+    moa.decode_attn(cache, q, out, workspace(moa.decode_attn_workspace_bytes(cache, 1)), accumulate=True, dev_status=c.status)
+    check(out, want, tol, "out")
+    check(score[:, :, :70], weight[:, :, :70], wtol[:, :, :70] + 2.0 ** -23 * weight[:, :, :70], "accounts")
+    assert float(score[:, :, 70:].abs().max()) == 0.0 and c.status.item() == 0
 
 
 def test_pool_of_more_than_4_gib():
