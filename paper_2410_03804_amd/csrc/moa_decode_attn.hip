@@ -221,7 +221,8 @@ __global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : HG == 8 && siz
             const T *p = (const T *)pool + (int64_t)row * dh + e0;
             x = u32x4{0u, 0u, 0u, 0u};
             if (row < 0 || ne == 0) return;
-            if (WIDE) x = *(const u32x4 *)p;
+            // (rows in single precision are whole lines where they are not short: as lds_gather16, 47 us without and 42 with)
+            if (WIDE) x = sizeof(T) == 4 ? __builtin_nontemporal_load((const u32x4 *)p) : *(const u32x4 *)p;
             else
 #pragma unroll
                 for (int e = 0; e < VE; ++e) {
@@ -312,9 +313,13 @@ __global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : HG == 8 && siz
 // ---------------------------------------------------------------- on the matrix cores: bf16, head_dim a multiple of 8 up to 128
 // 64 lanes x 16 (4) bytes, each from an address of its own, to 1 KB (256 bytes) of LDS at `lds`.  (As lds_dma16 in
 // moa_gemm_device.h, but a pool of pages takes 64-bit addresses; the s_nop stands between the write of m0 and its use.)
+// ONCE: nobody reads the line again.  Keys and values whose rows are whole lines: 8 x 32768 keys 180 us without, 159 with (6.7
+// TB/s), 64 ragged sequences 193 and 171.  Rows of 160 bytes share lines: 11.7 us without, 13.9 with.
+template <bool ONCE>
 __device__ __forceinline__ void lds_gather16(uint32_t lds, uint64_t at)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(at));
+    if (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(lds), "v"(at));
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(at));
 }
 __device__ __forceinline__ void lds_gather4(uint32_t lds, uint64_t at)
 {
@@ -396,7 +401,7 @@ __global__ __launch_bounds__(256, 2) void k_decode_attn_mfma(DecodeArgs a)
                 const uint32_t r = row[j / 4][j % 4];
                 const bool in = (int)r >= 0 && (!PAD || 8 * piece < dh);
                 const uint64_t from = in ? (uint64_t)(uintptr_t)pool + (uint64_t)r * (uint32_t)(2 * dh) + 16 * piece : zeros + 16 * piece;
-                lds_gather16(at + j * 1024, from);
+                lds_gather16<!PAD>(at + j * 1024, from);
             }
         };
         // key of the tile that score element e (row 16 (e >> 2) + 4 quad + (e & 3) in LDS) belongs to
