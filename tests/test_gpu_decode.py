@@ -172,6 +172,49 @@ def test_same_bits_again_and_on_another_stream(heads):
     assert torch.equal(out, first)
 
 
+@pytest.mark.parametrize("heads", ["8b", "tiny"])
+def test_sequences_that_share_pages(heads):
+    """A common prompt: the first pages of all sequences are the same ones."""
+    c = Cache(HEADS[heads], [600, 601, 700, 5], 16, seed=18)
+    for b in (1, 2):
+        c.table[b, :30] = c.table[0, :30]
+    c.t_table.copy_(torch.from_numpy(c.table))
+    q = queries(c, 18)
+    want, tol, _, _ = decode_reference(c, q)
+    check(run(c, q), want, tol, f"shared pages {heads}")
+
+
+@pytest.mark.parametrize("heads", [(1, 1, 8, "f32"), (2, 1, 16, "bf16")])
+def test_thousands_of_sequences(heads):
+    rng = np.random.default_rng(19)
+    lens = rng.integers(0, 20, 3000).tolist()
+    lens[2999], lens[64], lens[1000] = 600, 530, 0
+    c = Cache(heads, lens, 8, seed=19, accounts=True)
+    q = queries(c, 19)
+    before = c.score.cpu().double().numpy()
+    want, tol, weight, wtol = decode_reference(c, q)
+    check(run(c, q, accumulate=True), want, tol, "3000 sequences")
+    check(c.score, before + weight, wtol + 2.0 ** -23 * (np.abs(before) + weight), "accounts")
+
+
+@pytest.mark.parametrize("heads", ["8b", "tiny"])
+def test_two_calls_at_once(heads):
+    """On two streams, over one cache, with a workspace and an output each."""
+    c = Cache(HEADS[heads], [9000, 700, 3], 16, seed=20)
+    k = c.moa()
+    qs = [queries(c, 20), queries(c, 21)]
+    want = [run(c, q) for q in qs]
+    n = moa.decode_attn_workspace_bytes(k, c.H)
+    ws, out = [workspace(n) for _ in qs], [torch.zeros_like(q) for q in qs]
+    streams = [torch.cuda.Stream() for _ in qs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i in (0, 1):
+            moa.decode_attn(k, qs[i], out[i], ws[i], stream=streams[i])
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+
+
 def test_more_blocks_of_accounts_than_a_launch_is_wide():
     """Room for 2^28 slots, a few in use: blocks of 256 accounts in two rows of the second launch."""
     B, Hkv, dh, ps = 1, 1, 8, 16
