@@ -330,22 +330,33 @@ __global__ __launch_bounds__(EV_T) void k_kv_evict_select(EvictArgs a)
 template <typename T>
 __global__ __launch_bounds__(256) void k_kv_evict_move(EvictArgs a)
 {
-    constexpr int U = 4;                  // items in flight per thread
+    constexpr int U = 4;                  // items in flight per thread: a unit of a row of K and the same of V
     const int bh = blockIdx.y, b = bh / a.c.Hkv, h = bh - b * a.c.Hkv, units = (int)a.units.d;
-    const int n = a.count[bh];
     const int64_t at = (int64_t)bh * a.moves, acc = (int64_t)bh * a.c.cap;
-    const uint32_t work = (uint32_t)n * units, step = gridDim.x * 256;
+    const uint32_t step = gridDim.x * 256, room = (uint32_t)a.moves * units;
     T *const k = (T *)a.c.k, *const v = (T *)a.c.v;
-    for (uint32_t w0 = blockIdx.x * 256 + threadIdx.x; w0 < work; w0 += U * step) {
+    const int32_t *const count = a.count + bh;
+    int d[U], s[U];
+    auto read_moves = [&](uint32_t w0) {  // (beyond the last move there is room, with anything in it)
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+            const uint32_t i = a.units(min(w0 + q * step, room - 1));
+            d[q] = a.dst[at + i];
+            s[q] = a.src[at + i];
+        }
+    };
+    uint32_t w0 = blockIdx.x * 256 + threadIdx.x;
+    read_moves(w0);                       // on their way together with how many there are
+    const uint32_t work = (uint32_t)*count * units;
+    for (; w0 < work; w0 += U * step, read_moves(w0)) {
         int64_t to[U];
         T kx[U], vx[U];
 #pragma unroll
         for (int q = 0; q < U; ++q) {
-            const uint32_t w = w0 + q * step;
+            const uint32_t w = w0 + q * step, u = w - a.units(w) * units;
             to[q] = -1;
             if (w >= work) continue;
-            const uint32_t i = a.units(w), u = w - i * units;
-            const int d = a.dst[at + i], s = a.src[at + i], rd = a.c.row(b, h, d), rs = a.c.row(b, h, s);
+            const int rd = a.c.row(b, h, d[q]), rs = a.c.row(b, h, s[q]);
             if (rd >= 0 && rs >= 0) {
                 to[q] = (int64_t)rd * units + u;
                 // (nobody reads a row again where it was: 64 pairs of about 1700 moves 27.5 us so, 32 without)
@@ -353,8 +364,8 @@ __global__ __launch_bounds__(256) void k_kv_evict_move(EvictArgs a)
                 vx[q] = __builtin_nontemporal_load(v + (int64_t)rs * units + u);
             } else a.c.flag(MOA_DEV_BAD_PAGE);
             if (u == 0) {
-                a.c.pos[acc + d] = a.c.pos[acc + s];
-                a.c.score[acc + d] = a.c.score[acc + s];
+                a.c.pos[acc + d[q]] = a.c.pos[acc + s[q]];
+                a.c.score[acc + d[q]] = a.c.score[acc + s[q]];
             }
         }
 #pragma unroll
@@ -378,7 +389,7 @@ hipError_t launch_evict(const EvictArgs &a, hipStream_t st)
     prof_begin(K_KV_EVICT_SELECT, st);
     MOA_KLAUNCH(k_kv_evict_select, dim3(bh), dim3(EV_T), (size_t)a.keys * 4, st, a);
     prof_end(st);
-    const int64_t work = (int64_t)a.moves * a.units.d, blocks = (work + 1023) / 1024;
+    const int64_t work = (int64_t)a.moves * a.units.d, blocks = (work + 255) / 256;
     prof_begin(K_KV_EVICT_MOVE, st);
     MOA_KLAUNCH(k_kv_evict_move<T>, dim3((unsigned)(blocks < 64 ? blocks : 64), bh), dim3(256), 0, st, a);
     prof_end(st);
