@@ -315,7 +315,8 @@ int32_t moa_lm_head_argmax(int32_t dtype, const void *x, int32_t R, int32_t d, c
  *   len   [B], within the capacity cap = max_pages * page_size (clamped, MOA_DEV_BAD_LENGTH);
  *   pos   [B, Hkv, cap] the position of the token in each slot and seen [B] the tokens ever appended (both or neither);
  *   score [B, Hkv, cap] the attention weight each slot has received (or NULL).
- * moa_kv_evict needs pos, seen and score.  All of it belongs to the caller and is only described here.  Limits: head_dim <= 256,
+ * moa_kv_evict needs pos, seen and score.  All of it belongs to the caller and is only described here.  len, seen, pos and score go with
+ * one cache (one layer's); a table may serve several.  Limits: head_dim <= 256,
  * cap <= 2^30, n_pages * Hkv * page_size < 2^31, B * Hkv <= 2^20; for the attention B * n_q_heads <= 2^20 and B * n_q_heads *
  * ceil(cap / 128) <= 2^30, for the append B, Hkv <= 65535, M <= 2^24 and M * head_dim < 2^31, for the eviction B * Hkv <= 65535 and
  * min(budget, cap - budget) * head_dim <= 2^30 (MOA_ERR_SHAPE beyond).
@@ -336,7 +337,8 @@ int32_t moa_lm_head_argmax(int32_t dtype, const void *x, int32_t R, int32_t d, c
  * moa_kv_evict cuts every sequence of more than `budget` slots down to `budget`, for each KV head by itself.  Slots stay in this
  *   order: tokens with pos >= seen[b] - recent (all alike), then by score, larger first (NaN last); equal ones by lower slot.  A token that
  *   stays and lies in a slot >= budget moves, with its position and score, into a slot below whose token leaves, the first into the first
- *   and so on; len[b] = budget.  The attention does not see the order of slots.  Note that len then is no longer the position
+ *   and so on; len[b] = budget.  A move from or to a slot whose table entry is no page of the pool moves no row (MOA_DEV_BAD_PAGE).  The
+ *   attention does not see the order of slots.  Note that len then is no longer the position
  *   of the next token (seen is), which moa_tli_decoder_layer takes prefix_len for.
  *   0 <= recent <= budget, 1 <= budget, else MOA_ERR_RANGE.  Workspace: moa_kv_evict_workspace_bytes, 256-byte aligned. */
 typedef struct {
