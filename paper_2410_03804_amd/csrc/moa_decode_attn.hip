@@ -734,10 +734,14 @@ DecodePlan decode_plan(const moa_kv_cache_t &c, int H, bool accounts, bool mfma)
     p.HG = p.mfma ? (G < 16 ? G : 16) : G <= 2 || !p.wide ? 2 : G <= 4 ? 4 : 8;
     p.rtiles = (G + p.HG - 1) / p.HG;
     const int64_t pairs = (int64_t)c.B * c.n_kv_heads * p.rtiles;
-    // One workgroup per pair where that is a short walk, without a second launch.  Else a run per compute unit, of which one
-    // workgroup fills the LDS; shorter runs only start more often (8 x 32768 keys: 181 us with 256, 184 with 1024; 4 x 4097:
-    // 17.5 and 27.9).
-    p.runs = cap <= 512 && !(accounts && p.rtiles > 1) ? 0 : p.mfma ? 512 : 1024;
+    // One workgroup per pair, without a second launch (4 us), where that is a short walk, or not a long one and there are pairs
+    // enough for two workgroups a compute unit.  Else two runs per compute unit on the matrix cores, four element by element.
+    // Measured, us, per pair against runs + join, 8b heads: 1 x 512 tokens 8.7, 6.9 + 4.0; 1 x 1024 12.5, 5.8 + 4.1; 64 x 1024
+    // 38.9, 40.7 + 6.4; 64 x 17 .. 2048 55.3, 50.6 + 7.3.  Single precision: 1 x 256 11.4, 8.2 + 4.1; 1 x 512 19.3, 8.8 + 4.2.
+    // Half and twice as many runs: 64 ragged sequences up to 8192 181 and 176 against 173, 8 x 32768 158 and 164 against 158; single
+    // precision 4 x 32000 28.1 and 27.3 against 23.7.
+    const int64_t walk = p.mfma ? pairs >= 512 ? 1024 : 512 : 256;
+    p.runs = cap <= walk && !(accounts && p.rtiles > 1) ? 0 : p.mfma ? 512 : 1024;
     p.part_o = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * c.head_dim * 4) : 0;
     p.part_ml = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * 2 * 4) : 0;
     p.cap32 = (cap + 31) & ~31;
