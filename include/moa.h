@@ -314,7 +314,7 @@ int32_t moa_lm_head_argmax(int32_t dtype, const void *x, int32_t R, int32_t d, c
  *         call below writes to: the append writes slots len[b] .., the eviction any slot below len[b];
  *   len   [B], within the capacity cap = max_pages * page_size (clamped, MOA_DEV_BAD_LENGTH);
  *   pos   [B, Hkv, cap] the position of the token in each slot and seen [B] the tokens ever appended (both or neither);
- *   score [B, Hkv, cap] the attention weight each slot has received (or NULL).
+ *   score [B, Hkv, cap] the attention weight each slot has received from moa_decode_attn (or what else the caller wants it kept by), or NULL.
  * moa_kv_evict needs pos, seen and score.  All of it belongs to the caller and is only described here.  len, seen, pos and score go with
  * one cache (one layer's); a table may serve several.  Limits: head_dim <= 256,
  * cap <= 2^30, n_pages * Hkv * page_size < 2^31, B * Hkv <= 2^20; for the attention B * n_q_heads <= 2^20 and B * n_q_heads *

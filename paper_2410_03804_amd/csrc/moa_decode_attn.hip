@@ -179,7 +179,7 @@ __device__ __forceinline__ void for_each_pair(const DecodeArgs &a, const F &proc
     }
 }
 
-// ---------------------------------------------------------------- element by element: any head_dim, either type
+// ---------------------------------------------------------------- element by element: single precision, and rows of bf16 that are not in 16 bytes
 template <int LPR>
 __device__ __forceinline__ float sum_over_lanes(float x)
 {
@@ -193,9 +193,9 @@ __device__ __forceinline__ float sum_over_lanes(float x)
 }
 
 // A row of keys or values is spread over LPR lanes, VE = 16 bytes' worth of elements each; 64 / LPR keys at a time.
-// WIDE: rows can be read 16 bytes at a time.
+// WIDE: rows (of single precision: those of bf16 are then taken by the matrix cores) can be read 16 bytes at a time.
 template <typename T, int LPR, int HG, bool WIDE>
-__global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : HG == 8 && sizeof(T) == 2 ? 1 : 2) void k_decode_attn(DecodeArgs a)
+__global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : 2) void k_decode_attn(DecodeArgs a)
 {
     constexpr int VE = 16 / sizeof(T), KPW = 64 / LPR, U = KPW < 8 ? 4 : 2;
     static_assert(WK % (KPW * U) == 0, "rounds of a tile");
@@ -221,8 +221,8 @@ __global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : HG == 8 && siz
             const T *p = (const T *)pool + (int64_t)row * dh + e0;
             x = u32x4{0u, 0u, 0u, 0u};
             if (row < 0 || ne == 0) return;
-            // (rows in single precision are whole lines where they are not short: as lds_gather16, 47 us without and 42 with)
-            if (WIDE) x = sizeof(T) == 4 ? __builtin_nontemporal_load((const u32x4 *)p) : *(const u32x4 *)p;
+            // (whole lines where rows are not short: as lds_gather16, 64 sequences of up to 4000 keys 47 us without and 42 with)
+            if (WIDE) x = __builtin_nontemporal_load((const u32x4 *)p);
             else
 #pragma unroll
                 for (int e = 0; e < VE; ++e) {
@@ -310,7 +310,7 @@ __global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : HG == 8 && siz
     });
 }
 
-// ---------------------------------------------------------------- on the matrix cores: bf16, head_dim a multiple of 8 up to 128
+// ---------------------------------------------------------------- on the matrix cores: bf16, head_dim a multiple of 8
 // 64 lanes x 16 (4) bytes, each from an address of its own, to 1 KB (256 bytes) of LDS at `lds`.  (As lds_dma16 in
 // moa_gemm_device.h, but a pool of pages takes 64-bit addresses; the s_nop stands between the write of m0 and its use.)
 // ONCE: nobody reads the line again.  Keys and values whose rows are whole lines: 8 x 32768 keys 180 us without, 159 with (6.7
@@ -334,21 +334,28 @@ __device__ __forceinline__ void wait_loads()
 constexpr uint32_t RAWB = WK * 16 * 4;        // a tile's scores
 
 // what rows that do not count are read from
-__device__ const u32x4 zero_row[16] = {};
+__device__ const u32x4 zero_row[32] = {};
+
+// tiles that a wavefront holds in LDS, and the bytes of that
+constexpr int decode_stages(int DH) { return DH == 64 ? 2 : 1; }
+constexpr uint32_t decode_wave_bytes(int DH, bool accounts)
+{
+    return decode_stages(DH) * (2 * WK * DH * 2 + 256) + 128 + (accounts ? RAWB : 0);
+}
 
 // Sixteen query heads of a KV head are the columns of a tile: S^T = K Q^T, O^T += V^T P^T.  Every wavefront walks its own 32
 // keys of each tile of the run, with LDS of its own for NST tiles, so that there is no barrier before the run's end.  Keys and
 // values go straight into LDS: a tile's keys take the place of those NST tiles before as soon as these have been used, its
-// values likewise, and its table entries come another NST tiles before that.  Two workgroups share a compute unit, so that one
-// loads while the other begins or ends a run.  (Rings of two tiles and one workgroup a compute unit: 8 x 32768 keys 181 us against
+// values likewise, and its table entries come another NST tiles before that.  Two workgroups share a compute unit (one at 256
+// dims), so that one loads while the other begins or ends a run.  (Rings of two tiles and one workgroup a compute unit: 8 x 32768 keys 181 us against
 // 180, 64 ragged sequences up to 8192 207 against 192, 96 of up to 100 16.7 against 11.1.)
 // DH: head_dim as it lies in LDS; the rows in the pool may be shorter (PAD, a multiple of 8): their last pieces are then zeros.
 template <int DH, bool PAD, bool ACC>
-__global__ __launch_bounds__(256, 2) void k_decode_attn_mfma(DecodeArgs a)
+__global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void k_decode_attn_mfma(DecodeArgs a)
 {
     constexpr int ROWB = DH * 2, PIECES = ROWB / 16, RPI = 64 / PIECES, NL = WK / RPI;   // bytes and 16-byte pieces of a row; rows of a load, loads of K (or V)
-    constexpr int NST = 128 / DH, NKS = DH / 32, NDB = DH / 16;
-    constexpr uint32_t HALFB = WK * ROWB, STAGEB = 2 * HALFB, IDB = 256, WAVEB = NST * (STAGEB + IDB) + 128 + (ACC ? RAWB : 0);
+    constexpr int NST = decode_stages(DH), NKS = DH / 32, NDB = DH / 16;
+    constexpr uint32_t HALFB = WK * ROWB, STAGEB = 2 * HALFB, IDB = 256, WAVEB = decode_wave_bytes(DH, ACC);
     constexpr int PERTILE = 2 * NL + 1;                          // loads of a tile: keys, table entries for NST tiles later, values
     constexpr int BEHIND_K = (NST - 1) * PERTILE + NL, BEHIND_V = (NST - 1) * PERTILE + NL + 1;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -364,7 +371,7 @@ __global__ __launch_bounds__(256, 2) void k_decode_attn_mfma(DecodeArgs a)
     const int grp = lane / PIECES;
     // A piece of row p lies at position piece ^ f(p): reads of K touch 16 rows of one column, the transposing reads of V four
     // rows of 32 bytes.
-    auto swz = [](int p) { return DH == 128 ? 4 * (p & 3) + ((p >> 2) & 3) : (((p >> 1) & 3) << 1) | ((p >> 3) & 1); };
+    auto swz = [](int p) { return DH >= 128 ? 4 * (p & 3) + ((p >> 2) & 3) : (((p >> 1) & 3) << 1) | ((p >> 3) & 1); };
 
     for_each_pair(a, [&](int b, int len, int hb, uint32_t t0, uint32_t nt, bool whole, int64_t slot) {
         const int h = hb / a.rtiles, r0 = (hb - h * a.rtiles) * 16, rows = min(16, a.G - r0);
@@ -722,7 +729,7 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 // whether the matrix cores' form takes such a cache (and queries q, which it also reads 16 bytes at a time)
 bool takes_mfma(const moa_kv_cache_t &c, const void *q)
 {
-    return c.dtype == MOA_BF16 && c.head_dim <= 128 && kv_rows16(c, {q});
+    return c.dtype == MOA_BF16 && kv_rows16(c, {q});
 }
 
 DecodePlan decode_plan(const moa_kv_cache_t &c, int H, bool accounts, bool mfma)
@@ -730,7 +737,7 @@ DecodePlan decode_plan(const moa_kv_cache_t &c, int H, bool accounts, bool mfma)
     DecodePlan p;
     const int G = H / c.n_kv_heads, cap = c.max_pages * c.page_size;
     p.mfma = mfma;
-    p.wide = kv_rows16(c, {});
+    p.wide = c.dtype == MOA_F32 && kv_rows16(c, {});
     p.HG = p.mfma ? (G < 16 ? G : 16) : G <= 2 || !p.wide ? 2 : G <= 4 ? 4 : 8;
     p.rtiles = (G + p.HG - 1) / p.HG;
     const int64_t pairs = (int64_t)c.B * c.n_kv_heads * p.rtiles;
@@ -741,7 +748,7 @@ DecodePlan decode_plan(const moa_kv_cache_t &c, int H, bool accounts, bool mfma)
     // Half and twice as many runs: 64 ragged sequences up to 8192 181 and 176 against 173, 8 x 32768 158 and 164 against 158; single
     // precision 4 x 32000 28.1 and 27.3 against 23.7.
     const int64_t walk = p.mfma ? pairs >= 512 ? 1024 : 512 : 256;
-    p.runs = cap <= walk && !(accounts && p.rtiles > 1) ? 0 : p.mfma ? 512 : 1024;
+    p.runs = cap <= walk && !(accounts && p.rtiles > 1) ? 0 : !p.mfma ? 1024 : c.head_dim <= 128 ? 512 : 256;
     p.part_o = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * c.head_dim * 4) : 0;
     p.part_ml = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * 2 * 4) : 0;
     p.cap32 = (cap + 31) & ~31;
@@ -774,7 +781,7 @@ hipError_t launch_one(const DecodeArgs &a, int grid, hipStream_t st)
 template <int DH, bool PAD, bool ACC>
 hipError_t launch_mfma(const DecodeArgs &a, int grid, hipStream_t st)
 {
-    constexpr size_t lds = (size_t)WAVES * (128 / DH * (2 * WK * DH * 2 + 256) + 128 + (ACC ? RAWB : 0));
+    constexpr size_t lds = (size_t)WAVES * decode_wave_bytes(DH, ACC);
     static bool raised[16] = {};
     hipError_t e = raise_lds_limit_once(raised, (const void *)k_decode_attn_mfma<DH, PAD, ACC>, lds);
     if (e != hipSuccess) return e;
@@ -802,10 +809,11 @@ template <typename T>
 hipError_t launch_decode(const DecodeArgs &a, bool mfma, bool wide, hipStream_t st)
 {
     const int grid = a.runs ? a.runs : a.c.B * a.HB;
-    hipError_t e;
-    if (mfma) e = a.c.dh <= 64 ? launch_mfma<64>(a, grid, st) : launch_mfma<128>(a, grid, st);
+    hipError_t e = hipErrorInvalidValue;
+    if (mfma) e = a.c.dh <= 64 ? launch_mfma<64>(a, grid, st) : a.c.dh <= 128 ? launch_mfma<128>(a, grid, st) : launch_mfma<256>(a, grid, st);
     else if (!wide) e = launch_rows<T, 2, false>(a, grid, st);
-    else e = a.HG == 2 ? launch_rows<T, 2, true>(a, grid, st) : a.HG == 4 ? launch_rows<T, 4, true>(a, grid, st) : launch_rows<T, 8, true>(a, grid, st);
+    else if constexpr (sizeof(T) == 4)
+        e = a.HG == 2 ? launch_rows<T, 2, true>(a, grid, st) : a.HG == 4 ? launch_rows<T, 4, true>(a, grid, st) : launch_rows<T, 8, true>(a, grid, st);
     if (e != hipSuccess || !a.runs) return e;
     // (a dimension of a launch has less than 2^32 threads)
     const int64_t accounts = a.raw ? (int64_t)a.c.B * a.c.Hkv * ((a.c.cap + ACC_SLOTS - 1) / ACC_SLOTS) : 0;

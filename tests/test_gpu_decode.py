@@ -12,7 +12,8 @@ HEADS = {
     "tiny": (4, 2, 64, "f32"), "8b": (32, 8, 128, "bf16"), "mha64": (8, 8, 64, "bf16"), "g8": (16, 2, 128, "bf16"),
     "g20": (20, 1, 128, "bf16"), "g32": (64, 2, 64, "bf16"), "g9f": (9, 1, 128, "f32"), "d80": (6, 2, 80, "bf16"),
     "d33f": (5, 5, 33, "f32"), "d33": (3, 1, 33, "bf16"), "d256f": (2, 1, 256, "f32"), "d256": (8, 2, 256, "bf16"), "d1": (2, 2, 1, "f32"),
-    "g16": (16, 1, 128, "bf16"), "g9": (9, 1, 64, "bf16"), "d8": (4, 1, 8, "bf16"), "d72": (8, 2, 72, "bf16"), "d96": (12, 2, 96, "bf16"), "d120": (7, 1, 120, "bf16"), "d56": (4, 4, 56, "bf16"), "g3f": (6, 2, 100, "f32"),
+    "g16": (16, 1, 128, "bf16"), "g9": (9, 1, 64, "bf16"), "d8": (4, 1, 8, "bf16"), "d72": (8, 2, 72, "bf16"), "d96": (12, 2, 96, "bf16"), "d120": (7, 1, 120, "bf16"), "d56": (4, 4, 56, "bf16"), "g3f": (6, 2, 100, "f32"), "d192": (4, 4, 192, "bf16"), "d136": (10, 1, 136, "bf16"), "d248": (18, 1, 248, "bf16"),
+    "d255": (3, 1, 255, "bf16"), "d130": (4, 2, 130, "bf16"),
 }
 LENS = {
     "one": [1], "few": [5, 1, 17], "edges": [127, 128, 129, 31, 33], "edges512": [511, 512, 513], "ragged": [1000, 3, 0, 2500, 64],
@@ -77,7 +78,7 @@ def test_many_sequences(heads):
 
 
 @pytest.mark.parametrize("lens", [[1], [300, 0, 17], [2100, 1, 0, 640], [129]])
-@pytest.mark.parametrize("heads", ["8b", "tiny", "g20", "g32", "g9f", "d80", "mha64", "g16", "g9", "d33", "d72"])
+@pytest.mark.parametrize("heads", ["8b", "tiny", "g20", "g32", "g9f", "d80", "mha64", "g16", "g9", "d33", "d72", "d256", "d248", "d255"])
 def test_accounts(heads, lens):
     c = Cache(HEADS[heads], lens, 16, seed=7, accounts=True)
     q = queries(c, 7)
@@ -97,7 +98,7 @@ def test_accounts_are_left_alone_without_accumulate():
     assert torch.equal(c.score, before)
 
 
-@pytest.mark.parametrize("heads", ["8b", "tiny", "mha64"])
+@pytest.mark.parametrize("heads", ["8b", "tiny", "mha64", "d256", "d72"])
 def test_rows_that_are_not_16_byte_aligned(heads):
     c = Cache(HEADS[heads], [513, 40], 16, seed=9, offset=1)
     q = queries(c, 9)
@@ -140,7 +141,7 @@ def test_peaked_and_far_scores(heads):
     check(run(c, q), want, tol, f"peaked {heads}")
 
 
-@pytest.mark.parametrize("heads", ["8b", "tiny", "mha64", "d96", "d72"])
+@pytest.mark.parametrize("heads", ["8b", "tiny", "mha64", "d96", "d72", "d256", "d136"])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_a_query_that_is_no_number_stays_with_its_head(heads, bad):
     c = Cache(HEADS[heads], [700, 37, 0], 16, seed=16)
@@ -194,6 +195,18 @@ def test_thousands_of_sequences(heads):
     before = c.score.cpu().double().numpy()
     want, tol, weight, wtol = decode_reference(c, q)
     check(run(c, q, accumulate=True), want, tol, "3000 sequences")
+    check(c.score, before + weight, wtol + 2.0 ** -23 * (np.abs(before) + weight), "accounts")
+
+
+@pytest.mark.parametrize("heads", ["8b", "tiny", "d256"])
+def test_queries_that_are_not_16_byte_aligned(heads):
+    c = Cache(HEADS[heads], [900, 64, 0], 16, seed=22, accounts=True)
+    q = queries(c, 22)
+    flat = torch.empty(q.numel() + 1, dtype=q.dtype, device="cuda")
+    flat[1:].copy_(q.view(-1))
+    before = c.score.cpu().double().numpy()
+    want, tol, weight, wtol = decode_reference(c, q)
+    check(run(c, flat[1:].view(q.shape), accumulate=True), want, tol, f"queries {heads}")
     check(c.score, before + weight, wtol + 2.0 ** -23 * (np.abs(before) + weight), "accounts")
 
 
