@@ -164,7 +164,7 @@ def test_evict_long(n, budget):
     same(state(c), want)
 
 
-@pytest.mark.parametrize("kind", ["equal", "nan", "infinite", "negative", "tiny", "random"])
+@pytest.mark.parametrize("kind", ["equal", "nan", "infinite", "negative", "tiny", "random", "octave", "pairs", "few_bits"])
 def test_evict_kinds_of_accounts(kind):
     lens = [900, 70]
     c = Cache((4, 2, 16, "f32"), lens, 16, seed=21, accounts=True)
@@ -181,10 +181,32 @@ def test_evict_kinds_of_accounts(kind):
         s -= 0.5
     elif kind == "tiny":
         s *= 1e-40                                   # denormals keep their order
-    c.score.copy_(torch.from_numpy(s))
-    want = evict_expected(c, 60, 5, lens)
-    evict(c, 60, 5)
-    same(state(c), want)
+    elif kind == "octave":
+        s = (1.0 + s / 8192).astype(np.float32)      # one first digit, and second ones, for hundreds of slots
+    elif kind == "pairs":
+        s = np.repeat(s[..., ::2], 2, axis=-1)[..., : s.shape[-1]]
+    elif kind == "few_bits":
+        s = (np.floor(s * 3) / 4 + 1.0).astype(np.float32)
+    c.score.copy_(torch.from_numpy(np.ascontiguousarray(s)))
+    for budget in (600, 60):                         # the second time on what the first has left
+        want = evict_expected(c, budget, 5, lens)
+        evict(c, budget, 5)
+        same(state(c), want)
+        lens = c.t_len.tolist()
+
+
+def test_evict_random_sizes():
+    rng = np.random.default_rng(24)
+    for i in range(40):
+        n = int(np.exp(rng.uniform(np.log(2), np.log(9000))))
+        budget = int(rng.integers(1, n + 1))
+        c = Cache((2, 2, 4, "f32"), [n, int(rng.integers(0, n + 1))], int(rng.integers(1, 80)), seed=i, accounts=True)
+        if i % 2:
+            c.score.copy_(torch.exp(2 * torch.randn(c.score.shape, generator=torch.Generator().manual_seed(i))))
+        lens, recent = c.t_len.tolist(), int(rng.integers(0, budget + 1))
+        want = evict_expected(c, budget, recent, lens)
+        evict(c, budget, recent)
+        same(state(c), want)
 
 
 def test_evict_more_protected_than_the_budget_holds():
