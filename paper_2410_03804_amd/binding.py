@@ -17,7 +17,7 @@ if not _LIB_PATH.exists():
     raise ImportError(f"{_LIB_PATH} is missing: build it with `python {_LIB_PATH.with_name('build.py')}` (there is no fallback path)")
 _lib = C.CDLL(str(_LIB_PATH))
 try:
-    from ._argcheck import dev as _dev  # built with the library: csrc/argcheck.c
+    from ._argcheck import dev as _dev, dev_on as _dev_on, room_on as _room_on  # built with the library: csrc/argcheck.c
 except ImportError as e:
     raise ImportError(f"{_LIB_PATH.with_name('_argcheck.abi3.so')}, the argument check built with the library, does not load ({e}): "
                       f"build both with `python {_LIB_PATH.with_name('build.py')}` (there is no fallback path)") from e
@@ -481,29 +481,20 @@ class KVCache:
         if k.dtype not in (torch.float32, torch.bfloat16):
             raise ValueError(f"k: dtype {k.dtype}, expected float32 or bfloat16")
         i32, slots = torch.int32, B * Hkv * max_pages * page_size
-        self._index = k.get_device()
-        t = self._tensor
+        self._index = i = k.get_device()
         self._c = _KvCache(F32 if k.dtype == torch.float32 else BF16, Hkv, dh, B, n_pages, page_size, max_pages,
-                           t(k, k.dtype, 0, "k"), t(v, k.dtype, 0, "v"), t(table, i32, 0, "table"), t(len, i32, B, "len"),
-                           t(pos, i32, slots, "pos"), t(seen, i32, B, "seen"), t(score, torch.float32, slots, "score"))
+                           _dev(k, k.dtype, 0, "k"), _dev_on(v, k.dtype, 0, "v", i), _dev_on(table, i32, 0, "table", i),
+                           _dev_on(len, i32, B, "len", i), _dev_on(pos, i32, slots, "pos", i), _dev_on(seen, i32, B, "seen", i),
+                           _dev_on(score, torch.float32, slots, "score", i))
         self._ref = C.byref(self._c)
         self._dtype, self._dims = k.dtype, (B, Hkv, dh)
         self.k, self.v, self.table, self.len, self.pos, self.seen, self.score = k, v, table, len, pos, seen, score
 
-    def _tensor(self, t, dtype, numel, name):
-        if t is not None and t.get_device() != self._index and t.is_cuda:
-            raise ValueError(f"{name}: must be on the cache's device")
-        return _dev(t, dtype, numel, name)
-
-    def _ws(self, ws):
-        if ws is not None and ws.get_device() != self._index and ws.is_cuda:
-            raise ValueError("ws: must be on the cache's device")
-        return _ws(ws)
-
     def _stream(self, stream):
-        if torch._C._cuda_getDevice() != self._index or (stream is not None and stream.device_index != self._index):
+        i = self._index
+        if torch._C._cuda_getDevice() != i or (stream is not None and stream.device_index != i):
             raise ValueError("the cache's device must be the current one, and the stream's")
-        return torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream.cuda_stream
+        return torch._C._cuda_getCurrentRawStream(i) if stream is None else stream.cuda_stream
 
 
 def kv_append(cache: KVCache, k_new, v_new, path=None, n_new=None, dev_status=None, stream=None):
@@ -513,10 +504,11 @@ def kv_append(cache: KVCache, k_new, v_new, path=None, n_new=None, dev_status=No
     B, Hkv, dh = cache._dims
     if len(shape) != 4 or shape[0] != B or shape[1] != Hkv or shape[3] != dh or v_new.shape != shape:
         raise ValueError("k_new and v_new: must be [B, Hkv, M, dh] of the cache")
-    M, t, dt, i32 = shape[2], cache._tensor, cache._dtype, torch.int32
+    M, i, dt, i32 = shape[2], cache._index, cache._dtype, torch.int32
     n = B * Hkv * M * dh
-    rc = _lib.moa_kv_append(cache._ref, t(k_new, dt, n, "k_new"), t(v_new, dt, n, "v_new"), M, t(path, i32, B * M, "path"),
-                            t(n_new, i32, B, "n_new"), t(dev_status, i32, 1, "dev_status"), cache._stream(stream))
+    rc = _lib.moa_kv_append(cache._ref, _dev_on(k_new, dt, n, "k_new", i), _dev_on(v_new, dt, n, "v_new", i), M,
+                            _dev_on(path, i32, B * M, "path", i), _dev_on(n_new, i32, B, "n_new", i),
+                            _dev_on(dev_status, i32, 1, "dev_status", i), cache._stream(stream))
     if rc:
         _check(rc)
 
@@ -533,11 +525,11 @@ def decode_attn(cache: KVCache, q, out, ws, accumulate=False, dev_status=None, s
     B, _, dh = cache._dims
     if len(shape) != 3 or shape[0] != B or shape[2] != dh:
         raise ValueError("q: must be [B, H, dh] of the cache")
-    H, t, dt = shape[1], cache._tensor, cache._dtype
+    H, i, dt = shape[1], cache._index, cache._dtype
     n = B * H * dh
-    wsp, wsb = cache._ws(ws)
-    rc = _lib.moa_decode_attn(cache._ref, H, t(q, dt, n, "q"), t(out, dt, n, "out"), 1 if accumulate else 0,
-                              t(dev_status, torch.int32, 1, "dev_status"), wsp, wsb, cache._stream(stream))
+    wsp, wsb = _room_on(ws, "ws", i)
+    rc = _lib.moa_decode_attn(cache._ref, H, _dev_on(q, dt, n, "q", i), _dev_on(out, dt, n, "out", i), 1 if accumulate else 0,
+                              _dev_on(dev_status, torch.int32, 1, "dev_status", i), wsp, wsb, cache._stream(stream))
     if rc:
         _check(rc)
 
@@ -550,8 +542,9 @@ def kv_evict_workspace_bytes(cache: KVCache, budget: int) -> int:
 
 def kv_evict(cache: KVCache, budget: int, recent: int, ws, dev_status=None, stream=None):
     """Sequences of more than `budget` slots are cut down to it: the `recent` newest tokens and those with the largest score stay."""
-    wsp, wsb = cache._ws(ws)
-    rc = _lib.moa_kv_evict(cache._ref, int(budget), int(recent), cache._tensor(dev_status, torch.int32, 1, "dev_status"), wsp, wsb,
+    i = cache._index
+    wsp, wsb = _room_on(ws, "ws", i)
+    rc = _lib.moa_kv_evict(cache._ref, int(budget), int(recent), _dev_on(dev_status, torch.int32, 1, "dev_status", i), wsp, wsb,
                            cache._stream(stream))
     if rc:
         _check(rc)

@@ -99,3 +99,62 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         moa.KVCache(k, k[:, :1], table, n)
     with pytest.raises(ValueError, match="dtype"):
         moa.KVCache(k.half(), k.half(), table, n)
+
+
+class OnGpu(torch.Tensor):
+    """Stands in for a tensor on the GPU with that index."""
+    is_cuda = True
+
+    def get_device(self):
+        return getattr(self, "at", 0)
+
+
+def on_gpu(*shape, dtype=torch.int32, at=0):
+    t = torch.zeros(*shape, dtype=dtype).as_subclass(OnGpu)
+    t.at = at
+    return t
+
+
+def test_checks_of_tensors_on_a_device():
+    t = on_gpu(4, 6, at=1)
+    assert binding._dev_on(t, torch.int32, 24, "x", 1) == t.data_ptr() and binding._dev_on(None, torch.int32, 24, "x", 1) is None
+    with pytest.raises(ValueError, match="x: must be on the cache's device"):
+        binding._dev_on(t, torch.int32, 24, "x", 0)
+    with pytest.raises(ValueError, match="x: 24 elements, the call touches 25"):
+        binding._dev_on(t, torch.int32, 25, "x", 1)
+    with pytest.raises(TypeError):
+        binding._dev_on(t, torch.int32, 24, "x")
+    w = on_gpu(100, dtype=torch.float32)
+    assert binding._room_on(w, "ws", 0) == (w.data_ptr(), 400) and binding._room_on(None, "ws", 0) == (None, 0)
+    for bad, at, error, text in ((w, 1, ValueError, "ws: must be on the cache's device"), (torch.zeros(4), 0, ValueError, "contiguous CUDA"),
+                                 (on_gpu(4, 6).t(), 0, ValueError, "contiguous CUDA"), (3, 0, TypeError, "expected a torch tensor")):
+        with pytest.raises(error, match=text):
+            binding._room_on(bad, "ws", at)
+    with pytest.raises(TypeError):
+        binding._room_on(w, "ws")
+
+
+def test_a_cache_has_its_tensors_on_one_device_and_of_one_kind():
+    k = on_gpu(4, 2, 16, 64, dtype=torch.bfloat16)
+    table, n, acc = on_gpu(1, 2), on_gpu(1), on_gpu(1, 2, 32, dtype=torch.float32)
+    moa.KVCache(k, k, table, n, pos=on_gpu(1, 2, 32), seen=on_gpu(1), score=acc)
+    for kw, text in ((dict(table=on_gpu(1, 2, at=1)), "table: must be on"), (dict(v=on_gpu(4, 2, 16, 64, dtype=torch.bfloat16, at=1)), "v: must be on"),
+                     (dict(len=on_gpu(1, dtype=torch.int64)), "len: dtype"), (dict(score=on_gpu(1, 2, 31, dtype=torch.float32)), "score: 62 elements"),
+                     (dict(pos=on_gpu(1, 2, 32, at=1)), "pos: must be on"), (dict(v=on_gpu(4, 2, 16, 64, dtype=torch.float32)), "v: dtype")):
+        d = dict(k=k, v=k, table=table, len=n, score=acc)
+        d.update(kw)
+        with pytest.raises(ValueError, match=text):
+            moa.KVCache(**d)
+
+
+def test_shapes_the_calls_refuse():
+    k = on_gpu(4, 2, 16, 64, dtype=torch.bfloat16)
+    c = moa.KVCache(k, k, on_gpu(1, 2), on_gpu(1))
+    new = lambda *shape: on_gpu(*shape, dtype=torch.bfloat16)
+    for kn, vn in ((new(1, 2, 64), new(1, 2, 64)), (new(2, 2, 1, 64), new(2, 2, 1, 64)), (new(1, 2, 1, 64), new(1, 2, 2, 64)),
+                   (new(1, 4, 1, 64), new(1, 4, 1, 64)), (new(1, 2, 1, 32), new(1, 2, 1, 32))):
+        with pytest.raises(ValueError, match="of the cache"):
+            moa.kv_append(c, kn, vn)
+    for q in (new(1, 4, 32), new(2, 4, 64), new(1, 256)):
+        with pytest.raises(ValueError, match="of the cache"):
+            moa.decode_attn(c, q, q, None)
