@@ -156,6 +156,28 @@ def test_a_query_that_is_no_number_stays_with_its_head(heads, bad):
     assert (out[2] == 0).all()
 
 
+@pytest.mark.parametrize("seed", range(60))
+def test_random_calls(seed):
+    rng = np.random.default_rng(1000 + seed)
+    dtype = "bf16" if seed % 3 else "f32"
+    Hkv, G = int(rng.integers(1, 9)), int(rng.choice([1, 2, 3, 4, 5, 8, 16, 17]))
+    dh = int(rng.choice([64, 128, 8 * rng.integers(1, 33), rng.integers(1, 257)]))
+    top = int(np.exp(rng.uniform(0, np.log(3000 if Hkv * dh > 400 else 9000))))
+    lens = rng.integers(0, top + 1, int(rng.integers(1, 8))).tolist()
+    lens[0] = top
+    c = Cache((Hkv * G, Hkv, dh, dtype), lens, int(rng.choice([1, 16, 64, top, rng.integers(2, 300)])), seed=seed, accounts=bool(rng.integers(0, 2)))
+    q = queries(c, seed)
+    what = f"{dtype} Hkv {Hkv} G {G} dh {dh} lens {lens} page {c.page}"
+    print(what, flush=True)
+    want, tol, weight, wtol = decode_reference(c, q)
+    if c.score is None:
+        check(run(c, q), want, tol, what)
+        return
+    before = c.score.cpu().double().numpy()
+    check(run(c, q, accumulate=True), want, tol, what)
+    check(c.score, before + weight, wtol + 2.0 ** -23 * (np.abs(before) + weight), "accounts")
+
+
 @pytest.mark.parametrize("heads", ["8b", "tiny"])
 def test_same_bits_again_and_on_another_stream(heads):
     c = Cache(HEADS[heads], [3000, 2, 777], 16, seed=13)
