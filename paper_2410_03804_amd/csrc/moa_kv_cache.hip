@@ -132,14 +132,16 @@ hipError_t launch_append(const AppendArgs &a, hipStream_t st)
 
 // ---------------------------------------------------------------- evict
 constexpr int EV_T = 1024, EV_BITS = 11, EV_BINS = 1 << EV_BITS, EV_KEYS = 32768;
+constexpr int EV_U = 4;                // rounds of 64 slots of a wavefront at a time
 
 struct EvictArgs {
     KvDev c;
     int budget, recent;
     int moves;                // room for moves per (sequence, KV head)
-    int keys;                 // that LDS holds: a multiple of 64 per wavefront
+    int keys;                 // that LDS holds: a multiple of EV_U rounds per wavefront
     int32_t *count;           // [B, Hkv]
     int32_t *dst, *src;       // [B, Hkv, moves]
+    uint32_t *spill;          // [B, Hkv, cap] the keys that LDS does not hold; NULL where it holds all
     FastDiv units;
 };
 
@@ -167,18 +169,18 @@ __device__ __forceinline__ uint32_t lanes_below(uint64_t mask)
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
 }
 
-// One workgroup per (sequence, KV head).  Every wavefront has a stretch of the slots, whose keys it keeps in LDS (where there are
-// more than that holds, those behind are read again whenever they are wanted).  The key of the last slot that stays is found
-// digit by digit from histograms (11, 11 and 10 bits; the newest, whose key is the largest there is, are only counted); slots
-// with a larger key stay, and of those with an equal one the lowest, which only matters in the one wavefront where the equal
-// ones that stay end.  Each wavefront then lists what its stretch frees below the budget and what stays beyond it; the i-th of
-// either are one move.
+// One workgroup per (sequence, KV head).  Every wavefront has a stretch of the slots, whose keys it keeps in LDS, or in the
+// workspace where there are more than that holds.  The key of the last slot that stays is found digit by digit from histograms
+// (11, 11 and 10 bits; the newest, whose key is the largest there is, are only counted); slots with a larger key stay, and of
+// those with an equal one the lowest, which only matters in the one wavefront where the equal ones that stay end.  Each
+// wavefront then lists what its stretch frees below the budget and what stays beyond it; the i-th of either are one move.
 // What bounds it is instructions, all of them on the one compute unit that has the pair, and a pass over 8 bytes a slot that it loads
 // alone.  64 pairs of up to 16384 slots: 34 us with keys in registers and every pass unrolled (33 KB of code, fetched for one
-// pass), 35 with loops but sums by shuffles, 19.9 now; 128 pairs of 2112 9.6 us.
+// pass), 35 with loops but sums by shuffles, 19.5 now; 128 pairs of 2112 9.6 us.  Eight pairs of 131072: 206 us with accounts and positions read again
+// in every pass, 149 with the keys in the workspace.
 __global__ __launch_bounds__(EV_T) void k_kv_evict_select(EvictArgs a)
 {
-    constexpr int NW = EV_T / 64, U = 4, UL = 8;         // rounds of 64 slots at a time: from LDS, from memory
+    constexpr int NW = EV_T / 64, U = EV_U, UL = 8;      // rounds at a time: keys, accounts
     static_assert(NW == 16 && EV_BINS == 2 * EV_T, "sum_before; two digits a thread");
     constexpr uint32_t NEWEST = 0xffffffffu;
     __shared__ __attribute__((aligned(8))) uint32_t hist[EV_BINS];
@@ -198,7 +200,9 @@ __global__ __launch_bounds__(EV_T) void k_kv_evict_select(EvictArgs a)
     const int64_t oldest = (int64_t)a.c.seen[b] - a.recent;
     const int seg = ((n + NW - 1) / NW + 63) / 64 * 64, s0 = wave * seg, s1 = min(s0 + seg, n), rounds = s1 > s0 ? (s1 - s0 + 63) / 64 : 0;
     const int room = a.keys / NW, here = min(rounds, room / 64);
-    uint32_t *const mine = keys + wave * room;
+    // (said to be in LDS: as one of two places to read a key from it would become an address of either kind)
+    __attribute__((address_space(3))) uint32_t *const mine = (__attribute__((address_space(3))) uint32_t *)keys + wave * room;
+    uint32_t *const spill = a.spill + (int64_t)bh * a.c.cap;
     auto tally = [&](uint32_t d) {
         // sixty-four equal accounts would wait for each other at one address
         const uint32_t d0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)d);
@@ -223,6 +227,7 @@ __global__ __launch_bounds__(EV_T) void k_kv_evict_select(EvictArgs a)
             const bool in = s0 + 64 * (j + q) + lane < s1;
             const uint32_t x = stay_key(w[q], p[q] >= oldest);
             if (j + q < here) mine[64 * (j + q) + lane] = x;
+            else if (in) __builtin_nontemporal_store(x, spill + s0 + 64 * (j + q) + lane);
             newest += __popcll(__ballot(in && x == NEWEST));
             if (in && x != NEWEST) tally(x >> 21);
         }
@@ -232,12 +237,17 @@ __global__ __launch_bounds__(EV_T) void k_kv_evict_select(EvictArgs a)
 #pragma unroll 1
         for (int j = 0; j < rounds; j += U) {
             uint32_t x[U];
+            if (j + U <= room / 64) {
 #pragma unroll
-            for (int q = 0; q < U; ++q) {
-                const int s = s0 + 64 * (j + q) + lane;
-                x[q] = 0;
-                if (j + q < here) x[q] = mine[64 * (j + q) + lane];
-                else if (s < s1) x[q] = stay_key(score[s], pos[s] >= oldest);
+                for (int q = 0; q < U; ++q) x[q] = mine[64 * (j + q) + lane];
+            } else {                                       // (written by this very thread)
+#pragma unroll
+                for (int q = 0; q < U; ++q) {
+                    const int s = s0 + 64 * (j + q) + lane;
+                    x[q] = 0;
+                    if (j + q < here) x[q] = mine[64 * (j + q) + lane];
+                    else if (s < s1) x[q] = __builtin_nontemporal_load(spill + s);
+                }
             }
 #pragma unroll
             for (int q = 0; q < U; ++q) f(s0 + 64 * (j + q), x[q], s0 + 64 * (j + q) + lane < s1);
@@ -439,7 +449,8 @@ int32_t moa_kv_evict_workspace_bytes(const moa_kv_cache_t *cache, int32_t budget
     if (budget < 1) return api_fail(MOA_ERR_RANGE, "kv_evict_workspace_bytes: budget < 1");
     const int64_t bh = (int64_t)cache->B * cache->n_kv_heads;
     const int moves = evict_moves(*cache, budget);
-    *bytes_host = moves > 0 ? (size_t)bh * 4 * (1 + 2 * (size_t)moves) : 0;
+    const size_t cap = (size_t)cache->max_pages * cache->page_size;
+    *bytes_host = moves > 0 ? (size_t)bh * 4 * (1 + 2 * (size_t)moves + (cap > EV_KEYS ? cap : 0)) : 0;
     return MOA_OK;
 }
 
@@ -462,9 +473,11 @@ int32_t moa_kv_evict(const moa_kv_cache_t *cache, int32_t budget, int32_t recent
     const bool wide = kv_rows16(*cache, {});
     const int64_t bh = (int64_t)cache->B * cache->n_kv_heads;
     const int moves = evict_moves(*cache, budget);
-    const int cap = cache->max_pages * cache->page_size, keys = cap < EV_KEYS ? (cap + EV_T - 1) / EV_T * EV_T : EV_KEYS;
+    const int cap = cache->max_pages * cache->page_size, whole = EV_U * EV_T;
+    const int keys = cap < EV_KEYS ? (cap + whole - 1) / whole * whole : EV_KEYS;
     int32_t *w = (int32_t *)ws;
     EvictArgs a = {KvDev(*cache, dev_status), budget, recent, moves, keys, w, w + bh, w + bh + bh * moves,
+                   cap > EV_KEYS ? (uint32_t *)(w + bh + 2 * bh * moves) : nullptr,
                    FastDiv((uint32_t)(wide ? cache->head_dim * es / 16 : cache->head_dim))};
     prof_set_site(S_KV_CACHE);
     hipStream_t st = (hipStream_t)stream;

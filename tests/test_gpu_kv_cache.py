@@ -156,7 +156,7 @@ def test_evict(heads, page, budget, recent):
     assert c.status.item() == 0
 
 
-@pytest.mark.parametrize("n,budget", [(1025, 1024), (16384, 2048), (33000, 100), (20001, 20000)])
+@pytest.mark.parametrize("n,budget", [(1025, 1024), (16384, 2048), (33000, 100), (20001, 20000), (70001, 5000), (40000, 39990)])
 def test_evict_long(n, budget):
     c = Cache((2, 2, 8, "f32"), [n, n // 2], 64, seed=n, accounts=True)
     want = evict_expected(c, budget, budget // 4, [n, n // 2])
