@@ -269,6 +269,56 @@ def test_decoding_loop():
     assert c.seen.tolist() == [n + 40 for n in n_new]
 
 
+def test_verified_tree_committed_and_decoded_on():
+    """A tree verified over the contiguous caches, its accepted nodes' keys and values committed by the path of the accept walk, the next
+    token decoded over the same caches as pages of their capacity, and these cut down to a budget."""
+    B, H, dh, M, cap = 2, 4, 64, 9, 330
+    lens, budget = [300, 17], 200
+    g = torch.Generator().manual_seed(51)
+    bf16, i32 = torch.bfloat16, torch.int32
+    rand = lambda *shape: torch.randn(shape, generator=g).to(bf16).cuda()
+    c = Cache((H, H, dh, "bf16"), lens, cap, seed=51, accounts=True, spare=0)
+    c.table = np.arange(B, dtype=np.int32)[:, None]
+    c.t_table = torch.from_numpy(c.table).cuda()
+    c.k, c.v = rand(B, H, cap, dh), rand(B, H, cap, dh)
+    parent = torch.tensor([[-1, 0, 0, 1, 1, 2, 3, 3, 6], [-1, 0, 0, 0, 1, 2, 3, 4, 5]], dtype=i32, device="cuda")
+    tok = torch.arange(B * M, dtype=i32, device="cuda").view(B, M)
+    tgt = torch.full((B, M), 99, dtype=i32, device="cuda")
+    for b, path in enumerate(([0, 1, 3, 6], [0, 2])):           # each node's successor on the path is the LLM's token
+        for x, y in zip(path, path[1:]):
+            tgt[b, x] = tok[b, y]
+    mask, depth = torch.zeros(B, M, 1, dtype=torch.int64, device="cuda"), torch.zeros(B, M, dtype=i32, device="cuda")
+    moa.tree_build(parent, mask, depth, c.status)
+    shape = moa.Shape(1, H * dh, H, H, dh, H * dh, H, H, moa.BF16)
+    x, out = rand(B, M, H * dh), torch.zeros(B, M, H * dh, dtype=bf16, device="cuda")
+    kt, vt = (torch.zeros(B, H, M, dh, dtype=bf16, device="cuda") for _ in range(2))
+    moa.tree_verify_attn(shape, x, None, None, None, None, c.k, c.v, c.t_len, cap, mask, out, kt, vt,
+                         workspace(moa.workspace_bytes(shape, B, cap, M, 0)), c.status)
+    path, n_path, bonus = torch.zeros(B, M, dtype=i32, device="cuda"), torch.zeros(B, dtype=i32, device="cuda"), torch.zeros(B, dtype=i32, device="cuda")
+    moa.tree_accept(parent, tok, tgt, path, n_path, bonus)
+    cache = c.moa()
+    want = append_reference(c, kt, vt, path.cpu().numpy(), n_path.tolist(), lens)
+    moa.kv_append(cache, kt, vt, path=path, n_new=n_path, dev_status=c.status)
+    same(state(c), want)
+    assert c.t_len.tolist() == [304, 19] and n_path.tolist() == [4, 2]
+    for b, nodes in enumerate(([0, 1, 3, 6], [0, 2])):          # (without projections a node's key is its own row)
+        assert torch.equal(c.k[b, :, lens[b]:lens[b] + len(nodes)], x[b, nodes].view(-1, H, dh).transpose(0, 1))
+    ws = workspace(max(moa.decode_attn_workspace_bytes(cache, H), moa.kv_evict_workspace_bytes(cache, budget)))
+    for step in range(2):                                       # over the whole cache, then over what eviction leaves
+        c.lens = c.t_len.tolist()
+        q = rand(B, H, dh)
+        o = torch.zeros_like(q)
+        before = c.score.cpu().double().numpy()
+        ref, tol, weight, wtol = decode_reference(c, q)
+        moa.decode_attn(cache, q, o, ws, accumulate=True, dev_status=c.status)
+        check(o, ref, tol, f"step {step}")
+        check(c.score, before + weight, wtol + 2.0 ** -23 * (np.abs(before) + weight), "accounts")
+        want = evict_expected(c, budget, 20, c.lens)
+        moa.kv_evict(cache, budget, 20, ws, dev_status=c.status)
+        same(state(c), want)
+    assert c.t_len.tolist() == [200, 19] and c.status.item() == 0
+
+
 def test_captured_step_replayed():
     """Append, decode and evict captured into one graph; each replay against the same calls made eagerly on a copy."""
     budget = 600
