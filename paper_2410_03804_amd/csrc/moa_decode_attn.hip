@@ -331,35 +331,33 @@ __device__ __forceinline__ void wait_loads()
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-constexpr uint32_t RAWB = WK * 16 * 4;        // a tile's scores
-
 // what rows that do not count are read from
 __device__ const u32x4 zero_row[32] = {};
 
 // tiles that a wavefront holds in LDS, and the bytes of that
 constexpr int decode_stages(int DH) { return DH == 64 ? 2 : 1; }
-constexpr uint32_t decode_wave_bytes(int DH, bool accounts)
+constexpr uint32_t decode_wave_bytes(int DH, int CT, bool accounts)
 {
-    return decode_stages(DH) * (2 * WK * DH * 2 + 256) + 128 + (accounts ? RAWB : 0);
+    return decode_stages(DH) * (2 * WK * DH * 2 + 256) + 128 + (accounts ? WK * 16 * CT * 4 : 0);      // (the last: a tile's scores)
 }
 
-// Sixteen query heads of a KV head are the columns of a tile: S^T = K Q^T, O^T += V^T P^T.  Every wavefront walks its own 32
+// Sixteen query heads of a KV head are the columns of a tile, CT of which are computed side by side: S^T = K Q^T, O^T += V^T P^T.  Every wavefront walks its own 32
 // keys of each tile of the run, with LDS of its own for NST tiles, so that there is no barrier before the run's end.  Keys and
 // values go straight into LDS: a tile's keys take the place of those NST tiles before as soon as these have been used, its
 // values likewise, and its table entries come another NST tiles before that.  Two workgroups share a compute unit (one at 256
 // dims), so that one loads while the other begins or ends a run.  (Rings of two tiles and one workgroup a compute unit: 8 x 32768 keys 181 us against
 // 180, 64 ragged sequences up to 8192 207 against 192, 96 of up to 100 16.7 against 11.1.)
 // DH: head_dim as it lies in LDS; the rows in the pool may be shorter (PAD, a multiple of 8): their last pieces are then zeros.
-template <int DH, bool PAD, bool ACC>
-__global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void k_decode_attn_mfma(DecodeArgs a)
+template <int DH, int CT, bool PAD, bool ACC>
+__global__ __launch_bounds__(256, DH == 256 || CT == 2 ? 1 : 2) void k_decode_attn_mfma(DecodeArgs a)
 {
     constexpr int ROWB = DH * 2, PIECES = ROWB / 16, RPI = 64 / PIECES, NL = WK / RPI;   // bytes and 16-byte pieces of a row; rows of a load, loads of K (or V)
     constexpr int NST = decode_stages(DH), NKS = DH / 32, NDB = DH / 16;
-    constexpr uint32_t HALFB = WK * ROWB, STAGEB = 2 * HALFB, IDB = 256, WAVEB = decode_wave_bytes(DH, ACC);
+    constexpr uint32_t HALFB = WK * ROWB, STAGEB = 2 * HALFB, IDB = 256, WAVEB = decode_wave_bytes(DH, CT, ACC);
     constexpr int PERTILE = 2 * NL + 1;                          // loads of a tile: keys, table entries for NST tiles later, values
     constexpr int BEHIND_K = (NST - 1) * PERTILE + NL, BEHIND_V = (NST - 1) * PERTILE + NL + 1;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    __shared__ float ml_s[WAVES * 16 * 2], fin[16 * 2];
+    __shared__ float ml_s[WAVES * 16 * CT * 2], fin[16 * CT * 2];
     const int tid = threadIdx.x, lane = tid & 63, n16 = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int dh = PAD ? a.c.dh : DH;
@@ -374,7 +372,7 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void k_decode_attn_mfma(Dec
     auto swz = [](int p) { return DH >= 128 ? 4 * (p & 3) + ((p >> 2) & 3) : (((p >> 1) & 3) << 1) | ((p >> 3) & 1); };
 
     for_each_pair(a, [&](int b, int len, int hb, uint32_t t0, uint32_t nt, bool whole, int64_t slot) {
-        const int h = hb / a.rtiles, r0 = (hb - h * a.rtiles) * 16, rows = min(16, a.G - r0);
+        const int h = hb / a.rtiles, r0 = (hb - h * a.rtiles) * 16 * CT, rows = min(16 * CT, a.G - r0);
         const int cnt = (int)nt, key0 = (int)t0 * TK + wave * WK;
         const int32_t *table = a.c.table + (int64_t)b * a.c.max_pages;
         const bf16_t *q0 = (const bf16_t *)a.q + ((int64_t)b * a.H + h * a.G + r0) * dh;
@@ -420,21 +418,30 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void k_decode_attn_mfma(Dec
 #pragma unroll
             for (int i = 0; i < NST; ++i) fetch_ids(i);
         }
-        bf16x8 qf[NKS];
+        bf16x8 qf[CT][NKS];
 #pragma unroll
-        for (int ks = 0; ks < NKS; ++ks) {
-            const int d = 32 * ks + 8 * quad;
-            union { u32x4 u; bf16x8 v; } x;
-            x.u = u32x4{0u, 0u, 0u, 0u};
-            if (!PAD || d < dh) x.u = *(const u32x4 *)(q0 + min(n16, rows - 1) * dh + d);
-            qf[ks] = x.v;
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks) {
+                const int d = 32 * ks + 8 * quad;
+                union { u32x4 u; bf16x8 v; } x;
+                x.u = u32x4{0u, 0u, 0u, 0u};
+                if (!PAD || d < dh) x.u = *(const u32x4 *)(q0 + min(16 * ct + n16, rows - 1) * dh + d);
+                qf[ct][ks] = x.v;
+            }
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks) asm volatile("" : "+v"(qf[ct][ks]));       // waited for here, not among the loads below
+        f32x4 acc[CT][NDB];
+        float mref[CT], lsum[CT];                           // reference of the exponent (log2 domain); this lane's part of the sum
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+#pragma unroll
+            for (int d = 0; d < NDB; ++d) acc[ct][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+            mref[ct] = -INFINITY;
+            lsum[ct] = 0.f;
         }
-#pragma unroll
-        for (int ks = 0; ks < NKS; ++ks) asm volatile("" : "+v"(qf[ks]));       // waited for here, not among the loads below
-        f32x4 acc[NDB];
-#pragma unroll
-        for (int d = 0; d < NDB; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-        float mref = -INFINITY, lsum = 0.f;                                     // reference of the exponent (log2 domain); this lane's part of the sum
 
         uint32_t ok[NST];
         if (cnt > 0) {
@@ -459,31 +466,40 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void k_decode_attn_mfma(Dec
                 const bool next = i + NST < cnt;
                 if (i + NST <= cnt) wait_loads<BEHIND_K>();
                 else wait_loads<0>();
-                f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+                f32x4 s[CT][2];
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) s[ct][0] = s[ct][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int ks = 0; ks < NKS; ++ks)
 #pragma unroll
                     for (int hf = 0; hf < 2; ++hf) {
                         const int p = 16 * hf + n16;
                         const bf16x8 kf = *(const __attribute__((address_space(3))) bf16x8 *)(uintptr_t)(kb + p * ROWB + 16 * ((4 * ks + quad) ^ swz(p)));
-                        s[hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[ks], s[hf], 0, 0, 0);
+#pragma unroll
+                        for (int ct = 0; ct < CT; ++ct) s[ct][hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[ct][ks], s[ct][hf], 0, 0, 0);
                     }
-                float x[8], tm = -INFINITY;
+                float x[CT][8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * a.scale;
-                if (count != 0xffffffffu) {
+                for (int ct = 0; ct < CT; ++ct) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (!(count >> key_of(e) & 1u)) x[e] = -INFINITY;
+                    for (int e = 0; e < 8; ++e) x[ct][e] = s[ct][e >> 2][e & 3] * a.scale;
+                    if (count != 0xffffffffu) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (!(count >> key_of(e) & 1u)) x[ct][e] = -INFINITY;
+                    }
                 }
                 // (in front of the next loads, so that nobody waits for these with the stores.  The stores are most of what accounts
                 // cost: 8 x 8192 keys, 8 query heads per KV head, 49.5 us without, 59.5 with, 52 with all but the stores.)
                 if (ACC && key0 + i * TK < len) {
                     // through LDS, where a tile's scores lie as they do in memory
-                    if (n16 < rows) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) *(__attribute__((address_space(3))) float *)(uintptr_t)(raw0 + (key_of(e) * a.HG + n16) * 4) = x[e];
-                    }
+                    for (int ct = 0; ct < CT; ++ct)
+                        if (16 * ct + n16 < rows) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                *(__attribute__((address_space(3))) float *)(uintptr_t)(raw0 + (key_of(e) * a.HG + 16 * ct + n16) * 4) = x[ct][e];
+                        }
                     float *raw = a.raw + (((int64_t)b * a.HB + hb) * a.cap32 + key0 + i * TK) * a.HG;
                     for (int at = 4 * lane; at < WK * a.HG; at += 256)
                         *(u32x4 *)(raw + at) = *(const __attribute__((address_space(3))) u32x4 *)(uintptr_t)(raw0 + at * 4);
@@ -493,28 +509,33 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void k_decode_attn_mfma(Dec
                     fetch(a.c.k, kb);
                     fetch_ids(i + 2 * NST);
                 }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) tm = fmaxf(tm, x[e]);
-                if (__ballot(tm > mref)) {
-                    tm = over_lanes<4>(tm, fmaxf);
-                    const float mnew = fmaxf(mref, tm), corr = mnew == -INFINITY ? 1.f : fast_exp2(mref - mnew);
-                    mref = mnew;
-                    lsum *= corr;
-#pragma unroll
-                    for (int d = 0; d < NDB; ++d)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[d][e] *= corr;
-                }
-                const float ms = mref == -INFINITY ? 0.f : mref;
                 // A weight as the sum of two bf16 numbers, so that it counts with 2^-16 like in single precision: the matrix
                 // cores have nothing else to do, and one bf16 alone (2^-8) would double the result's own rounding.
-                union { uint32_t w[4]; bf16x8 v; } hi, lo;
+                union { uint32_t w[4]; bf16x8 v; } hi[CT], lo[CT];
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const float p0 = fast_exp2(x[e] - ms), p1 = fast_exp2(x[e + 1] - ms);
-                    lsum += p0 + p1;
-                    hi.w[e / 2] = pack_bf16x2(p0, p1);
-                    lo.w[e / 2] = pack_bf16x2(p0 - __uint_as_float(hi.w[e / 2] << 16), p1 - __uint_as_float(hi.w[e / 2] & 0xffff0000u));
+                for (int ct = 0; ct < CT; ++ct) {
+                    float tm = -INFINITY;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) tm = fmaxf(tm, x[ct][e]);
+                    if (__ballot(tm > mref[ct])) {
+                        tm = over_lanes<4>(tm, fmaxf);
+                        const float mnew = fmaxf(mref[ct], tm), corr = mnew == -INFINITY ? 1.f : fast_exp2(mref[ct] - mnew);
+                        mref[ct] = mnew;
+                        lsum[ct] *= corr;
+#pragma unroll
+                        for (int d = 0; d < NDB; ++d)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[ct][d][e] *= corr;
+                    }
+                    const float ms = mref[ct] == -INFINITY ? 0.f : mref[ct];
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const float p0 = fast_exp2(x[ct][e] - ms), p1 = fast_exp2(x[ct][e + 1] - ms);
+                        lsum[ct] += p0 + p1;
+                        const uint32_t w = pack_bf16x2(p0, p1);
+                        hi[ct].w[e / 2] = w;
+                        lo[ct].w[e / 2] = pack_bf16x2(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xffff0000u));
+                    }
                 }
                 if (next) wait_loads<BEHIND_V>();
                 else wait_loads<0>();
@@ -528,21 +549,28 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 2) void k_decode_attn_mfma(Dec
                         u.h[hf] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(uintptr_t)(
                             vb + p * ROWB + 16 * ((2 * d + ((n16 & 3) >> 1)) ^ swz(p)) + 8 * (n16 & 1)));
                     }
-                    acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u.v, hi.v, acc[d], 0, 0, 0);
-                    acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u.v, lo.v, acc[d], 0, 0, 0);
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) {
+                        acc[ct][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u.v, hi[ct].v, acc[ct][d], 0, 0, 0);
+                        acc[ct][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u.v, lo[ct].v, acc[ct][d], 0, 0, 0);
+                    }
                 }
                 if (next) fetch(a.c.v, vb);
             }
         wait_loads<0>();
-        lsum = over_lanes<4>(lsum, add);
         float *acc_s = (float *)mine;                              // the stages are free again
-        if (n16 < rows) {
 #pragma unroll
-            for (int d = 0; d < NDB; ++d)
-                if (!PAD || 16 * d + 4 * quad < dh) *(f32x4 *)(acc_s + n16 * dh + 16 * d + 4 * quad) = acc[d];
-            if (quad == 0) {
-                ml_s[(wave * a.HG + n16) * 2] = mref;
-                ml_s[(wave * a.HG + n16) * 2 + 1] = lsum;
+        for (int ct = 0; ct < CT; ++ct) {
+            const float l = over_lanes<4>(lsum[ct], add);
+            const int r = 16 * ct + n16;
+            if (r < rows) {
+#pragma unroll
+                for (int d = 0; d < NDB; ++d)
+                    if (!PAD || 16 * d + 4 * quad < dh) *(f32x4 *)(acc_s + r * dh + 16 * d + 4 * quad) = acc[ct][d];
+                if (quad == 0) {
+                    ml_s[(wave * a.HG + r) * 2] = mref[ct];
+                    ml_s[(wave * a.HG + r) * 2 + 1] = l;
+                }
             }
         }
         finish<bf16_t, PAD ? 0 : DH>(a, b, len, hb, whole, slot, (const float *)smem, WAVEB / 4, ml_s, fin);
@@ -556,7 +584,7 @@ constexpr int ACC_SLOTS = 256;
 template <typename T>
 __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
 {
-    __shared__ float sm[2][16][16], fin[16][2];
+    __shared__ float sm[2][32][8], fin[32][2];
     __shared__ __attribute__((aligned(16))) float part[1024];
     const int tid = threadIdx.x, lane = tid & 63, dh = a.c.dh;
     const int nb = a.c.B * a.H;
@@ -576,16 +604,16 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
     }
     // this thread's account and scores, while the lengths are on their way (where there are several row tiles, those of the first)
     const int mine = chunk * ACC_SLOTS + tid;
-    float score = 0.f, weight = 0.f, raw[16];
+    float score = 0.f, weight = 0.f, raw[32];
     auto load_raw = [&](int rt) {
         const float *p = a.raw + ((((int64_t)b * a.HB + h * a.rtiles + rt)) * a.cap32 + mine) * a.HG;
         if ((a.HG & 3) == 0) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int q = 0; q < 8; ++q)
                 if (4 * q < a.HG) *(f32x4 *)(raw + 4 * q) = *(const f32x4 *)(p + 4 * q);
         } else {
 #pragma unroll
-            for (int q = 0; q < 16; ++q)
+            for (int q = 0; q < 32; ++q)
                 if (q < a.HG) raw[q] = p[q];
         }
     };
@@ -680,19 +708,19 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
         const int r0 = rt * a.HG, rows = min(a.HG, a.G - r0);
         runs_of(rt, w0, ns, slot0);
         if (ns == 1 && a.rtiles == 1) return;                // the first launch had all of it
-        // of each row the maximum and the sum: sixteen threads a row
-        const int row = tid & 15, p = tid >> 4;
+        // of each row the maximum and the sum: eight threads a row
+        const int row = tid & 31, p = tid >> 5;
         float m = -INFINITY, l = 0.f;
         if (row < rows)
-            for (uint32_t s = p; s < ns; s += 16) m = fmaxf(m, a.part_ml[((slot0 + s) * a.HG + row) * 2]);
+            for (uint32_t s = p; s < ns; s += 8) m = fmaxf(m, a.part_ml[((slot0 + s) * a.HG + row) * 2]);
         __syncthreads();
         sm[0][row][p] = m;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) m = fmaxf(m, sm[0][row][i]);
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, sm[0][row][i]);
         const float ms = m == -INFINITY ? 0.f : m;
         if (row < rows)
-            for (uint32_t s = p; s < ns; s += 16) {
+            for (uint32_t s = p; s < ns; s += 8) {
                 const float *ml = a.part_ml + ((slot0 + s) * a.HG + row) * 2;
                 l += ml[1] * fast_exp2(ml[0] - ms);
             }
@@ -701,7 +729,7 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
         if (p == 0) {
             l = 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) l += sm[1][row][i];
+            for (int i = 0; i < 8; ++i) l += sm[1][row][i];
             fin[row][0] = ms;
             fin[row][1] = l == 0.f ? 0.f : 1.f / l;
         }
@@ -709,7 +737,7 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
         if (mine < len) {
             if (rt > 0) load_raw(rt);
 #pragma unroll
-            for (int q = 0; q < 16; ++q)
+            for (int q = 0; q < 32; ++q)
                 if (q < rows) weight += fast_exp2(raw[q] - fin[q][0]) * fin[q][1];
         }
     }
@@ -738,7 +766,11 @@ DecodePlan decode_plan(const moa_kv_cache_t &c, int H, bool accounts, bool mfma)
     const int G = H / c.n_kv_heads, cap = c.max_pages * c.page_size;
     p.mfma = mfma;
     p.wide = c.dtype == MOA_F32 && kv_rows16(c, {});
-    p.HG = p.mfma ? (G < 16 ? G : 16) : G <= 2 || !p.wide ? 2 : G <= 4 ? 4 : 8;
+    // On the matrix cores 32 query heads share a pass over the keys where there is enough of it, and 16 where more runs are wanted (or
+    // two tiles of columns do not fit the registers).  32 heads on one KV head, us, 16 a pass against 32: 1 x 8000 keys 8.6, 12.8; 16 x
+    // 8000 25.7, 26.0, and with 64 heads 39.4, 33; 64 x 8000 68.5, 45.5; 64 x 32000 312, 168.
+    const int most = c.head_dim <= 128 && (int64_t)c.B * c.n_kv_heads * ((cap + TK - 1) / TK) >= 512 ? 32 : 16;
+    p.HG = p.mfma ? (G < most ? G : most) : G <= 2 || !p.wide ? 2 : G <= 4 ? 4 : 8;
     p.rtiles = (G + p.HG - 1) / p.HG;
     const int64_t pairs = (int64_t)c.B * c.n_kv_heads * p.rtiles;
     // One workgroup per pair, without a second launch (4 us), where that is a short walk, or not a long one and there are pairs
@@ -748,7 +780,7 @@ DecodePlan decode_plan(const moa_kv_cache_t &c, int H, bool accounts, bool mfma)
     // Half and twice as many runs: 64 ragged sequences up to 8192 181 and 176 against 173, 8 x 32768 158 and 164 against 158; single
     // precision 4 x 32000 28.1 and 27.3 against 23.7.
     const int64_t walk = p.mfma ? pairs >= 512 ? 1024 : 512 : 256;
-    p.runs = cap <= walk && !(accounts && p.rtiles > 1) ? 0 : !p.mfma ? 1024 : c.head_dim <= 128 ? 512 : 256;
+    p.runs = cap <= walk && !(accounts && p.rtiles > 1) ? 0 : !p.mfma ? 1024 : c.head_dim <= 128 && p.HG <= 16 ? 512 : 256;
     p.part_o = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * c.head_dim * 4) : 0;
     p.part_ml = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * 2 * 4) : 0;
     p.cap32 = (cap + 31) & ~31;
@@ -778,24 +810,32 @@ hipError_t launch_one(const DecodeArgs &a, int grid, hipStream_t st)
     return hipGetLastError();
 }
 
-template <int DH, bool PAD, bool ACC>
+template <int DH, int CT, bool PAD, bool ACC>
 hipError_t launch_mfma(const DecodeArgs &a, int grid, hipStream_t st)
 {
-    constexpr size_t lds = (size_t)WAVES * decode_wave_bytes(DH, ACC);
+    constexpr size_t lds = (size_t)WAVES * decode_wave_bytes(DH, CT, ACC);
     static bool raised[16] = {};
-    hipError_t e = raise_lds_limit_once(raised, (const void *)k_decode_attn_mfma<DH, PAD, ACC>, lds);
+    hipError_t e = raise_lds_limit_once(raised, (const void *)k_decode_attn_mfma<DH, CT, PAD, ACC>, lds);
     if (e != hipSuccess) return e;
     prof_begin(K_DECODE_ATTN_MFMA, st);
-    MOA_KLAUNCH((k_decode_attn_mfma<DH, PAD, ACC>), dim3(grid), dim3(64 * WAVES), lds, st, a);
+    MOA_KLAUNCH((k_decode_attn_mfma<DH, CT, PAD, ACC>), dim3(grid), dim3(64 * WAVES), lds, st, a);
     prof_end(st);
     return hipGetLastError();
+}
+
+template <int DH, int CT>
+hipError_t launch_mfma(const DecodeArgs &a, int grid, hipStream_t st)
+{
+    if (a.c.dh == DH) return a.raw ? launch_mfma<DH, CT, false, true>(a, grid, st) : launch_mfma<DH, CT, false, false>(a, grid, st);
+    return a.raw ? launch_mfma<DH, CT, true, true>(a, grid, st) : launch_mfma<DH, CT, true, false>(a, grid, st);
 }
 
 template <int DH>
 hipError_t launch_mfma(const DecodeArgs &a, int grid, hipStream_t st)
 {
-    if (a.c.dh == DH) return a.raw ? launch_mfma<DH, false, true>(a, grid, st) : launch_mfma<DH, false, false>(a, grid, st);
-    return a.raw ? launch_mfma<DH, true, true>(a, grid, st) : launch_mfma<DH, true, false>(a, grid, st);
+    if constexpr (DH <= 128)
+        if (a.HG > 16) return launch_mfma<DH, 2>(a, grid, st);
+    return launch_mfma<DH, 1>(a, grid, st);
 }
 
 template <typename T, int HG, bool WIDE>

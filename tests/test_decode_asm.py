@@ -22,6 +22,6 @@ def test_gathers_have_their_wait_state_and_the_counts_hold():
         assert lines[i - 1] == "s_nop 0" and re.fullmatch(r"s_mov_b32 m0, \w+", lines[i - 2]), lines[i - 2:i + 1]
     assert sum(bool(re.search(r"\bm0\b", l)) for l in lines) == len(loads)
     bodies = re.findall(r"^(\S*k_decode_attn_mfma\S*):(.*?)s_endpgm.*?\.section", asm, flags=re.S | re.M)
-    assert len(bodies) == 12
+    assert len(bodies) == 20
     for name, body in bodies:
         assert "scratch_" not in body and "flat_" not in body, name

@@ -13,6 +13,7 @@ HEADS = {
     "g20": (20, 1, 128, "bf16"), "g32": (64, 2, 64, "bf16"), "g9f": (9, 1, 128, "f32"), "d80": (6, 2, 80, "bf16"),
     "d33f": (5, 5, 33, "f32"), "d33": (3, 1, 33, "bf16"), "d256f": (2, 1, 256, "f32"), "d256": (8, 2, 256, "bf16"), "d1": (2, 2, 1, "f32"),
     "g16": (16, 1, 128, "bf16"), "g9": (9, 1, 64, "bf16"), "d8": (4, 1, 8, "bf16"), "d72": (8, 2, 72, "bf16"), "d96": (12, 2, 96, "bf16"), "d120": (7, 1, 120, "bf16"), "d56": (4, 4, 56, "bf16"), "g3f": (6, 2, 100, "f32"), "d192": (4, 4, 192, "bf16"), "d136": (10, 1, 136, "bf16"), "d248": (18, 1, 248, "bf16"),
+    "g64": (64, 1, 128, "bf16"), "g33": (33, 1, 64, "bf16"), "g31d256": (31, 1, 256, "bf16"), "g24d72": (48, 2, 72, "bf16"),
     "d255": (3, 1, 255, "bf16"), "d130": (4, 2, 130, "bf16"),
 }
 LENS = {
@@ -58,7 +59,9 @@ def test_page_sizes(heads, page):
     assert c.status.item() == 0
 
 
-@pytest.mark.parametrize("heads,lens,page", [("8b", [33001], 64), ("g8", [16385, 9], 16), ("tiny", [20000, 1, 4097], 16)])
+@pytest.mark.parametrize("heads,lens,page", [("8b", [33001], 64), ("g8", [16385, 9], 16), ("tiny", [20000, 1, 4097], 16),
+                                             ("g32", [30000, 900, 0], 16), ("g33", [40000, 3, 1025, 129], 64), ("g24d72", [17000, 17000, 5, 0], 50),
+                                             ("g64", [33001, 31, 32, 900], 128)])
 def test_long(heads, lens, page):
     c = Cache(HEADS[heads], lens, page, seed=3)
     q = queries(c, 3)
@@ -78,7 +81,8 @@ def test_many_sequences(heads):
 
 
 @pytest.mark.parametrize("lens", [[1], [300, 0, 17], [2100, 1, 0, 640], [129]])
-@pytest.mark.parametrize("heads", ["8b", "tiny", "g20", "g32", "g9f", "d80", "mha64", "g16", "g9", "d33", "d72", "d256", "d248", "d255"])
+@pytest.mark.parametrize("heads", ["8b", "tiny", "g20", "g32", "g9f", "d80", "mha64", "g16", "g9", "d33", "d72", "d256", "d248", "d255", "g64", "g33",
+                                   "g31d256", "g24d72"])
 def test_accounts(heads, lens):
     c = Cache(HEADS[heads], lens, 16, seed=7, accounts=True)
     q = queries(c, 7)
@@ -89,6 +93,16 @@ def test_accounts(heads, lens):
     check(c.score, before + weight, wtol + 2.0 ** -23 * (np.abs(before) + weight), f"accounts {heads} {lens}")
     for b, n in enumerate(lens):
         assert np.array_equal(c.score.cpu().numpy()[b, :, n:], before[b, :, n:].astype(np.float32))
+
+
+@pytest.mark.parametrize("heads,lens", [("g64", [33000, 31, 0, 1500]), ("g32", [30000, 900, 3]), ("g33", [33100, 5, 1025, 129]), ("8b", [9000, 1, 3000])])
+def test_accounts_of_long_sequences(heads, lens):
+    c = Cache(HEADS[heads], lens, 64, seed=23, accounts=True)
+    q = queries(c, 23)
+    before = c.score.cpu().double().numpy()
+    want, tol, weight, wtol = decode_reference(c, q)
+    check(run(c, q, accumulate=True), want, tol, f"{heads} {lens}")
+    check(c.score, before + weight, wtol + 2.0 ** -23 * (np.abs(before) + weight), "accounts")
 
 
 def test_accounts_are_left_alone_without_accumulate():
@@ -160,7 +174,7 @@ def test_a_query_that_is_no_number_stays_with_its_head(heads, bad):
 def test_random_calls(seed):
     rng = np.random.default_rng(1000 + seed)
     dtype = "bf16" if seed % 3 else "f32"
-    Hkv, G = int(rng.integers(1, 9)), int(rng.choice([1, 2, 3, 4, 5, 8, 16, 17]))
+    Hkv, G = int(rng.integers(1, 9)), int(rng.choice([1, 2, 3, 4, 5, 8, 16, 17, 32, 40]))
     dh = int(rng.choice([64, 128, 8 * rng.integers(1, 33), rng.integers(1, 257)]))
     top = int(np.exp(rng.uniform(0, np.log(3000 if Hkv * dh > 400 else 9000))))
     lens = rng.integers(0, top + 1, int(rng.integers(1, 8))).tolist()
