@@ -467,11 +467,22 @@ for _n in _SYMBOLS[-5:]:
     getattr(_lib, _n).restype = C.c_int32
 
 
+def _int32(n, name) -> int:
+    """ctypes would keep the low 32 bits of any other number."""
+    n = int(n)
+    if not -2**31 <= n < 2**31:
+        raise ValueError(f"{name}: {n} does not fit 32 bits")
+    return n
+
+
 class KVCache:
     """moa_kv_cache_t: a KV cache in pages.  k, v [n_pages, Hkv, page_size, dh]; table [B, max_pages], len [B], optionally pos
     [B, Hkv, max_pages * page_size] with seen [B], score [B, Hkv, max_pages * page_size] (fp32; all others int32).  The tensors
     are checked here, once, and kept alive; their contents belong to the caller.  A contiguous cache [B, Hkv, P_cap, dh] is
     KVCache(k, v, torch.arange(B)[:, None], prefix_len).  Calls on it are made with its device as the current one."""
+
+    # (not to be replaced: the description that the calls get has the addresses of these)
+    k, v, table, len, pos, seen, score = (property(lambda self, i=i: self._tensors[i]) for i in range(7))
 
     def __init__(self, k, v, table, len, pos=None, seen=None, score=None):
         n_pages, Hkv, page_size, dh = k.shape
@@ -482,13 +493,13 @@ class KVCache:
             raise ValueError(f"k: dtype {k.dtype}, expected float32 or bfloat16")
         i32, slots = torch.int32, B * Hkv * max_pages * page_size
         self._index = i = k.get_device()
-        self._c = _KvCache(F32 if k.dtype == torch.float32 else BF16, Hkv, dh, B, n_pages, page_size, max_pages,
+        self._c = _KvCache(F32 if k.dtype == torch.float32 else BF16, *(_int32(n, "the cache's dimensions") for n in (Hkv, dh, B, n_pages, page_size, max_pages)),
                            _dev(k, k.dtype, 0, "k"), _dev_on(v, k.dtype, 0, "v", i), _dev_on(table, i32, 0, "table", i),
                            _dev_on(len, i32, B, "len", i), _dev_on(pos, i32, slots, "pos", i), _dev_on(seen, i32, B, "seen", i),
                            _dev_on(score, torch.float32, slots, "score", i))
         self._ref = C.byref(self._c)
         self._dtype, self._dims = k.dtype, (B, Hkv, dh)
-        self.k, self.v, self.table, self.len, self.pos, self.seen, self.score = k, v, table, len, pos, seen, score
+        self._tensors = k, v, table, len, pos, seen, score
 
     def _stream(self, stream):
         i = self._index
@@ -504,7 +515,7 @@ def kv_append(cache: KVCache, k_new, v_new, path=None, n_new=None, dev_status=No
     B, Hkv, dh = cache._dims
     if len(shape) != 4 or shape[0] != B or shape[1] != Hkv or shape[3] != dh or v_new.shape != shape:
         raise ValueError("k_new and v_new: must be [B, Hkv, M, dh] of the cache")
-    M, i, dt, i32 = shape[2], cache._index, cache._dtype, torch.int32
+    M, i, dt, i32 = _int32(shape[2], "M"), cache._index, cache._dtype, torch.int32
     n = B * Hkv * M * dh
     rc = _lib.moa_kv_append(cache._ref, _dev_on(k_new, dt, n, "k_new", i), _dev_on(v_new, dt, n, "v_new", i), M,
                             _dev_on(path, i32, B * M, "path", i), _dev_on(n_new, i32, B, "n_new", i),
@@ -515,7 +526,7 @@ def kv_append(cache: KVCache, k_new, v_new, path=None, n_new=None, dev_status=No
 
 def decode_attn_workspace_bytes(cache: KVCache, n_q_heads: int) -> int:
     out = _sz(0)
-    _check(_lib.moa_decode_attn_workspace_bytes(cache._ref, int(n_q_heads), C.byref(out)))
+    _check(_lib.moa_decode_attn_workspace_bytes(cache._ref, _int32(n_q_heads, "n_q_heads"), C.byref(out)))
     return int(out.value)
 
 
@@ -525,7 +536,7 @@ def decode_attn(cache: KVCache, q, out, ws, accumulate=False, dev_status=None, s
     B, _, dh = cache._dims
     if len(shape) != 3 or shape[0] != B or shape[2] != dh:
         raise ValueError("q: must be [B, H, dh] of the cache")
-    H, i, dt = shape[1], cache._index, cache._dtype
+    H, i, dt = _int32(shape[1], "H"), cache._index, cache._dtype
     n = B * H * dh
     wsp, wsb = _room_on(ws, "ws", i)
     rc = _lib.moa_decode_attn(cache._ref, H, _dev_on(q, dt, n, "q", i), _dev_on(out, dt, n, "out", i), 1 if accumulate else 0,
@@ -536,7 +547,7 @@ def decode_attn(cache: KVCache, q, out, ws, accumulate=False, dev_status=None, s
 
 def kv_evict_workspace_bytes(cache: KVCache, budget: int) -> int:
     out = _sz(0)
-    _check(_lib.moa_kv_evict_workspace_bytes(cache._ref, int(budget), C.byref(out)))
+    _check(_lib.moa_kv_evict_workspace_bytes(cache._ref, _int32(budget, "budget"), C.byref(out)))
     return int(out.value)
 
 
@@ -544,7 +555,7 @@ def kv_evict(cache: KVCache, budget: int, recent: int, ws, dev_status=None, stre
     """Sequences of more than `budget` slots are cut down to it: the `recent` newest tokens and those with the largest score stay."""
     i = cache._index
     wsp, wsb = _room_on(ws, "ws", i)
-    rc = _lib.moa_kv_evict(cache._ref, int(budget), int(recent), _dev_on(dev_status, torch.int32, 1, "dev_status", i), wsp, wsb,
+    rc = _lib.moa_kv_evict(cache._ref, _int32(budget, "budget"), _int32(recent, "recent"), _dev_on(dev_status, torch.int32, 1, "dev_status", i), wsp, wsb,
                            cache._stream(stream))
     if rc:
         _check(rc)

@@ -158,3 +158,34 @@ def test_shapes_the_calls_refuse():
     for q in (new(1, 4, 32), new(2, 4, 64), new(1, 256)):
         with pytest.raises(ValueError, match="of the cache"):
             moa.decode_attn(c, q, q, None)
+
+
+def test_numbers_beyond_32_bits_are_refused_not_wrapped(monkeypatch):
+    monkeypatch.setattr(moa.KVCache, "_stream", lambda self, stream: None)     # (nothing gets as far as a launch)
+    k = on_gpu(4, 2, 16, 64, dtype=torch.bfloat16)
+    c = moa.KVCache(k, k, on_gpu(1, 2), on_gpu(1), pos=on_gpu(1, 2, 32), seen=on_gpu(1), score=on_gpu(1, 2, 32, dtype=torch.float32))
+    for budget, recent in ((2 ** 32 + 1000, 0), (-2 ** 32 + 1000, 0), (1000, 2 ** 32), (1000, -2 ** 32)):
+        with pytest.raises(ValueError, match="32 bits"):
+            moa.kv_evict(c, budget, recent, None)
+    for call in (moa.kv_evict_workspace_bytes, moa.decode_attn_workspace_bytes):
+        with pytest.raises(ValueError, match="32 bits"):
+            call(c, 2 ** 32 + 4)
+    many = torch.zeros(1, dtype=torch.bfloat16).expand(2 ** 32 + 4, 1, 1, 1).as_subclass(OnGpu)
+    with pytest.raises(ValueError, match="32 bits"):
+        moa.KVCache(many, many, on_gpu(1, 2), on_gpu(1))
+    one = on_gpu(4, 1, 16, 1, dtype=torch.bfloat16)
+    c = moa.KVCache(one, one, on_gpu(1, 2), on_gpu(1))
+    with pytest.raises(ValueError, match="32 bits"):
+        moa.kv_append(c, many.view(1, 1, -1, 1), many.view(1, 1, -1, 1))
+    with pytest.raises(ValueError, match="32 bits"):
+        moa.decode_attn(c, many.view(1, -1, 1), many.view(1, -1, 1), None)
+
+
+def test_a_caches_tensors_stay_the_checked_ones():
+    k = on_gpu(4, 2, 16, 64, dtype=torch.bfloat16)
+    table = on_gpu(1, 2)
+    c = moa.KVCache(k, k, table, on_gpu(1))
+    for name in ("k", "v", "table", "len", "pos", "seen", "score"):
+        with pytest.raises(AttributeError):
+            setattr(c, name, on_gpu(1, 2))
+    assert c.table is table and c.k is k and c.pos is None
