@@ -341,12 +341,13 @@ constexpr uint32_t decode_wave_bytes(int DH, int CT, bool accounts)
     return decode_stages(DH) * (2 * WK * DH * 2 + 256) + 128 + (accounts ? WK * 16 * CT * 4 : 0);      // (the last: a tile's scores)
 }
 
-// Sixteen query heads of a KV head are the columns of a tile, CT of which are computed side by side: S^T = K Q^T, O^T += V^T P^T.  Every wavefront walks its own 32
-// keys of each tile of the run, with LDS of its own for NST tiles, so that there is no barrier before the run's end.  Keys and
-// values go straight into LDS: a tile's keys take the place of those NST tiles before as soon as these have been used, its
-// values likewise, and its table entries come another NST tiles before that.  Two workgroups share a compute unit (one at 256
-// dims), so that one loads while the other begins or ends a run.  (Rings of two tiles and one workgroup a compute unit: 8 x 32768 keys 181 us against
-// 180, 64 ragged sequences up to 8192 207 against 192, 96 of up to 100 16.7 against 11.1.)
+// Sixteen query heads of a KV head are the columns of a tile, CT of which are computed side by side from the same keys and values:
+// S^T = K Q^T, O^T += V^T P^T.  Every wavefront walks its own 32 keys of each tile of the run, with LDS of its own for NST tiles, so
+// that there is no barrier before the run's end.  Keys and values go straight into LDS: a tile's keys take the place of those NST
+// tiles before as soon as these have been used, its values likewise, and its table entries come another NST tiles before that.  Two
+// workgroups share a compute unit (one at 256 dims or two column tiles, whose registers would not fit twice), so that one loads while
+// the other begins or ends a run.  (Rings of two tiles and one workgroup a compute unit: 8 x 32768 keys 181 us against 180, 64 ragged
+// sequences up to 8192 207 against 192, 96 of up to 100 16.7 against 11.1.)
 // DH: head_dim as it lies in LDS; the rows in the pool may be shorter (PAD, a multiple of 8): their last pieces are then zeros.
 template <int DH, int CT, bool PAD, bool ACC>
 __global__ __launch_bounds__(256, DH == 256 || CT == 2 ? 1 : 2) void k_decode_attn_mfma(DecodeArgs a)
