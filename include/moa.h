@@ -56,7 +56,7 @@ enum { MOA_F32 = 0, MOA_BF16 = 1 };
 enum {
     MOA_DEV_BAD_PARENT = 1,   /* parent[0] != -1 or parent[i] outside [0, i)                */
     MOA_DEV_BAD_LENGTH = 2,   /* prefix_len / ca_len outside [0, P_cap] (clamped)           */
-    MOA_DEV_EMPTY_KEYS = 4,   /* cross-attention over an empty memory (output row = 0)      */
+    MOA_DEV_EMPTY_KEYS = 4,   /* attention over an empty memory or cache (output row = 0)  */
     MOA_DEV_CACHE_FULL = 8,   /* kv append would pass P_cap (rows beyond it are dropped)    */
     MOA_DEV_BAD_MESSAGE = 16, /* a token id or tree position does not fit its message field */
     MOA_DEV_BAD_PAGE = 32,    /* a page table names no page of the pool where a row is wanted */
@@ -331,7 +331,8 @@ int32_t moa_lm_head_argmax(int32_t dtype, const void *x, int32_t R, int32_t d, c
  * moa_decode_attn is the attention of one new token per sequence, whose own key and value are appended first:
  *   q, out [B, H*dh] (H = n_q_heads); one softmax over the len[b] slots.  len[b] = 0: zeros and MOA_DEV_EMPTY_KEYS.  A slot whose
  *   table entry is no page of the pool is left out (MOA_DEV_BAD_PAGE).  Where a value of a slot in use is infinite, its dimension of out
- *   is infinite or NaN.  accumulate != 0: score[b][h][s] grows by the weight that
+ *   is infinite or NaN.  A query head with a score that is NaN or +infinity, or with keys and none whose score is not -infinity, has no
+ *   softmax: its row of out is NaN, and so are, with accumulate, the accounts of all slots below len[b] of its KV head.  accumulate != 0: score[b][h][s] grows by the weight that
  *   slot s received, summed over the query heads of KV head h.  Results do not depend on what else is on the GPU, but how a
  *   sequence's keys are cut (and so the last bits) on the other sequences' lengths.
  *   Workspace: moa_decode_attn_workspace_bytes (for this cache description; where it has accounts 4 bytes a slot of capacity and query

@@ -9,6 +9,8 @@
 #include "moa_attn_device.h"
 #include "moa_kv_device.h"
 
+#include <float.h>
+
 namespace moa {
 
 namespace {
@@ -57,6 +59,12 @@ __device__ __forceinline__ float over_lanes(float x, const F &f)
     return FROM <= 5 ? with_lane32(x, f) : x;
 }
 __device__ __forceinline__ float add(float x, float y) { return x + y; }
+
+// The maximum that keys whose scores are all -infinity leave, where no key at all leaves -infinity: below every other score, so that
+// other keys' results stand when the two are joined.
+__device__ __forceinline__ float max_of_keys(float m, bool any) { return any && m == -INFINITY ? -FLT_MAX : m; }
+// what the sum is divided by: nothing where there was no key, and a softmax of nothing but -infinity is no number
+__device__ __forceinline__ float inverse_sum(float m, float l) { return l != 0.f ? 1.f / l : m == -INFINITY ? 0.f : __builtin_nanf(""); }
 
 // Where the tiles of the sequences lie in the list of all tiles: every wavefront works this out for itself.
 struct TileList {
@@ -114,7 +122,7 @@ __device__ __forceinline__ void finish(const DecodeArgs &a, int b, int len, int 
             l = fmaf(ml[(w * a.HG + r) * 2 + 1], c, l);
             o = fmaf(acc[w * stride + i], c, o);
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float inv = inverse_sum(m, l);
         if (whole) st((T *)a.out + ((int64_t)b * a.H + h * a.G + r0 + r) * dh + d, o * inv);
         else a.part_o[(slot * a.HG + r) * dh + d] = o;
         if (d != 0) continue;
@@ -123,7 +131,7 @@ __device__ __forceinline__ void finish(const DecodeArgs &a, int b, int len, int 
             a.part_ml[(slot * a.HG + r) * 2] = m;
             a.part_ml[(slot * a.HG + r) * 2 + 1] = l;
         }
-        if (whole && l == 0.f) a.c.flag(MOA_DEV_EMPTY_KEYS);
+        if (whole && m == -INFINITY && l == 0.f) a.c.flag(MOA_DEV_EMPTY_KEYS);
         fin[r * 2] = ms;
         fin[r * 2 + 1] = inv;
     }
@@ -206,6 +214,7 @@ __global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : 2) void k_deco
     for_each_pair(a, [&](int b, int len, int hb, uint32_t t0, uint32_t nt, bool whole, int64_t slot) {
         const int h = hb / a.rtiles, r0 = (hb - h * a.rtiles) * HG, rows = min(HG, a.G - r0);
         float qf[HG][VE], acc[HG][VE], m[HG], l[HG];
+        bool any = false;                        // whether this lane has had a key
 #pragma unroll
         for (int r = 0; r < HG; ++r) {
             const T *qr = (const T *)a.q + ((int64_t)b * a.H + h * a.G + r0 + min(r, rows - 1)) * dh + e0;
@@ -253,6 +262,7 @@ __global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : 2) void k_deco
                 slots[u] = slot_of(t, u);
                 row[u] = slots[u] < len ? row_next[u] : -1;
                 if (slots[u] < len && row[u] < 0) a.c.flag(MOA_DEV_BAD_PAGE);
+                any |= row[u] >= 0;
             }
             look_up(t + 1);
 #pragma unroll
@@ -291,6 +301,7 @@ __global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : 2) void k_deco
             }
         }
         // the lane groups' parts of a head, then one per wavefront into LDS
+        any = __ballot(any) != 0;
 #pragma unroll
         for (int r = 0; r < HG; ++r) {
             constexpr int FROM = LPR == 8 ? 3 : LPR == 16 ? 4 : LPR == 32 ? 5 : 6;
@@ -302,7 +313,7 @@ __global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : 2) void k_deco
                 if (grp == 0 && e < ne) acc_s[(wave * HG + r) * dh + e0 + e] = o;
             }
             if (lane == 0) {
-                ml_s[(wave * HG + r) * 2] = mn;
+                ml_s[(wave * HG + r) * 2] = max_of_keys(mn, any);
                 ml_s[(wave * HG + r) * 2 + 1] = l[r];
             }
         }
@@ -444,7 +455,7 @@ __global__ __launch_bounds__(256, DH == 256 || CT == 2 ? 1 : 2) void k_decode_at
             lsum[ct] = 0.f;
         }
 
-        uint32_t ok[NST];
+        uint32_t ok[NST], any = 0;                          // keys of the tiles that count; whether any did
         if (cnt > 0) {
             wait_loads<0>();
 #pragma unroll
@@ -465,6 +476,7 @@ __global__ __launch_bounds__(256, DH == 256 || CT == 2 ? 1 : 2) void k_decode_at
                 if (i >= cnt) break;
                 const uint32_t kb = lds0 + st * STAGEB, vb = kb + HALFB, count = ok[st];
                 const bool next = i + NST < cnt;
+                any |= count;
                 if (i + NST <= cnt) wait_loads<BEHIND_K>();
                 else wait_loads<0>();
                 f32x4 s[CT][2];
@@ -569,7 +581,7 @@ __global__ __launch_bounds__(256, DH == 256 || CT == 2 ? 1 : 2) void k_decode_at
                 for (int d = 0; d < NDB; ++d)
                     if (!PAD || 16 * d + 4 * quad < dh) *(f32x4 *)(acc_s + r * dh + 16 * d + 4 * quad) = acc[ct][d];
                 if (quad == 0) {
-                    ml_s[(wave * a.HG + r) * 2] = mref[ct];
+                    ml_s[(wave * a.HG + r) * 2] = max_of_keys(mref[ct], any != 0);
                     ml_s[(wave * a.HG + r) * 2 + 1] = l;
                 }
             }
@@ -677,8 +689,8 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
         const float ms = m == -INFINITY ? 0.f : m;
         for (uint32_t s = lane; s < ns; s += 64) l += ml[s * ml_step + 1] * fast_exp2(ml[s * ml_step] - ms);
         l = over_lanes<0>(l, add);
-        if (tid == 0 && l == 0.f) a.c.flag(MOA_DEV_EMPTY_KEYS);
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+        if (tid == 0 && m == -INFINITY && l == 0.f) a.c.flag(MOA_DEV_EMPTY_KEYS);
+        const float inv = inverse_sum(m, l);
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
         for (uint32_t s = g0; s < ns; s += U * groups) {
             f32x4 y[U];
@@ -732,7 +744,7 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
 #pragma unroll
             for (int i = 0; i < 8; ++i) l += sm[1][row][i];
             fin[row][0] = ms;
-            fin[row][1] = l == 0.f ? 0.f : 1.f / l;
+            fin[row][1] = inverse_sum(m, l);
         }
         __syncthreads();
         if (mine < len) {
