@@ -8,6 +8,7 @@ function will touch -- the kernels trust their sizes.
 from __future__ import annotations
 
 import ctypes as C
+from operator import index
 from pathlib import Path
 
 import torch
@@ -468,8 +469,8 @@ for _n in _SYMBOLS[-5:]:
 
 
 def _int32(n, name) -> int:
-    """ctypes would keep the low 32 bits of any other number."""
-    n = int(n)
+    """A whole number; ctypes would keep the low 32 bits of any other."""
+    n = index(n)
     if not -2**31 <= n < 2**31:
         raise ValueError(f"{name}: {n} does not fit 32 bits")
     return n
