@@ -476,6 +476,12 @@ def _int32(n, name) -> int:
     return n
 
 
+def _per_sequence(t, B, n, name):
+    """A tensor of more than is needed has that behind the last sequence, and not between them."""
+    if t is not None and t.dim() > 1 and t.numel() != B * n and t.numel() != t.shape[0] * n:
+        raise ValueError(f"{name}: {t.numel() // t.shape[0]} elements per sequence, the call takes them to be {n}")
+
+
 class KVCache:
     """moa_kv_cache_t: a KV cache in pages.  k, v [n_pages, Hkv, page_size, dh]; table [B, max_pages], len [B], optionally pos
     [B, Hkv, max_pages * page_size] with seen [B], score [B, Hkv, max_pages * page_size] (fp32; all others int32).  The tensors
@@ -498,6 +504,8 @@ class KVCache:
                            _dev(k, k.dtype, 0, "k"), _dev_on(v, k.dtype, 0, "v", i), _dev_on(table, i32, 0, "table", i),
                            _dev_on(len, i32, B, "len", i), _dev_on(pos, i32, slots, "pos", i), _dev_on(seen, i32, B, "seen", i),
                            _dev_on(score, torch.float32, slots, "score", i))
+        _per_sequence(pos, B, Hkv * max_pages * page_size, "pos")
+        _per_sequence(score, B, Hkv * max_pages * page_size, "score")
         self._ref = C.byref(self._c)
         self._dtype, self._dims = k.dtype, (B, Hkv, dh)
         self._tensors = k, v, table, len, pos, seen, score
@@ -518,6 +526,7 @@ def kv_append(cache: KVCache, k_new, v_new, path=None, n_new=None, dev_status=No
         raise ValueError("k_new and v_new: must be [B, Hkv, M, dh] of the cache")
     M, i, dt, i32 = _int32(shape[2], "M"), cache._index, cache._dtype, torch.int32
     n = B * Hkv * M * dh
+    _per_sequence(path, B, M, "path")
     rc = _lib.moa_kv_append(cache._ref, _dev_on(k_new, dt, n, "k_new", i), _dev_on(v_new, dt, n, "v_new", i), M,
                             _dev_on(path, i32, B * M, "path", i), _dev_on(n_new, i32, B, "n_new", i),
                             _dev_on(dev_status, i32, 1, "dev_status", i), cache._stream(stream))
