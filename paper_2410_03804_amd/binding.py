@@ -526,9 +526,9 @@ def kv_append(cache: KVCache, k_new, v_new, path=None, n_new=None, dev_status=No
         raise ValueError("k_new and v_new: must be [B, Hkv, M, dh] of the cache")
     M, i, dt, i32 = _int32(shape[2], "M"), cache._index, cache._dtype, torch.int32
     n = B * Hkv * M * dh
+    at = _dev_on(path, i32, B * M, "path", i)
     _per_sequence(path, B, M, "path")
-    rc = _lib.moa_kv_append(cache._ref, _dev_on(k_new, dt, n, "k_new", i), _dev_on(v_new, dt, n, "v_new", i), M,
-                            _dev_on(path, i32, B * M, "path", i), _dev_on(n_new, i32, B, "n_new", i),
+    rc = _lib.moa_kv_append(cache._ref, _dev_on(k_new, dt, n, "k_new", i), _dev_on(v_new, dt, n, "v_new", i), M, at, _dev_on(n_new, i32, B, "n_new", i),
                             _dev_on(dev_status, i32, 1, "dev_status", i), cache._stream(stream))
     if rc:
         _check(rc)

@@ -39,3 +39,9 @@ def test_a_path_of_another_tree(monkeypatch):
     for shape in ((B, 5), (B + 1, 5), (B * 5,)):
         with pytest.raises(Reached):
             moa.kv_append(c, new, new, path=on_gpu(*shape))
+
+
+def test_a_path_that_is_no_tensor():
+    new = on_gpu(B, Hkv, 2, dh, dtype=torch.bfloat16)
+    with pytest.raises(TypeError, match="path: expected a torch tensor"):
+        moa.kv_append(cache(), new, new, path=[[0, 1], [0, 1]])
