@@ -7,6 +7,7 @@
 // that has all tiles of a pair writes its result; other pairs leave m, l and the unnormalised o (single precision) of each run
 // that touched them in the workspace for a second launch to join.
 #include "moa_attn_device.h"
+#include "moa_decode_plan.h"
 #include "moa_kv_device.h"
 
 #include <float.h>
@@ -15,7 +16,7 @@ namespace moa {
 
 namespace {
 
-constexpr int TK = 128, WAVES = 4, WK = TK / WAVES;        // keys of a tile, wavefronts, keys of a tile that a wavefront takes
+constexpr int WAVES = 4, WK = TK / WAVES;        // wavefronts, keys of a tile that a wavefront takes
 
 struct DecodeArgs {
     KvDev c;
@@ -758,47 +759,15 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
 }
 
 // ---------------------------------------------------------------- host
-struct DecodePlan {
-    bool mfma, wide;
-    int HG, rtiles, runs, cap32;
-    size_t part_o, part_ml, raw;       // bytes
-    size_t total() const { return part_o + part_ml + raw; }
-};
-
-size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
-
 // whether the matrix cores' form takes such a cache (and queries q, which it also reads 16 bytes at a time)
 bool takes_mfma(const moa_kv_cache_t &c, const void *q)
 {
     return c.dtype == MOA_BF16 && kv_rows16(c, {q});
 }
 
-DecodePlan decode_plan(const moa_kv_cache_t &c, int H, bool accounts, bool mfma)
+DecodePlan plan_of(const moa_kv_cache_t &c, int H, bool accounts, bool mfma)
 {
-    DecodePlan p;
-    const int G = H / c.n_kv_heads, cap = c.max_pages * c.page_size;
-    p.mfma = mfma;
-    p.wide = c.dtype == MOA_F32 && kv_rows16(c, {});
-    // On the matrix cores 32 query heads share a pass over the keys where there is enough of it, and 16 where more runs are wanted (or
-    // two tiles of columns do not fit the registers).  32 heads on one KV head, us, 16 a pass against 32: 1 x 8000 keys 8.6, 12.8; 16 x
-    // 8000 25.7, 26.0, and with 64 heads 39.4, 33; 64 x 8000 68.5, 45.5; 64 x 32000 312, 168.
-    const int most = c.head_dim <= 128 && (int64_t)c.B * c.n_kv_heads * ((cap + TK - 1) / TK) >= 512 ? 32 : 16;
-    p.HG = p.mfma ? (G < most ? G : most) : G <= 2 || !p.wide ? 2 : G <= 4 ? 4 : 8;
-    p.rtiles = (G + p.HG - 1) / p.HG;
-    const int64_t pairs = (int64_t)c.B * c.n_kv_heads * p.rtiles;
-    // One workgroup per pair, without a second launch (4 us), where that is a short walk, or not a long one and there are pairs
-    // enough for two workgroups a compute unit.  Else two runs per compute unit on the matrix cores, four element by element.
-    // Measured, us, per pair against runs + join, 8b heads: 1 x 512 tokens 8.7, 6.9 + 4.0; 1 x 1024 12.5, 5.8 + 4.1; 64 x 1024
-    // 38.9, 40.7 + 6.4; 64 x 17 .. 2048 55.3, 50.6 + 7.3.  Single precision: 1 x 256 11.4, 8.2 + 4.1; 1 x 512 19.3, 8.8 + 4.2.
-    // Half and twice as many runs: 64 ragged sequences up to 8192 181 and 176 against 173, 8 x 32768 158 and 164 against 158; single
-    // precision 4 x 32000 28.1 and 27.3 against 23.7.
-    const int64_t walk = p.mfma ? pairs >= 512 ? 1024 : 512 : 256;
-    p.runs = cap <= walk && !(accounts && p.rtiles > 1) ? 0 : !p.mfma ? 1024 : c.head_dim <= 128 && p.HG <= 16 ? 512 : 256;
-    p.part_o = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * c.head_dim * 4) : 0;
-    p.part_ml = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * 2 * 4) : 0;
-    p.cap32 = (cap + 31) & ~31;
-    p.raw = accounts ? align256((size_t)pairs * p.cap32 * p.HG * 4) : 0;
-    return p;
+    return decode_plan(c.B, c.n_kv_heads, c.head_dim, c.max_pages * c.page_size, H, accounts, mfma, c.dtype == MOA_F32 && kv_rows16(c, {}));
 }
 
 // enough for either form, and for accounts where the cache keeps them
@@ -807,7 +776,7 @@ size_t workspace_bytes(const moa_kv_cache_t &c, int H)
     size_t most = 0;
     for (const bool mfma : {false, takes_mfma(c, nullptr)})
         for (const bool accounts : {false, c.score != nullptr}) {
-            const size_t n = decode_plan(c, H, accounts, mfma).total();
+            const size_t n = plan_of(c, H, accounts, mfma).total();
             if (n > most) most = n;
         }
     return most;
@@ -915,7 +884,7 @@ int32_t moa_decode_attn(const moa_kv_cache_t *cache, int32_t n_q_heads, const vo
     if (accumulate && !cache->score) return api_fail(MOA_ERR_NULL, "decode_attn: the cache keeps no accounts (score)");
     const size_t es = kv_esize(*cache);
     if (((uintptr_t)q | (uintptr_t)out) & (es - 1)) return api_fail(MOA_ERR_SHAPE, "decode_attn: q / out not aligned to their elements");
-    const DecodePlan p = decode_plan(*cache, n_q_heads, accumulate != 0, takes_mfma(*cache, q));
+    const DecodePlan p = plan_of(*cache, n_q_heads, accumulate != 0, takes_mfma(*cache, q));
     const size_t need = workspace_bytes(*cache, n_q_heads);
     if (need && (!ws || (((uintptr_t)ws) & 255) || ws_bytes < need))
         return api_fail(MOA_ERR_WORKSPACE, "decode_attn: workspace NULL, misaligned or smaller than moa_decode_attn_workspace_bytes");
