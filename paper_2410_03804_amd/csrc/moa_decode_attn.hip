@@ -215,7 +215,7 @@ __global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : 2) void k_deco
     for_each_pair(a, [&](int b, int len, int hb, uint32_t t0, uint32_t nt, bool whole, int64_t slot) {
         const int h = hb / a.rtiles, r0 = (hb - h * a.rtiles) * HG, rows = min(HG, a.G - r0);
         float qf[HG][VE], acc[HG][VE], m[HG], l[HG];
-        bool any = false;                        // whether this lane has had a key
+        uint64_t any = 0;                        // lanes that have had a key
 #pragma unroll
         for (int r = 0; r < HG; ++r) {
             const T *qr = (const T *)a.q + ((int64_t)b * a.H + h * a.G + r0 + min(r, rows - 1)) * dh + e0;
@@ -263,7 +263,7 @@ __global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : 2) void k_deco
                 slots[u] = slot_of(t, u);
                 row[u] = slots[u] < len ? row_next[u] : -1;
                 if (slots[u] < len && row[u] < 0) a.c.flag(MOA_DEV_BAD_PAGE);
-                any |= row[u] >= 0;
+                any |= __ballot(row[u] >= 0);
             }
             look_up(t + 1);
 #pragma unroll
@@ -302,7 +302,6 @@ __global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : 2) void k_deco
             }
         }
         // the lane groups' parts of a head, then one per wavefront into LDS
-        any = __ballot(any) != 0;
 #pragma unroll
         for (int r = 0; r < HG; ++r) {
             constexpr int FROM = LPR == 8 ? 3 : LPR == 16 ? 4 : LPR == 32 ? 5 : 6;
@@ -314,7 +313,7 @@ __global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : 2) void k_deco
                 if (grp == 0 && e < ne) acc_s[(wave * HG + r) * dh + e0 + e] = o;
             }
             if (lane == 0) {
-                ml_s[(wave * HG + r) * 2] = max_of_keys(mn, any);
+                ml_s[(wave * HG + r) * 2] = max_of_keys(mn, any != 0);
                 ml_s[(wave * HG + r) * 2 + 1] = l[r];
             }
         }
