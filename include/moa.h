@@ -336,7 +336,8 @@ int32_t moa_lm_head_argmax(int32_t dtype, const void *x, int32_t R, int32_t d, c
  *   slot s received, summed over the query heads of KV head h.  Results do not depend on what else is on the GPU, but how a
  *   sequence's keys are cut (and so the last bits) on the other sequences' lengths.
  *   Workspace: moa_decode_attn_workspace_bytes (for this cache description; where it has accounts 4 bytes a slot of capacity and query
- *   head are most of it), 256-byte aligned.
+ *   head are most of it), 256-byte aligned.  With accumulate the time goes with cap as well as with len (the scores of the whole
+ *   capacity are read): describe a cache with no more pages per sequence than the longest one may come to use.
  * moa_kv_evict cuts every sequence of more than `budget` slots down to `budget`, for each KV head by itself.  Slots stay in this
  *   order: tokens with pos >= seen[b] - recent (all alike), then by score, larger first (NaN last); equal ones by lower slot.  A token that
  *   stays and lies in a slot >= budget moves, with its position and score, into a slot below whose token leaves, the first into the first

@@ -2,8 +2,9 @@
 //
 // One pass over the keys and values with the running maximum m and sum l of a softmax per query head, scores in the log2 domain:
 //   s_j = q . k_j log2(e) / sqrt(dh),  l = sum 2^(s_j - m),  o = sum 2^(s_j - m) v_j / l.
-// The work is the list of all tiles of TK keys of all (sequence, KV head) pairs, in that order, cut into equal runs, one per
-// workgroup: lengths are only known on the device, and a batch of very different ones is then as fast as an even one.  A run
+// The work is the list of all tiles of TK keys of all (sequence, KV head) pairs, in that order, cut into runs of equally many whole
+// tiles, one per workgroup: lengths are only known on the device, and a batch of very different ones is then as fast as an even
+// one.  (Rounding up leaves the last runs without any: 2070 tiles in 512 runs are five for each of 414.)  A run
 // that has all tiles of a pair writes its result; other pairs leave m, l and the unnormalised o (single precision) of each run
 // that touched them in the workspace for a second launch to join.
 #include "moa_attn_device.h"
@@ -231,7 +232,8 @@ __global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : 2) void k_deco
             const T *p = (const T *)pool + (int64_t)row * dh + e0;
             x = u32x4{0u, 0u, 0u, 0u};
             if (row < 0 || ne == 0) return;
-            // (whole lines where rows are not short: as lds_gather16, 64 sequences of up to 4000 keys 47 us without and 42 with)
+            // (whole lines where rows are not short: as lds_gather16, 64 sequences of up to 4000 keys 47 us without and 42 with; 16
+            // heads on one KV head, which are two tiles, 8 x 8000 keys 59 and 62)
             if (WIDE) x = __builtin_nontemporal_load((const u32x4 *)p);
             else
 #pragma unroll
@@ -324,8 +326,11 @@ __global__ __launch_bounds__(256, HG == 2 && sizeof(T) == 4 ? 4 : 2) void k_deco
 // ---------------------------------------------------------------- on the matrix cores: bf16, head_dim a multiple of 8
 // 64 lanes x 16 (4) bytes, each from an address of its own, to 1 KB (256 bytes) of LDS at `lds`.  (As lds_dma16 in
 // moa_gemm_device.h, but a pool of pages takes 64-bit addresses; the s_nop stands between the write of m0 and its use.)
-// ONCE: nobody reads the line again.  Keys and values whose rows are whole lines: 8 x 32768 keys 180 us without, 159 with (6.7
-// TB/s), 64 ragged sequences 193 and 171.  Rows of 160 bytes share lines: 11.7 us without, 13.9 with.
+// ONCE: said to be read once only.  Keys and values whose rows are whole lines: 8 x 32768 keys 180 us without, 159 with (6.7
+// TB/s), 64 ragged sequences 193 and 171.  Rows of 160 bytes share lines: 11.7 us without, 13.9 with.  It is not true of every line
+// that it is said of.  Where several tiles of query heads read a KV head's keys it costs: 128 heads on one KV head, 16 x 32000
+// keys, 155 us without, 173 with; 31 heads of 256 dims, 8 x 8000, 31 and 34.5.  Where sequences share pages it does not: 64 x
+// 4500 keys, the first 1024 of them common, 167 without, 149 with; 4096 of them 72 and 73.
 template <bool ONCE>
 __device__ __forceinline__ void lds_gather16(uint32_t lds, uint64_t at)
 {
@@ -356,8 +361,9 @@ constexpr uint32_t decode_wave_bytes(int DH, int CT, bool accounts)
 // S^T = K Q^T, O^T += V^T P^T.  Every wavefront walks its own 32 keys of each tile of the run, with LDS of its own for NST tiles, so
 // that there is no barrier before the run's end.  Keys and values go straight into LDS: a tile's keys take the place of those NST
 // tiles before as soon as these have been used, its values likewise, and its table entries come another NST tiles before that.  Two
-// workgroups share a compute unit (one at 256 dims or two column tiles, whose registers would not fit twice), so that one loads while
-// the other begins or ends a run.  (Rings of two tiles and one workgroup a compute unit: 8 x 32768 keys 181 us against 180, 64 ragged
+// workgroups share a compute unit, so that one loads while the other begins or ends a run; at 256 dims, and at 128 with two column
+// tiles, the registers fit once only.  (At 64 dims with two column tiles they would fit twice, 227 of 256; it is launched as at
+// 128.)  (Rings of two tiles and one workgroup a compute unit: 8 x 32768 keys 181 us against 180, 64 ragged
 // sequences up to 8192 207 against 192, 96 of up to 100 16.7 against 11.1.)
 // DH: head_dim as it lies in LDS; the rows in the pool may be shorter (PAD, a multiple of 8): their last pieces are then zeros.
 template <int DH, int CT, bool PAD, bool ACC>
@@ -593,6 +599,9 @@ __global__ __launch_bounds__(256, DH == 256 || CT == 2 ? 1 : 2) void k_decode_at
 // ---------------------------------------------------------------- the second launch
 // Workgroups 0 .. B H - 1 join the partial results of one query head; the others bring the accounts of 256 slots of a (sequence,
 // KV head) up to date from its scores, now that the sums are known.  Either leaves alone what the first launch finished.
+// The latter are as many as the capacity has, and read their scores before they know the length, which hides the one behind the other
+// where most slots are in use and is paid for where few are.  16 sequences of 2048 tokens, 8b heads, us: 7.2 in a capacity of
+// 2112, 19.3 of 16384, 48.5 of 65536; 64 of 1000: none in a capacity of 1024, 36 of 8192, 91 of 32768.  (Without accounts 4 in any.)
 constexpr int ACC_SLOTS = 256;
 template <typename T>
 __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)

@@ -15,7 +15,10 @@ struct DecodePlan {
     size_t total() const { return part_o + part_ml + raw; }
 };
 
-// mfma: rows and queries are bf16 and can be read 16 bytes at a time; wide: rows are single precision and can be
+// mfma: rows and queries are bf16 and can be read 16 bytes at a time; wide: rows are single precision and can be.
+// The host knows the capacity, not the lengths, so that short sequences in a wide table get the form that long ones want.  Us, in a
+// capacity of their length against one of 65536: 32 heads on one KV head, 1 x 8000 keys 8.4 + 5.9, 12.5 + 6.1; 8b heads, 1 x 400 9.2, 6.3 +
+// 4.3; 64 x 1000 in 1024 42.0, in 32768 42.1 + 4.0.
 inline DecodePlan decode_plan(int B, int Hkv, int dh, int cap, int H, bool accounts, bool mfma, bool wide)
 {
     auto align256 = [](size_t n) { return (n + 255) & ~(size_t)255; };
@@ -23,8 +26,8 @@ inline DecodePlan decode_plan(int B, int Hkv, int dh, int cap, int H, bool accou
     const int G = H / Hkv;
     p.mfma = mfma;
     p.wide = wide;
-    // On the matrix cores 32 query heads share a pass over the keys where there is enough of it, and 16 where more runs are wanted (or
-    // two tiles of columns do not fit the registers).  32 heads on one KV head, us, 16 a pass against 32: 1 x 8000 keys 8.6, 12.8; 16 x
+    // On the matrix cores 32 query heads share a pass over the keys where there is enough of it, and 16 where more runs are wanted (or,
+    // beyond 128 dims, two tiles of columns do not fit the registers).  32 heads on one KV head, us, 16 a pass against 32: 1 x 8000 keys 8.6, 12.8; 16 x
     // 8000 25.7, 26.0, and with 64 heads 39.4, 33; 64 x 8000 68.5, 45.5; 64 x 32000 312, 168.
     const int most = dh <= 128 && (int64_t)B * Hkv * ((cap + TK - 1) / TK) >= 512 ? 32 : 16;
     p.HG = p.mfma ? (G < most ? G : most) : G <= 2 || !p.wide ? 2 : G <= 4 ? 4 : 8;

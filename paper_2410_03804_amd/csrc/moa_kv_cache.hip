@@ -174,10 +174,10 @@ __device__ __forceinline__ uint32_t lanes_below(uint64_t mask)
 // (11, 11 and 10 bits; the newest, whose key is the largest there is, are only counted); slots with a larger key stay, and of
 // those with an equal one the lowest, which only matters in the one wavefront where the equal ones that stay end.  Each
 // wavefront then lists what its stretch frees below the budget and what stays beyond it; the i-th of either are one move.
-// What bounds it is instructions, all of them on the one compute unit that has the pair, and a pass over 8 bytes a slot that it loads
-// alone.  64 pairs of up to 16384 slots: 34 us with keys in registers and every pass unrolled (33 KB of code, fetched for one
+// What bounds it is that one compute unit has all of a pair: its vector units are busy 45 % of the time at up to 16384 slots (32 % at
+// 2112), and its wavefronts wait 54 % (64 %) of theirs, for barriers, LDS and the pass over 8 bytes a slot that it loads alone.  64 pairs of up to 16384 slots: 34 us with keys in registers and every pass unrolled (33 KB of code, fetched for one
 // pass), 35 with loops but sums by shuffles, 19.5 now; 128 pairs of 2112 9.6 us.  Eight pairs of 131072: 206 us with accounts and positions read again
-// in every pass, 149 with the keys in the workspace.
+// in every pass, 149 with the keys in the workspace; of 32768 33.  (Those use eight compute units of 256.)
 __global__ __launch_bounds__(EV_T) void k_kv_evict_select(EvictArgs a)
 {
     constexpr int NW = EV_T / 64, U = EV_U, UL = 8;      // rounds at a time: keys, accounts
