@@ -332,8 +332,8 @@ int32_t moa_lm_head_argmax(int32_t dtype, const void *x, int32_t R, int32_t d, c
  *   q, out [B, H*dh] (H = n_q_heads); one softmax over the len[b] slots.  len[b] = 0: zeros and MOA_DEV_EMPTY_KEYS.  A slot whose
  *   table entry is no page of the pool is left out (MOA_DEV_BAD_PAGE).  Where a value of a slot in use is infinite, its dimension of out
  *   is infinite or NaN.  A query head with a score that is NaN or +infinity, or with keys and none whose score is not -infinity, has no
- *   softmax: its row of out is NaN, and so are, with accumulate, the accounts of all slots below len[b] of its KV head.  accumulate != 0: score[b][h][s] grows by the weight that
- *   slot s received, summed over the query heads of KV head h.  Results do not depend on what else is on the GPU, but how a
+ *   softmax: its row of out is NaN, and so are, with accumulate, the accounts of all slots below len[b] of its KV head.
+ *   accumulate != 0: score[b][h][s] grows by the weight that slot s received, summed over the query heads of KV head h.  Results do not depend on what else is on the GPU, but how a
  *   sequence's keys are cut (and so the last bits) on the other sequences' lengths.
  *   Workspace: moa_decode_attn_workspace_bytes (for this cache description; where it has accounts 4 bytes a slot of capacity and query
  *   head are most of it), 256-byte aligned.  With accumulate the time goes with cap as well as with len (the scores of the whole
