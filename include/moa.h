@@ -368,6 +368,98 @@ int32_t moa_kv_evict_workspace_bytes(const moa_kv_cache_t *cache, int32_t budget
 int32_t moa_kv_evict(const moa_kv_cache_t *cache, int32_t budget, int32_t recent,
                      int32_t *dev_status, void *ws, size_t ws_bytes, void *stream);
 
+/* Pages of a pool handed out to the sequences of a batch and taken back on the device, so that a server that decodes over a cache of pages
+ * (Sec. 2.1, one token per forward pass; Sec. 2.2, the tokens of a draft) builds its tables without a trip to the host.  A table entry below
+ * 0 names no page.  free_pages [n_pages] is a stack of the pages that nobody has, of which the first *n_free count; it, the table [B,
+ * max_pages] and *n_free belong to the caller, who has them start somewhere (all pages free, all entries -1).  A table serves the caches of
+ * all layers.  len [B] is the slots in use, as in moa_kv_cache_t, within max_pages * page_size (clamped, MOA_DEV_BAD_LENGTH).
+ *
+ * moa_kv_reserve: sequence b is about to get n_new[b] tokens, into slots len[b] ..; the batch holds them packed, one sequence behind the
+ *   other, in T rows.
+ *   tok_off [B + 1]: the first row of each sequence, and of what lies behind the last.  n_new is taken to be at least 0 and at most what
+ *     is left of T (MOA_DEV_BAD_LENGTH) and of the capacity (MOA_DEV_CACHE_FULL).
+ *   Table entries that these slots lie in and that name no page get one: the i-th such entry of the batch, by sequence and slot, free_pages[*n_free
+ *     - 1 - i].  A sequence gets all that it lacks or nothing: from the first one on whose pages are not there any more, those that lack
+ *     some get none (MOA_DEV_CACHE_FULL), those that lack none are not held up.  *n_free falls by what was taken.
+ *   n_got [B] (may be n_new itself): the tokens of b, or 0 where it got no pages.
+ *   pos, slot [T] (either may be NULL): row t's position, seen[b] + i (seen NULL: len[b] + i) for token i of b, and its slot in the pool, page *
+ *     page_size + row in the page; -1 where b got no pages or an entry is no page of the pool (MOA_DEV_BAD_PAGE).  Rows behind the last
+ *     token get position 0 and slot -1.
+ * moa_kv_release: entries behind the page of slot len[b] - 1 that name a page lose it (-1); the pages go back, so that the first of them by
+ *   sequence and slot is the next one to be taken.  For a sequence that is done, set its len to 0 first; behind moa_kv_evict or a rejected draft
+ *   it gives back what they left.  A page that several sequences share is for the caller to take out of all tables but one: *n_free never
+ *   passes n_pages (what would is dropped, MOA_DEV_BAD_PAGE), but a page that is in the list twice is handed out twice.  The whole table is read, by
+ *   one workgroup.
+ * Both are one launch of one workgroup; reserve writes pos and slot by a second one beyond 8192 rows or 1024 sequences.  Limits: B <= 2^20, T <=
+ * 2^21, max_pages * page_size <= 2^30, n_pages * page_size and B * max_pages < 2^31 (MOA_ERR_SHAPE). */
+int32_t moa_kv_reserve(int32_t B, int32_t n_pages, int32_t page_size, int32_t max_pages, const int32_t *len /*[B]*/,
+                       const int32_t *n_new /*[B]*/, const int32_t *seen /*[B] or NULL*/, int32_t *table, int32_t *free_pages,
+                       int32_t *n_free, int32_t T, int32_t *tok_off, int32_t *n_got, int32_t *pos, int32_t *slot,
+                       int32_t *dev_status, void *stream);
+int32_t moa_kv_release(int32_t B, int32_t n_pages, int32_t page_size, int32_t max_pages, const int32_t *len /*[B]*/,
+                       int32_t *table, int32_t *free_pages, int32_t *n_free, int32_t *dev_status, void *stream);
+
+/* Queries and keys between their projection and the attention: RMS norm of each head and rotation to the token's position in one pass
+ * (what moa_tli_decoder_layer does inside, Sec. 3.2, for those who decode over a cache of pages, whose keys are held as they are to be
+ * attended; the norm is of LLMs that have one per head).  Token t's queries are n_q_heads rows of head_dim behind each other at q + t * q_stride
+ * (elements; q and k may be parts of one projection's output), its keys and the results likewise:
+ *   y = x / sqrt(mean(x^2) + rms_eps) * g over a head, g = gq or gk [head_dim] (NULL: y = x);
+ *   pairs (c, c + rot_dim/2), c < rot_dim/2, are rotated by pos[t] * rope_theta^(-2c/rot_dim); dims from rot_dim on are y.
+ * rot_dim = 0: the norm alone.  In single precision, the angle in double, rounded once.  q_out may be q with the same stride, k_out k; other
+ * overlaps are not allowed.  0 heads: q (or k) is not looked at.  T = 0 is a no-op.  MOA_ERR_SHAPE: head_dim outside [1, 256], rot_dim odd or beyond
+ * head_dim, strides smaller than the heads take, T > 2^24. */
+int32_t moa_qk_norm_rope(int32_t dtype, const void *q, int64_t q_stride, int32_t n_q_heads, const void *k, int64_t k_stride,
+                         int32_t n_kv_heads, int64_t T, int32_t head_dim, const void *gq, const void *gk, float rms_eps,
+                         const int32_t *pos /*[T]*/, float rope_theta, int32_t rot_dim, void *q_out, int64_t q_out_stride,
+                         void *k_out, int64_t k_out_stride, void *stream);
+
+/* The cache of pages with its keys and values held in 8 bits, for decoding as above (Sec. 2.1): half of what moa_decode_attn reads.  Codes are e4m3 numbers
+ * (sign, 4 bits of exponent, 3 of mantissa; up to 448, NaN, no infinity); the MOA_KVQ_BLOCK rows r with the same r / MOA_KVQ_BLOCK of a page and KV head have one
+ * scale for their keys and one for their values (the last block of a page may be shorter), and a code stands for code * scale.
+ *   k, v             [n_pages, Hkv, page_size, dh] codes;
+ *   k_scale, v_scale [n_pages, Hkv, ceil(page_size / MOA_KVQ_BLOCK)] fp32, positive and finite; of blocks that hold no row they do not matter;
+ *   table, len       as in moa_kv_cache_t; `dtype` is that of the rows given, of queries and of results.
+ * Limits as there.  No accounts, and so no eviction by them.
+ *
+ * moa_kvq_append puts rows into the cache as moa_kv_append does (k_new, v_new [B, Hkv, M, dh], path, n_new; len grows).  moa_kvq_append_rows takes them
+ *   packed: row tok_off[b] + i of T, heads behind each other, k_stride (v_stride) elements from row to row, for i < tok_off[b + 1] - tok_off[b], or
+ *   n_new[b] of these (tok_off and n_got of moa_kv_reserve).  Offsets outside [0, T], falling ones, and more n_new than there are rows are
+ *   clamped (MOA_DEV_BAD_LENGTH).
+ *   The scale of a block that gets rows becomes the smallest power of two, within 2^-120 .. 2^120, by which the finite numbers of its new rows are at most 448,
+ *   or stays where it is larger and the block holds rows already; if it grows, these are rounded to the new one's codes (which changes
+ *   only what is below 2^-6 of it).  New rows are rounded to nearest even, once.  Infinite values are held as NaN.
+ *   A row whose table entry is no page is not written but counted (MOA_DEV_BAD_PAGE).  Two sequences may share a page that no call writes to; the
+ *   block of slot len[b] is written to, its earlier rows too.
+ * moa_kvq_read gives rows back as values: slot s < min(len[b], P_cap) of sequence b and KV head h to row s of k_out, v_out [B, Hkv, P_cap, dh], the caches
+ *   that moa_tree_verify_attn reads (with P_cap); rows behind these, and of slots without a page (MOA_DEV_BAD_PAGE), are left as they were.  len[b] > P_cap:
+ *   MOA_DEV_CACHE_FULL.  Exact wherever dtype holds the number.
+ * moa_kvq_decode_attn is moa_decode_attn (without accounts) over such a cache: q, out [B, H*dh], one softmax over the len[b] slots; empty sequences, slots
+ *   without a page, scores without a softmax and NaN as there.  Scores, weights and sums are fp32, scales are multiplied into them.  Workspace:
+ *   moa_kvq_decode_attn_workspace_bytes, 256-byte aligned. */
+#define MOA_KVQ_BLOCK 16
+typedef struct {
+    int32_t dtype;                    /* MOA_F32 | MOA_BF16                                  */
+    int32_t n_kv_heads, head_dim;
+    int32_t B;                        /* sequences                                           */
+    int32_t n_pages, page_size;       /* pages of the pool, rows of a page                   */
+    int32_t max_pages;                /* row length of the table                             */
+    void *k, *v;                      /* codes                                               */
+    float *k_scale, *v_scale;
+    const int32_t *table;
+    int32_t *len;
+} moa_kvq_cache_t;
+
+int32_t moa_kvq_append(const moa_kvq_cache_t *cache, const void *k_new, const void *v_new, int32_t M,
+                       const int32_t *path /*[B,M] or NULL*/, const int32_t *n_new /*[B] or NULL*/,
+                       int32_t *dev_status, void *stream);
+int32_t moa_kvq_append_rows(const moa_kvq_cache_t *cache, const void *k_new, int64_t k_stride, const void *v_new, int64_t v_stride,
+                            int32_t T, const int32_t *tok_off /*[B+1]*/, const int32_t *n_new /*[B] or NULL*/,
+                            int32_t *dev_status, void *stream);
+int32_t moa_kvq_read(const moa_kvq_cache_t *cache, int32_t P_cap, void *k_out, void *v_out, int32_t *dev_status, void *stream);
+int32_t moa_kvq_decode_attn_workspace_bytes(const moa_kvq_cache_t *cache, int32_t n_q_heads, size_t *bytes_host);
+int32_t moa_kvq_decode_attn(const moa_kvq_cache_t *cache, int32_t n_q_heads, const void *q, void *out,
+                            int32_t *dev_status, void *ws, size_t ws_bytes, void *stream);
+
 /* Client-server messages (Sec. 4.2; appendix table of message lengths).
  * Client -> server: each node of the draft tree as 3 bytes of token id (little-endian) and 1 byte for
  * its position in the tree = the index of its parent, 0xFF for the root: msg [B, 4 M] bytes (4-byte

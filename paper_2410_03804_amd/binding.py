@@ -78,7 +78,9 @@ _SYMBOLS = ["moa_status_str", "moa_last_error", "moa_workspace_bytes", "moa_tree
             "moa_self_attn_draft", "moa_tli_workspace_bytes", "moa_tli_decoder_layer", "moa_tree_expand_level", "moa_tree_finalize", "moa_topk_logprob", "moa_topk_workspace_bytes", "moa_lm_head_workspace_bytes", "moa_lm_head_argmax", "moa_msg_pack_tree", "moa_msg_unpack_tree", "moa_msg_accept_bytes", "moa_msg_pack_accept",
             "moa_msg_unpack_accept", "moa_msg_gzip_bound", "moa_msg_gzip", "moa_msg_gunzip", "moa_linear_workspace_bytes", "moa_linear", "moa_fold_projection", "moa_lsa_packed_weight_bytes", "moa_lsa_pack_weights", "moa_lsa_packed", "moa_mlp_block_workspace_bytes", "moa_mlp_block", "moa_rmsnorm", "moa_profile_enable", "moa_profile_sample_every", "moa_profile_collect", "moa_profile_kernel_name", "moa_profile_site_name", "moa_probe_read", "moa_probe_mfma",
             "moa_debug_force_attn_kernel", "moa_debug_force_lsa_kernel", "moa_tree_verify_attn_noalloc",
-            "moa_kv_append", "moa_decode_attn_workspace_bytes", "moa_decode_attn", "moa_kv_evict_workspace_bytes", "moa_kv_evict"]
+            "moa_kv_append", "moa_decode_attn_workspace_bytes", "moa_decode_attn", "moa_kv_evict_workspace_bytes", "moa_kv_evict",
+            "moa_kv_reserve", "moa_kv_release", "moa_qk_norm_rope", "moa_kvq_append", "moa_kvq_append_rows", "moa_kvq_read",
+            "moa_kvq_decode_attn_workspace_bytes", "moa_kvq_decode_attn"]
 
 _lib.moa_status_str.restype = C.c_char_p
 _lib.moa_status_str.argtypes = [C.c_int32]
@@ -464,7 +466,22 @@ _lib.moa_decode_attn_workspace_bytes.argtypes = [C.POINTER(_KvCache), _i32, C.PO
 _lib.moa_decode_attn.argtypes = [C.POINTER(_KvCache), _i32, _vp, _vp, _i32, _vp, _vp, _sz, _vp]
 _lib.moa_kv_evict_workspace_bytes.argtypes = [C.POINTER(_KvCache), _i32, C.POINTER(_sz)]
 _lib.moa_kv_evict.argtypes = [C.POINTER(_KvCache), _i32, _i32, _vp, _vp, _sz, _vp]
-for _n in _SYMBOLS[-5:]:
+_lib.moa_kv_reserve.argtypes = [_i32] * 4 + [_vp] * 6 + [_i32] + [_vp] * 6
+_lib.moa_kv_release.argtypes = [_i32] * 4 + [_vp] * 6
+_lib.moa_qk_norm_rope.argtypes = [_i32, _vp, _i64, _i32, _vp, _i64, _i32, _i64, _i32, _vp, _vp, C.c_float, _vp, C.c_float, _i32, _vp, _i64, _vp, _i64, _vp]
+
+
+class _KvqCache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_kv_heads", "head_dim", "B", "n_pages", "page_size", "max_pages")] + [
+        (n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "table", "len")]
+
+
+_lib.moa_kvq_append.argtypes = [C.POINTER(_KvqCache), _vp, _vp, _i32, _vp, _vp, _vp, _vp]
+_lib.moa_kvq_append_rows.argtypes = [C.POINTER(_KvqCache), _vp, _i64, _vp, _i64, _i32, _vp, _vp, _vp, _vp]
+_lib.moa_kvq_read.argtypes = [C.POINTER(_KvqCache), _i32, _vp, _vp, _vp, _vp]
+_lib.moa_kvq_decode_attn_workspace_bytes.argtypes = [C.POINTER(_KvqCache), _i32, C.POINTER(_sz)]
+_lib.moa_kvq_decode_attn.argtypes = [C.POINTER(_KvqCache), _i32, _vp, _vp, _vp, _vp, _sz, _vp]
+for _n in _SYMBOLS[_SYMBOLS.index("moa_kv_append"):]:
     getattr(_lib, _n).restype = C.c_int32
 
 
@@ -567,6 +584,194 @@ def kv_evict(cache: KVCache, budget: int, recent: int, ws, dev_status=None, stre
     wsp, wsb = _room_on(ws, "ws", i)
     rc = _lib.moa_kv_evict(cache._ref, _int32(budget, "budget"), _int32(recent, "recent"), _dev_on(dev_status, torch.int32, 1, "dev_status", i), wsp, wsb,
                            cache._stream(stream))
+    if rc:
+        _check(rc)
+
+
+KVQ_BLOCK = 16            # rows of a page and KV head that share a scale (MOA_KVQ_BLOCK)
+
+
+def _device_of(t, stream):
+    """The index of a tensor's device, which the calls below want to be the current one, and the stream's handle."""
+    i = t.get_device()
+    if torch._C._cuda_getDevice() != i or (stream is not None and stream.device_index != i):
+        raise ValueError("the tensors' device must be the current one, and the stream's")
+    return i, torch._C._cuda_getCurrentRawStream(i) if stream is None else stream.cuda_stream
+
+
+def _rows_on(t, dtype, heads, dh, name, at):
+    """Address and row stride of a tensor [T, heads, dh] whose rows may lie apart (a part of a projection's output)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dh:
+        raise ValueError(f"{name}: must be [T, {heads}, {dh}]")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
+    step, of_head, of_elem = t.stride()
+    few = t.shape[0] <= 1                              # a stride that is never taken may be any number
+    if not t.is_cuda or (of_elem != 1 and dh > 1) or (of_head != dh and heads > 1) or (step < heads * dh and not few):
+        raise ValueError(f"{name}: must be a CUDA tensor whose heads lie behind each other")
+    if t.get_device() != at:
+        raise ValueError(f"{name}: must be on the same device as the others")
+    return t.data_ptr(), heads * dh if few else step
+
+
+def _page_args(table, length, page_size, free, n_free, i):
+    B, max_pages = table.shape
+    i32 = torch.int32
+    return (_int32(B, "B"), _int32(free.numel(), "n_pages"), _int32(page_size, "page_size"), _int32(max_pages, "max_pages")), (
+        _dev_on(table, i32, 0, "table", i), _dev_on(length, i32, B, "length", i), _dev_on(free, i32, 0, "free", i), _dev_on(n_free, i32, 1, "n_free", i))
+
+
+def kv_reserve(table, length, n_new, page_size, free, n_free, tok_off, n_got, pos=None, slot=None, seen=None, rows=None, dev_status=None, stream=None):
+    """Pages for the n_new[b] tokens behind the length[b] slots in use of each sequence, from the stack free [n_pages] of n_free [1] pages; tok_off
+    [B + 1], n_got [B] and, of the packed batch's rows, pos and slot [T] are written.  rows: T where neither is given, or fewer than they hold."""
+    i, st = _device_of(table, stream)
+    i32 = torch.int32
+    dims, (t, n, f, nf) = _page_args(table, length, page_size, free, n_free, i)
+    B = dims[0]
+    have = [x.numel() for x in (pos, slot) if x is not None]
+    T = _int32(rows if rows is not None else min(have) if have else 1 << 21, "rows")
+    rc = _lib.moa_kv_reserve(*dims, n, _dev_on(n_new, i32, B, "n_new", i), _dev_on(seen, i32, B, "seen", i), t, f, nf, T, _dev_on(tok_off, i32, B + 1, "tok_off", i),
+                             _dev_on(n_got, i32, B, "n_got", i), _dev_on(pos, i32, T, "pos", i), _dev_on(slot, i32, T, "slot", i),
+                             _dev_on(dev_status, i32, 1, "dev_status", i), st)
+    if rc:
+        _check(rc)
+
+
+def kv_release(table, length, page_size, free, n_free, dev_status=None, stream=None):
+    """Pages that the table names behind the length[b] slots in use of each sequence go back to the stack."""
+    i, st = _device_of(table, stream)
+    dims, (t, n, f, nf) = _page_args(table, length, page_size, free, n_free, i)
+    rc = _lib.moa_kv_release(*dims, n, t, f, nf, _dev_on(dev_status, torch.int32, 1, "dev_status", i), st)
+    if rc:
+        _check(rc)
+
+
+def qk_norm_rope(q, k, q_out, k_out, pos, rope_theta=10000.0, rot_dim=None, gq=None, gk=None, rms_eps=1e-6, stream=None):
+    """Queries [T, H, dh] and keys [T, Hkv, dh] normalised per head (where gq / gk [dh] are given) and rotated to pos [T]; either may be None.  Their
+    rows may be parts of one projection's output, and the results may be written over them.  rot_dim: dims that are rotated (None: all; 0: none)."""
+    some = q if q is not None else k
+    if some is None:
+        raise ValueError("q and k: one of them must be given")
+    i, st = _device_of(some, stream)
+    T, _, dh = some.shape
+    dt = some.dtype
+    if dt not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"q: dtype {dt}, expected float32 or bfloat16")
+    if q is not None and k is not None and k.shape[0] != T:
+        raise ValueError("q and k: must have the same number of rows")
+    at = []
+    for x, y, names in ((q, q_out, ("q", "q_out")), (k, k_out, ("k", "k_out"))):
+        if x is None:
+            at.append((None, 0, 0, None, 0))
+            continue
+        heads = x.shape[1]
+        xp, xs = _rows_on(x, dt, heads, dh, names[0], i)
+        if y is None or y.shape != x.shape:
+            raise ValueError(f"{names[1]}: must be as {names[0]}")
+        yp, ys = _rows_on(y, dt, heads, dh, names[1], i)
+        at.append((xp, xs, _int32(heads, "heads"), yp, ys))
+    (qp, qs, H, qop, qos), (kp, ks, Hkv, kop, kos) = at
+    rot = dh if rot_dim is None else _int32(rot_dim, "rot_dim")
+    rc = _lib.moa_qk_norm_rope(F32 if dt == torch.float32 else BF16, qp, qs, H, kp, ks, Hkv, T, _int32(dh, "dh"), _dev_on(gq, dt, dh, "gq", i),
+                               _dev_on(gk, dt, dh, "gk", i), float(rms_eps), _dev_on(pos, torch.int32, T, "pos", i), float(rope_theta), rot, qop, qos, kop, kos, st)
+    if rc:
+        _check(rc)
+
+
+class QuantKVCache:
+    """moa_kvq_cache_t: a KV cache in pages held in 8 bits.  k, v [n_pages, Hkv, page_size, dh] float8_e4m3fn; k_scale, v_scale [n_pages, Hkv,
+    ceil(page_size / KVQ_BLOCK)] fp32; table [B, max_pages], len [B] int32; dtype: torch.float32 or torch.bfloat16, of the rows given, queries
+    and results.  The tensors are checked here, once, and kept alive; their contents belong to the caller."""
+
+    k, v, k_scale, v_scale, table, len = (property(lambda self, i=i: self._tensors[i]) for i in range(6))
+
+    def __init__(self, k, v, k_scale, v_scale, table, len, dtype):
+        n_pages, Hkv, page_size, dh = k.shape
+        B, max_pages = table.shape
+        if v.shape != k.shape:
+            raise ValueError("k and v: must have the same shape")
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"dtype {dtype}, expected float32 or bfloat16")
+        blocks = (n_pages, Hkv, (page_size + KVQ_BLOCK - 1) // KVQ_BLOCK)
+        if tuple(k_scale.shape) != blocks or tuple(v_scale.shape) != blocks:
+            raise ValueError(f"k_scale and v_scale: must be {list(blocks)}")
+        code, i32 = torch.float8_e4m3fn, torch.int32
+        self._index = i = k.get_device()
+        self._c = _KvqCache(F32 if dtype == torch.float32 else BF16, *(_int32(n, "the cache's dimensions") for n in (Hkv, dh, B, n_pages, page_size, max_pages)),
+                            _dev(k, code, 0, "k"), _dev_on(v, code, 0, "v", i), _dev_on(k_scale, torch.float32, 0, "k_scale", i),
+                            _dev_on(v_scale, torch.float32, 0, "v_scale", i), _dev_on(table, i32, 0, "table", i), _dev_on(len, i32, B, "len", i))
+        self._ref = C.byref(self._c)
+        self._dtype, self._dims = dtype, (B, Hkv, dh)
+        self._tensors = k, v, k_scale, v_scale, table, len
+
+    _stream = KVCache._stream
+
+
+def kvq_append(cache: QuantKVCache, k_new, v_new, path=None, n_new=None, dev_status=None, stream=None):
+    """kv_append for a cache held in 8 bits: rows path[b][:n_new[b]] of k_new / v_new [B, Hkv, M, dh] are encoded into the slots behind len[b]."""
+    shape = k_new.shape
+    B, Hkv, dh = cache._dims
+    if len(shape) != 4 or shape[0] != B or shape[1] != Hkv or shape[3] != dh or v_new.shape != shape:
+        raise ValueError("k_new and v_new: must be [B, Hkv, M, dh] of the cache")
+    M, i, dt, i32 = _int32(shape[2], "M"), cache._index, cache._dtype, torch.int32
+    n = B * Hkv * M * dh
+    at = _dev_on(path, i32, B * M, "path", i)
+    _per_sequence(path, B, M, "path")
+    rc = _lib.moa_kvq_append(cache._ref, _dev_on(k_new, dt, n, "k_new", i), _dev_on(v_new, dt, n, "v_new", i), M, at, _dev_on(n_new, i32, B, "n_new", i),
+                             _dev_on(dev_status, i32, 1, "dev_status", i), cache._stream(stream))
+    if rc:
+        _check(rc)
+
+
+def kvq_append_rows(cache: QuantKVCache, k_new, v_new, tok_off, n_new=None, dev_status=None, stream=None):
+    """kvq_append of a packed batch: rows tok_off[b] .. tok_off[b + 1] - 1 (the first n_new[b] of them) of k_new / v_new [T, Hkv, dh], whose rows may
+    be parts of a projection's output."""
+    B, Hkv, dh = cache._dims
+    i, dt, i32 = cache._index, cache._dtype, torch.int32
+    kp, ks = _rows_on(k_new, dt, Hkv, dh, "k_new", i)
+    vp, vs = _rows_on(v_new, dt, Hkv, dh, "v_new", i)
+    T = _int32(k_new.shape[0], "T")
+    if v_new.shape[0] != T:
+        raise ValueError("k_new and v_new: must have the same number of rows")
+    rc = _lib.moa_kvq_append_rows(cache._ref, kp, ks, vp, vs, T, _dev_on(tok_off, i32, B + 1, "tok_off", i), _dev_on(n_new, i32, B, "n_new", i),
+                                  _dev_on(dev_status, i32, 1, "dev_status", i), cache._stream(stream))
+    if rc:
+        _check(rc)
+
+
+def kvq_read(cache: QuantKVCache, k_out, v_out, dev_status=None, stream=None):
+    """The rows of each sequence's slots as values, into k_out, v_out [B, Hkv, P_cap, dh]; rows behind its length are left as they were."""
+    shape = k_out.shape
+    B, Hkv, dh = cache._dims
+    if len(shape) != 4 or shape[0] != B or shape[1] != Hkv or shape[3] != dh or v_out.shape != shape:
+        raise ValueError("k_out and v_out: must be [B, Hkv, P_cap, dh] of the cache")
+    P, i, dt = _int32(shape[2], "P_cap"), cache._index, cache._dtype
+    n = B * Hkv * P * dh
+    rc = _lib.moa_kvq_read(cache._ref, P, _dev_on(k_out, dt, n, "k_out", i), _dev_on(v_out, dt, n, "v_out", i),
+                           _dev_on(dev_status, torch.int32, 1, "dev_status", i), cache._stream(stream))
+    if rc:
+        _check(rc)
+
+
+def kvq_decode_attn_workspace_bytes(cache: QuantKVCache, n_q_heads: int) -> int:
+    out = _sz(0)
+    _check(_lib.moa_kvq_decode_attn_workspace_bytes(cache._ref, _int32(n_q_heads, "n_q_heads"), C.byref(out)))
+    return int(out.value)
+
+
+def kvq_decode_attn(cache: QuantKVCache, q, out, ws, dev_status=None, stream=None):
+    """Attention of one new token per sequence (q, out [B, H, dh]) over a cache held in 8 bits."""
+    shape = q.shape
+    B, _, dh = cache._dims
+    if len(shape) != 3 or shape[0] != B or shape[2] != dh:
+        raise ValueError("q: must be [B, H, dh] of the cache")
+    H, i, dt = _int32(shape[1], "H"), cache._index, cache._dtype
+    n = B * H * dh
+    wsp, wsb = _room_on(ws, "ws", i)
+    rc = _lib.moa_kvq_decode_attn(cache._ref, H, _dev_on(q, dt, n, "q", i), _dev_on(out, dt, n, "out", i), _dev_on(dev_status, torch.int32, 1, "dev_status", i),
+                                  wsp, wsb, cache._stream(stream))
     if rc:
         _check(rc)
 

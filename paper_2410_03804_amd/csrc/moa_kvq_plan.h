@@ -1,0 +1,28 @@
+// Which form the attention of one token per sequence over a cache held in 8 bits takes (moa_kvq_decode.hip) and what workspace it
+// needs.  Host arithmetic only, so that a test on a machine without a GPU can go through it.
+#pragma once
+#include "moa_decode_plan.h"
+
+namespace moa {
+
+struct KvqPlan {
+    int HG, rtiles, runs;              // query heads in a tile; tiles per KV head; workgroups, 0: one per pair
+    size_t part_o, part_ml;            // bytes
+    size_t total() const { return part_o + part_ml; }
+};
+
+inline KvqPlan kvq_plan(int B, int Hkv, int dh, int cap, int H)
+{
+    auto align256 = [](size_t n) { return (n + 255) & ~(size_t)255; };
+    KvqPlan p;
+    const int G = H / Hkv;
+    p.HG = G < 4 ? G : 4;
+    p.rtiles = (G + p.HG - 1) / p.HG;
+    const int64_t pairs = (int64_t)B * Hkv * p.rtiles;
+    p.runs = cap <= 512 ? 0 : 1024;
+    p.part_o = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * dh * 4) : 0;
+    p.part_ml = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * 2 * 4) : 0;
+    return p;
+}
+
+}  // namespace moa
