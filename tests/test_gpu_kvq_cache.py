@@ -1,0 +1,279 @@
+"""moa_kvq_append, moa_kvq_append_rows and moa_kvq_read against their definitions in 64 bits: every code, scale and length, and every byte that is
+not theirs to write."""
+import numpy as np
+import pytest
+import torch
+
+import kvq_util as U
+import paper_2410_03804_amd as moa
+
+pytestmark = pytest.mark.gpu
+
+TINY, B8, SA, ODD, ODDF, D33, D33F, WIDE, ONE = ((4, 2, 64, "f32"), (32, 8, 128, "bf16"), (32, 4, 128, "bf16"), (6, 2, 80, "bf16"), (6, 2, 80, "f32"),
+                                                 (3, 3, 33, "bf16"), (3, 1, 33, "f32"), (4, 1, 256, "bf16"), (2, 2, 1, "bf16"))
+
+
+def values(rng, shape, kind="normal"):
+    """Rows whose size differs by block and head, so that scales grow and stay."""
+    x = rng.standard_normal(shape) * np.exp2(rng.integers(-3, 4, shape[:-1] + (1,)))
+    if kind == "zeros":
+        x[rng.random(shape[:-1]) < 0.6] = 0.0
+    if kind == "wide":                              # all sizes that single precision has, denormal numbers among them
+        x = np.sign(x) * np.exp2(rng.uniform(-149, 127.9, shape[:-1] + (1,)) - rng.uniform(0, 12, shape))
+    if kind == "special":
+        x[rng.random(shape) < 0.05] = np.inf
+        x[rng.random(shape) < 0.05] = -np.inf
+        x[rng.random(shape) < 0.05] = np.nan
+    if kind == "ties":
+        x = np.sign(x) * rng.integers(0, 449, shape) * 0.5
+    return x.astype(np.float32)
+
+
+def given(c, x):
+    t = torch.from_numpy(x).to(U.TDT[c.dtype])
+    return t.to("cuda"), t.double().numpy()
+
+
+def append_slab(c, new, M, kind="normal", path=False):
+    rng = c.rng
+    B = len(c.lens)
+    (k, kd), (v, vd) = (given(c, values(rng, (B, c.Hkv, M, c.dh), kind)) for _ in range(2))
+    p = np.stack([rng.integers(0, M, M) for _ in range(B)]).astype(np.int32) if path else np.tile(np.arange(M, dtype=np.int32), (B, 1))
+    cache = c.moa()
+    moa.kvq_append(cache, k, v, path=torch.from_numpy(p).cuda() if path else None, n_new=None if new is None else torch.tensor(new, dtype=torch.int32, device="cuda"),
+                   dev_status=c.status)
+    torch.cuda.synchronize()
+    new = new or [M] * B
+    c.append([(kd[b][:, p[b, :new[b]]], vd[b][:, p[b, :new[b]]]) for b in range(B)])
+
+
+@pytest.mark.parametrize("kind", ["normal", "zeros", "wide", "special", "ties"])
+@pytest.mark.parametrize("heads", [TINY, B8, ODD, ODDF, D33, D33F, WIDE, ONE], ids=str)
+def test_rows_of_every_kind(heads, kind):
+    c = U.QCache(heads, [0, 1, 15, 16, 37], 16, seed=5, room=60)
+    append_slab(c, [1, 20, 1, 60, 0], 60, kind)
+    c.check_state("first")
+    append_slab(c, [0, 3, 17, 0, 7], 17, kind)
+    c.check_state("second")
+    assert c.status.item() == 0
+
+
+@pytest.mark.parametrize("page", [1, 7, 16, 24, 40, 100])
+@pytest.mark.parametrize("heads", [TINY, B8, D33], ids=str)
+def test_pages_of_every_size(heads, page):
+    c = U.QCache(heads, [0, 5, 16, 99], page, seed=6, room=151)
+    append_slab(c, [100, 1, 150, 33], 150)
+    c.check_state("many")
+    append_slab(c, None, 1)
+    c.check_state("one each")
+    assert c.status.item() == 0
+
+
+def test_one_token_at_a_time_is_every_block_s_history():
+    c = U.QCache(SA, [3, 0], 40, seed=7, room=70)
+    for step in range(60):
+        append_slab(c, None, 1, "wide" if step % 9 == 4 else "normal")
+    c.check_state("sixty tokens")
+    grown = np.isfinite(c.scales[0]).sum()
+    assert grown >= 2 * c.Hkv * 4 and c.status.item() == 0
+
+
+@pytest.mark.parametrize("heads", [TINY, B8, ODDF], ids=str)
+def test_accepted_nodes(heads):
+    c = U.QCache(heads, [10, 0, 200], 32, seed=8, room=40)
+    append_slab(c, [7, 1, 0], 60, path=True)
+    append_slab(c, [2, 25, 9], 25, path=True)                # the same node twice is two rows
+    c.check_state("path")
+    assert c.status.item() == 0
+
+
+@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("heads", [TINY, B8, ODD, D33, D33F], ids=str)
+def test_packed_rows_of_a_projection(heads, many):
+    scale = 40 if many else 1
+    new = [x * scale for x in (5, 0, 17, 1)]
+    c = U.QCache(heads, [0, 9, 31, 16], 48, seed=9, room=17 * scale + 2)
+    rng, T = c.rng, sum(new) + 3
+    x = values(rng, (T, c.H + 2 * c.Hkv, c.dh))
+    dev, d = given(c, x)
+    k, v = dev[:, c.H:c.H + c.Hkv], dev[:, c.H + c.Hkv:]
+    off = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    moa.kvq_append_rows(c.moa(), k, v, torch.from_numpy(off).cuda(), dev_status=c.status)
+    torch.cuda.synchronize()
+    part = lambda b, n, first: d[off[b]:off[b] + n, first:first + c.Hkv].transpose(1, 0, 2)
+    c.append([(part(b, n, c.H), part(b, n, c.H + c.Hkv)) for b, n in enumerate(new)])
+    c.check_state("packed")
+    # fewer of them than there are rows
+    if not many:
+        got = [2, 0, 0, 1]
+        moa.kvq_append_rows(c.moa(), k, v, torch.from_numpy(off).cuda(), n_new=torch.tensor(got, dtype=torch.int32, device="cuda"), dev_status=c.status)
+        torch.cuda.synchronize()
+        c.append([(part(b, n, c.H), part(b, n, c.H + c.Hkv)) for b, n in enumerate(got)])
+        c.check_state("fewer")
+    assert c.status.item() == 0
+
+
+@pytest.mark.parametrize("offset", [1, 4, 8])
+def test_codes_that_are_not_aligned(offset):
+    for heads in (TINY, B8):
+        c = U.QCache(heads, [3, 40], 16, seed=10, room=30, offset=offset)
+        append_slab(c, [30, 11], 30)
+        c.check_state(offset)
+
+
+def test_rows_that_are_not_aligned():
+    c = U.QCache(B8, [3, 40], 16, seed=11, room=30)
+    n = 2 * c.Hkv * 5 * c.dh
+    flat = torch.randn(2 * n + 3, device="cuda").to(torch.bfloat16)
+    k, v = flat[3:3 + n].view(2, c.Hkv, 5, c.dh), flat[3 + n:3 + 2 * n].view(2, c.Hkv, 5, c.dh)
+    moa.kvq_append(c.moa(), k, v)
+    c.append([(U.host(k)[b], U.host(v)[b]) for b in range(2)])
+    c.check_state("rows")
+
+
+def test_a_scale_that_is_no_power_of_two_is_kept_or_grows_out_of():
+    """A block quantised elsewhere: where its scale is large enough, new rows are divided by it; else it becomes a power of two and the rows held
+    are rounded once more, code * (old / new) in single precision."""
+    c = U.QCache(TINY, [5, 5], 16, seed=12, room=16)
+    for w in range(2):
+        c.scales[w][c.table[0, 0]] = np.float32(0.3)
+        c.scales[w][c.table[1, 0]] = np.float32(0.3 / 128)
+    c.upload()
+    x = c.rng.uniform(-100, 100, (2, c.Hkv, 3, c.dh)).astype(np.float32)
+    x[:, :, 0, 0] = 100.0
+    k = torch.from_numpy(x).cuda()
+    moa.kvq_append(c.moa(), k, k)
+    torch.cuda.synchronize()
+    codes, scales = c.downloaded()
+    for w in range(2):
+        p = c.table[0, 0]
+        assert np.all(scales[w][p] == np.float32(0.3))
+        want = U.encode((x[0] / np.float32(0.3)).astype(np.float64))
+        assert np.array_equal(codes[w][p, :, 5:8], want) and np.array_equal(codes[w][p, :, :5], c.codes[w][p, :, :5])
+        p = c.table[1, 0]
+        assert np.all(scales[w][p] == 0.25)
+        held = U.VALUES[c.codes[w][p, :, :5]].astype(np.float32) * (np.float32(0.3 / 128) / np.float32(0.25))
+        assert np.array_equal(codes[w][p, :, :5], U.encode(held.astype(np.float64)))
+        assert np.array_equal(codes[w][p, :, 5:8], U.encode(x[1].astype(np.float64) / 0.25))
+
+
+@pytest.mark.parametrize("M", [3, 90])
+def test_numbers_outside_their_ranges_are_clamped_and_said(M):
+    c = U.QCache(B8, [4, 10, 70, 0], 16, seed=13, room=20, mp=6)                # a capacity of 96
+    (k, kd), (v, vd) = (given(c, values(c.rng, (4, c.Hkv, M, c.dh))) for _ in range(2))
+    c.table[0, 1] = 1 << 28                                                     # no page where rows are wanted
+    c.t_table.copy_(torch.from_numpy(c.table))
+    new = [M, -5, M, 2]
+    path = np.tile(np.arange(M, dtype=np.int32), (4, 1))
+    path[3, :2] = (-7, M)
+    c.t_len[1] = 10
+    moa.kvq_append(c.moa(), k, v, path=torch.from_numpy(path).cuda(), n_new=torch.tensor(new, dtype=torch.int32, device="cuda"), dev_status=c.status)
+    torch.cuda.synchronize()
+    want = moa.DEV_BAD_LENGTH | moa.DEV_BAD_PARENT
+    assert c.status.item() & want == want
+    assert bool(c.status.item() & moa.DEV_CACHE_FULL) == (M > 26)
+    assert c.t_len.tolist() == [4 + min(M, 92), 10, 70 + min(M, 26), 2]
+    codes, _ = c.downloaded()
+    p = c.table[3, 0]
+    x = np.stack([kd[3][:, 0], kd[3][:, M - 1]], 1)
+    for h in range(c.Hkv):
+        assert np.array_equal(codes[0][p, h, :2], U.encode(x[h] / U.smallest_scale(x[h])))
+
+
+def test_a_row_without_a_page_is_counted_and_not_written():
+    c = U.QCache(TINY, [10], 16, seed=14, room=40)
+    lost = int(c.table[0, 1])
+    c.table[0, 1] = -1
+    c.upload()
+    k, kd = given(c, values(c.rng, (1, c.Hkv, 30, c.dh)))
+    moa.kvq_append(c.moa(), k, k, dev_status=c.status)
+    torch.cuda.synchronize()
+    assert c.status.item() == moa.DEV_BAD_PAGE and c.t_len.tolist() == [40]
+    codes, scales = c.downloaded()
+    assert np.all(codes[0][lost] == c.codes[0][lost]) and np.isnan(scales[0][lost]).all()
+    p = int(c.table[0, 2])
+    for h in range(c.Hkv):
+        x = kd[0, h, 22:30]
+        assert np.array_equal(codes[1][p, h, :8], U.encode(x / U.smallest_scale(x)))
+
+
+def test_offsets_that_are_none_touch_nothing_else():
+    c = U.QCache(B8, [4, 10, 0], 16, seed=15, room=20)
+    T = 8
+    dev, d = given(c, values(c.rng, (T, c.Hkv, c.dh)))
+    for off, n, got in (([0, 6, 3, 8], None, [6, 0, 5]), ([-4, 2, 100, 100], None, [2, 6, 0]), ([0, 2, 4, 6], [3, -1, 2], [2, 0, 2])):
+        c.status.zero_()
+        before = list(c.lens)
+        moa.kvq_append_rows(c.moa(), dev, dev, torch.tensor(off, dtype=torch.int32, device="cuda"),
+                            n_new=None if n is None else torch.tensor(n, dtype=torch.int32, device="cuda"), dev_status=c.status)
+        torch.cuda.synchronize()
+        assert c.status.item() == moa.DEV_BAD_LENGTH, off
+        first = [min(max(o, 0), T) for o in off]
+        c.append([(d[first[b]:first[b] + got[b]].transpose(1, 0, 2),) * 2 for b in range(3)])
+        assert [a - b for a, b in zip(c.lens, before)] == got
+        c.check_state(off)
+
+
+# ---------------------------------------------------------------- read
+
+@pytest.mark.parametrize("page", [1, 16, 40, 300])
+@pytest.mark.parametrize("heads", [TINY, B8, ODD, ODDF, D33, WIDE, ONE], ids=str)
+def test_read_gives_the_values(heads, page):
+    c = U.QCache(heads, [0, 1, 15, 33, 290], page, seed=16)
+    P = 300
+    out = [torch.full((5, c.Hkv, P, c.dh), 7.0, dtype=U.TDT[c.dtype], device="cuda") for _ in range(2)]
+    moa.kvq_read(c.moa(), *out, dev_status=c.status)
+    torch.cuda.synchronize()
+    for w in range(2):
+        got = U.host(out[w])
+        for b, n in enumerate(c.lens):
+            for h in range(c.Hkv):
+                assert np.array_equal(got[b, h, :n], c.rows(w, b, h, n))           # (four significant bits: exact in either type)
+            assert np.all(got[b, :, n:] == 7.0)
+    assert c.status.item() == 0
+
+
+def test_read_of_less_than_there_is_and_of_what_is_not_there():
+    c = U.QCache(B8, [50, 20], 16, seed=17)
+    c.table[0, 1] = 1 << 28
+    c.upload()
+    out = [torch.full((2, c.Hkv, 33, c.dh), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    moa.kvq_read(c.moa(), *out, dev_status=c.status)
+    torch.cuda.synchronize()
+    assert c.status.item() == moa.DEV_CACHE_FULL | moa.DEV_BAD_PAGE
+    got = U.host(out[1])
+    for h in range(c.Hkv):
+        assert np.array_equal(got[1, h, :20], c.rows(1, 1, h, 20)) and np.array_equal(got[0, h, :16], c.rows(1, 0, h, 16))
+    assert np.all(got[0, :, 16:32] == 7.0) and np.all(got[1, :, 20:] == 7.0)
+
+
+def test_read_into_rows_that_are_not_aligned():
+    c = U.QCache(B8, [50, 20], 16, seed=18, offset=3)
+    n = 2 * c.Hkv * 50 * c.dh
+    flat = torch.zeros(2 * n + 1, dtype=torch.bfloat16, device="cuda")
+    out = [flat[1 + w * n:1 + (w + 1) * n].view(2, c.Hkv, 50, c.dh) for w in range(2)]
+    moa.kvq_read(c.moa(), *out)
+    for w in range(2):
+        assert np.array_equal(U.host(out[w])[1, 3, :20], c.rows(w, 1, 3, 20))
+    assert flat[0].item() == 0.0
+
+
+def test_pages_beyond_4_gib():
+    """Offsets of codes that pass 32 bits: 2^21 rows of 128 heads' worth in one pool."""
+    n_pages, page, Hkv, dh = 1100, 256, 64, 256                                     # 4.6e9 codes
+    k = torch.zeros(n_pages, Hkv, page, dh, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    scale = torch.ones(n_pages, Hkv, page // 16, device="cuda")
+    table = torch.tensor([[n_pages - 1, 3]], dtype=torch.int32, device="cuda")
+    length = torch.tensor([250], dtype=torch.int32, device="cuda")
+    cache = moa.QuantKVCache(k, k, scale, scale, table, length, torch.bfloat16)
+    new = torch.randn(1, Hkv, 10, dh, device="cuda").to(torch.bfloat16)
+    moa.kvq_append(cache, new, new)
+    out = torch.zeros(1, Hkv, 260, dh, dtype=torch.bfloat16, device="cuda")
+    other = torch.zeros_like(out)
+    moa.kvq_read(cache, out, other)
+    x = U.host(new)[0]
+    for h in (0, 63):
+        # (the block in front holds rows of scale 1, which is the larger one)
+        assert np.array_equal(U.host(out)[0, h, 250:256], U.VALUES[U.encode(x[h, :6])])
+        s = U.smallest_scale(x[h, 6:])
+        assert np.array_equal(U.host(out)[0, h, 256:260], U.VALUES[U.encode(x[h, 6:] / s)] * s)

@@ -1,0 +1,221 @@
+"""moa_kvq_decode_attn against attention in 64 bits over what the codes stand for, with bounds derived beside it (kvq_util.decode_reference)."""
+import numpy as np
+import pytest
+import torch
+
+import kvq_util as U
+import paper_2410_03804_amd as moa
+
+pytestmark = pytest.mark.gpu
+
+TINY, B8, B70, SA, ODD, ODDF, D33, D33F, WIDE, WIDEF, ONE, MANY, MANYF = (
+    (4, 2, 64, "f32"), (32, 8, 128, "bf16"), (64, 8, 128, "bf16"), (32, 4, 128, "bf16"), (6, 2, 80, "bf16"), (6, 2, 80, "f32"), (3, 3, 33, "bf16"), (3, 1, 33, "f32"),
+    (4, 1, 256, "bf16"), (10, 2, 256, "f32"), (2, 2, 1, "bf16"), (40, 1, 64, "bf16"), (17, 1, 112, "f32"))
+
+
+def queries(c, scale=1.5, offset=0):
+    B = len(c.lens)
+    n = B * c.H * c.dh
+    flat = torch.from_numpy((scale * c.rng.standard_normal(n + offset)).astype(np.float32)).to(U.TDT[c.dtype]).cuda()
+    return flat[offset:].view(B, c.H, c.dh)
+
+
+def attend(c, q, ws=None, cache=None):
+    cache = cache or c.moa()
+    out = torch.full(q.shape, 77.0, dtype=q.dtype, device="cuda")
+    ws = U.workspace(moa.kvq_decode_attn_workspace_bytes(cache, c.H)) if ws is None else ws
+    moa.kvq_decode_attn(cache, q, out, ws, dev_status=c.status)
+    torch.cuda.synchronize()
+    return out
+
+
+def both(c, q, what, skip=()):
+    out = attend(c, q)
+    want, tol = U.decode_reference(c, q, skip)
+    U.check(out, want, tol, what)
+    return out
+
+
+@pytest.mark.parametrize("lens", [[1], [2, 1, 31], [16, 17, 32, 33], [127, 128, 129, 0, 5], [500], [513, 40], [1500, 3, 700]], ids=str)
+@pytest.mark.parametrize("heads", [TINY, B8, B70, SA, ODD, ODDF, D33, D33F, WIDE, WIDEF, ONE, MANY, MANYF], ids=str)
+def test_lengths_and_heads(heads, lens):
+    c = U.QCache(heads, lens, 16, seed=sum(lens))
+    both(c, queries(c), f"{heads} {lens}")
+    assert c.status.item() == (moa.DEV_EMPTY_KEYS if 0 in lens else 0)
+
+
+@pytest.mark.parametrize("page", [1, 5, 24, 40, 64, 1000, 4097])
+@pytest.mark.parametrize("heads", [TINY, B8, ODD], ids=str)
+def test_pages_of_every_size(heads, page):
+    c = U.QCache(heads, [900, 17, 333], page, seed=page)
+    both(c, queries(c), f"{heads} page {page}")
+    assert c.status.item() == 0
+
+
+@pytest.mark.parametrize("heads", [TINY, B8, SA, WIDEF], ids=str)
+def test_long_and_ragged(heads):
+    c = U.QCache(heads, [9000, 1, 0, 4097, 128], 64, seed=3)
+    out = both(c, queries(c), f"{heads} ragged")
+    assert c.status.item() == moa.DEV_EMPTY_KEYS and torch.all(out[2] == 0)
+
+
+def test_many_sequences():
+    rng = np.random.default_rng(4)
+    c = U.QCache(ODD, [int(n) for n in rng.integers(0, 700, 130)], 32, seed=4)
+    both(c, queries(c), "130 sequences")
+
+
+@pytest.mark.parametrize("offset", [1, 4, 8])
+@pytest.mark.parametrize("heads", [TINY, B8], ids=str)
+def test_codes_and_queries_that_are_not_aligned(heads, offset):
+    c = U.QCache(heads, [700, 33], 16, seed=5, offset=offset)
+    both(c, queries(c), f"{heads} codes at {offset}")
+    c = U.QCache(heads, [700, 33], 16, seed=5)
+    both(c, queries(c, offset=1), f"{heads} queries at 1")
+
+
+@pytest.mark.parametrize("heads", [TINY, B8, D33], ids=str)
+def test_scales_that_span_everything(heads):
+    """Scales of neighbouring blocks 2^40 apart, and ones that are no powers of two."""
+    c = U.QCache(heads, [300, 90], 16, seed=6)
+    for w in range(2):
+        s = c.scales[w]
+        e = c.rng.integers(-30, 11, s.shape) if w else c.rng.integers(-14, -8, s.shape)
+        c.scales[w] = np.where(np.isfinite(s), np.ldexp(c.rng.uniform(1, 2, s.shape), e), np.nan).astype(np.float32)
+    c.upload()
+    both(c, queries(c), f"{heads} scales")
+
+
+@pytest.mark.parametrize("heads", [TINY, B8, WIDE], ids=str)
+def test_large_scores(heads):
+    """One key far ahead of all others, and all of them alike far from zero."""
+    c = U.QCache(heads, [200, 650], 16, seed=7)
+    both(c, queries(c, scale=200.0), f"{heads} sharp")
+    for b, n in enumerate(c.lens):
+        s = np.arange(n)
+        c.codes[0][c.table[b, s // 16], :, s % 16] = c.codes[0][c.table[b, 0], :, 0]
+        c.scales[0][c.table[b, s // 16]] = 2.0 ** -5
+    c.upload()
+    both(c, queries(c, scale=200.0), f"{heads} alike")
+
+
+@pytest.mark.parametrize("n", [40, 900])
+@pytest.mark.parametrize("heads", [TINY, B8, D33], ids=str)
+def test_slots_without_a_page_are_left_out(heads, n):
+    c = U.QCache(heads, [n, n - 9], 16, seed=8)
+    gone = [(0, 1), (1, 0), (1, (n - 10) // 16)]
+    for b, p in gone:
+        c.table[b, p] = -1 if p else 1 << 30
+    c.upload()
+    both(c, queries(c), f"{heads} holes", skip=set(gone))
+    # (of the shorter one's 31 slots none is left)
+    assert c.status.item() == moa.DEV_BAD_PAGE | (moa.DEV_EMPTY_KEYS if n == 40 else 0)
+    c.table[0, :] = -1
+    c.upload()
+    c.status.zero_()
+    skip = {(0, p) for p in range(c.mp)} | set(gone)
+    out = both(c, queries(c), f"{heads} none", skip=skip)
+    assert c.status.item() == moa.DEV_BAD_PAGE | moa.DEV_EMPTY_KEYS and torch.all(out[0] == 0)
+
+
+@pytest.mark.parametrize("n", [40, 900])
+@pytest.mark.parametrize("heads", [TINY, B8, D33], ids=str)
+def test_what_is_not_a_number_reaches_its_own_results_only(heads, n):
+    c = U.QCache(heads, [n, n], 16, seed=9)
+    q = queries(c)
+    want, tol = U.decode_reference(c, q)
+    G = c.H // c.Hkv
+    p = c.table[0, (n - 3) // 16]
+    c.codes[0][p, 0, (n - 3) % 16, 0] = U.NAN            # a key of sequence 0, KV head 0: its query heads have no softmax
+    p1 = c.table[1, 1]
+    c.codes[1][p1, c.Hkv - 1, 4, c.dh - 1] = 0x80 | U.NAN    # a value of sequence 1: its dimension alone
+    c.upload()
+    out = U.host(attend(c, q))
+    assert np.all(np.isnan(out[0, :G]))
+    assert np.all(np.isnan(out[1, -G:, c.dh - 1]))
+    fine = np.ones(out.shape, bool)
+    fine[0, :G] = False
+    fine[1, -G:, c.dh - 1] = False
+    assert np.all(np.isfinite(out[fine])) and np.all(np.abs(out - want)[fine] <= tol[fine])
+
+
+@pytest.mark.parametrize("heads", [TINY, B8], ids=str)
+def test_queries_that_have_no_softmax(heads):
+    c = U.QCache(heads, [60, 600], 16, seed=10)
+    c.codes[0][..., 0] = np.where(c.codes[0][..., 0] & 0x7F == U.NAN, U.NAN, 0x40)      # keys whose first number is positive
+    c.upload()
+    q = queries(c)
+    q[0, 0, 0], q[0, 1, 0], q[1, 2, 0], q[1, 3, 0] = float("nan"), float("inf"), -float("inf"), float("inf")
+    out = U.host(attend(c, q))
+    assert np.all(np.isnan(out[0, :2])) and np.all(np.isnan(out[1, 2:4]))
+    assert np.all(np.isfinite(out[0, 2:])) and np.all(np.isfinite(out[1, :2])) and np.all(np.isfinite(out[1, 4:]))
+
+
+def test_lengths_that_are_none():
+    c = U.QCache(B8, [100, 60], 16, seed=11, room=0)
+    q = queries(c)
+    c.t_len.copy_(torch.tensor([-3, 10 ** 6], dtype=torch.int32))
+    out = attend(c, q)
+    assert c.status.item() & moa.DEV_BAD_LENGTH and c.status.item() & moa.DEV_EMPTY_KEYS and c.status.item() & moa.DEV_BAD_PAGE
+    assert torch.all(out[0] == 0)
+
+
+def test_sequences_share_pages():
+    c = U.QCache(B8, [700, 700, 650], 16, seed=12)
+    c.table[1, :40] = c.table[0, :40]
+    c.table[2, :40] = c.table[0, :40]
+    c.upload()
+    both(c, queries(c), "shared")
+
+
+@pytest.mark.parametrize("heads", [TINY, B8, D33], ids=str)
+def test_the_same_call_twice_has_the_same_bits_whatever_the_workspace_held(heads):
+    c = U.QCache(heads, [3000, 17, 1200], 16, seed=13)
+    q = queries(c)
+    cache = c.moa()
+    ws = U.workspace(moa.kvq_decode_attn_workspace_bytes(cache, c.H))
+    ws.fill_(0xFF)
+    a = attend(c, q, ws, cache)
+    ws.random_(0, 256)
+    assert torch.equal(a, attend(c, q, ws, cache))
+
+
+def test_on_another_stream_and_captured():
+    c = U.QCache(B8, [1500, 300], 16, seed=14, room=40)
+    cache, q = c.moa(), queries(c)
+    ws = U.workspace(moa.kvq_decode_attn_workspace_bytes(cache, c.H))
+    side = torch.cuda.Stream()
+    out = torch.zeros_like(q)
+    new = torch.randn(2, c.Hkv, 1, c.dh, device="cuda").to(torch.bfloat16)
+    side.wait_stream(torch.cuda.current_stream())
+    moa.kvq_decode_attn(cache, q, out, ws, dev_status=c.status, stream=side)
+    side.synchronize()
+    want, tol = U.decode_reference(c, q)
+    U.check(out, want, tol, "other stream")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        moa.kvq_append(cache, new, new, dev_status=c.status)
+        moa.kvq_decode_attn(cache, q, out, ws, dev_status=c.status)
+    for step in range(5):
+        new.copy_(torch.randn(new.shape, device="cuda"))
+        q.copy_(1.5 * torch.randn(q.shape, device="cuda"))
+        graph.replay()
+        x = U.host(new)
+        c.append([(x[b], x[b]) for b in range(2)])
+        want, tol = U.decode_reference(c, q)
+        U.check(out, want, tol, f"replay {step}")
+        c.check_state(f"replay {step}")
+        torch.cuda.synchronize()
+    assert c.status.item() == 0
+
+
+def test_random_calls():
+    rng = np.random.default_rng(15)
+    for i in range(25):
+        Hkv = int(rng.integers(1, 5))
+        heads = (Hkv * int(rng.integers(1, 20)), Hkv, int(rng.choice([8, 16, 24, 48, 64, 96, 100, 128, 160, 192, 208, 256])), str(rng.choice(["f32", "bf16"])))
+        lens = [int(n) for n in np.exp(rng.uniform(0, np.log(3000), int(rng.integers(1, 7)))).astype(int)]
+        page = int(rng.choice([1, 3, 16, 16, 33, 48, 64, 256]))
+        print(f"[case] {i}: {heads} {lens} page {page}", flush=True)
+        c = U.QCache(heads, lens, page, seed=100 + i)
+        both(c, queries(c), f"{i}")
