@@ -135,7 +135,286 @@ __global__ __launch_bounds__(256, 2) void k_kvq_decode(KvqDecodeArgs k)
     });
 }
 
+// ---------------------------------------------------------------- on the matrix cores: head_dim a multiple of 16
+// tiles that a wavefront holds in LDS, and the bytes of that
+constexpr int kvq_stages(int DH) { return 256 / DH; }
+constexpr uint32_t kvq_wave_bytes(int DH) { return kvq_stages(DH) * (2 * WK * DH + 512) + 128; }
+
+// x as the sum of N bf16 numbers, each the rounding of what the ones before leave: to 2^-8, 2^-16, 2^-24 of x
+template <int N>
+__device__ __forceinline__ void split_pair(float x0, float x1, uint32_t (&part)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        part[i] = pack_bf16x2(x0, x1);
+        x0 -= __uint_as_float(part[i] << 16);
+        x1 -= __uint_as_float(part[i] & 0xffff0000u);
+    }
+}
+
+typedef union { uint32_t w[4]; bf16x8 v; } Frag;
+
+// eight codes as bf16, which holds every one of them
+__device__ __forceinline__ bf16x8 widen(uint32_t c0, uint32_t c1)
+{
+    Frag f;
+    f.w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c0, 1.f, false));
+    f.w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c0, 1.f, true));
+    f.w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, 1.f, false));
+    f.w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, 1.f, true));
+    return f.v;
+}
+
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+
+// Sixteen query heads of a KV head are the columns of a tile: S^T = K Q^T, O^T += V^T P^T, codes widened to bf16 on their way into the matrix
+// cores.  Every wavefront walks its own 32 keys of each tile of the run, with LDS of its own for NST tiles, so that there is no barrier
+// before the run's end.  Codes go straight into LDS: a tile's keys take the place of those NST tiles before as soon as these have been used,
+// their scales and its values likewise, and its table entries come another NST tiles before that.
+// DH: head_dim as it lies in LDS; the rows in the pool may be shorter (PAD, a multiple of 16): their last pieces are then zeros.
+template <typename T, int DH, bool PAD>
+__global__ __launch_bounds__(256, 2) void k_kvq_decode_mfma(KvqDecodeArgs k)
+{
+    constexpr int PIECES = DH / 16, RPI = 64 / PIECES, NL = WK / RPI;      // 16-byte pieces of a row; rows of a load, loads of K (or V)
+    constexpr int NST = kvq_stages(DH), NKS = DH / 32, NDB = DH / 16;
+    constexpr int QP = sizeof(T) == 4 ? 3 : 1, WP = sizeof(T) == 4 ? 3 : 2;    // bf16 numbers that a query's element, a weight is the sum of
+    constexpr uint32_t HALFB = WK * DH, STAGEB = 2 * HALFB, IDB = 256, WAVEB = kvq_wave_bytes(DH);
+    constexpr int PERTILE = 2 * NL + 2;                          // loads of a tile: keys, scales, table entries for NST tiles later, values
+    constexpr int BEHIND_K = (NST - 1) * PERTILE + NL, BEHIND_V = (NST - 1) * PERTILE + NL + 2;
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    __shared__ float ml_s[WAVES * 16 * 2], fin[16 * 2];
+    const DecodeArgs &a = k.d;
+    const int tid = threadIdx.x, lane = tid & 63, n16 = lane & 15, quad = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int dh = PAD ? a.c.dh : DH;
+    // [stages: K rows, V rows][table entries][scales][row numbers] of this wavefront.  Rows lie in LDS in the order in which the loads
+    // bring them: load j has the keys g (32 / RPI) + j of its lane groups g, so that a lane's keys are neighbours.
+    char *mine = smem + wave * WAVEB;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem + (uint32_t)wave * WAVEB;
+    const uint32_t ids0 = lds0 + NST * STAGEB, scales0 = ids0 + NST * IDB, rows0 = scales0 + NST * IDB;
+    const int grp = lane / PIECES;
+    // key of a tile that lies in row p = lane % 32 in LDS
+    const int key_p = (lane & 31) % RPI * NL + (lane & 31) / RPI;
+    const float *const my_scales = lane < 32 ? k.k_scale : k.v_scale;
+    // A piece of row p lies at position piece ^ f(p): reads of K touch 16 rows of one column, the transposing reads of V eight rows of
+    // one column in each of two groups, 16 of 256 bytes in every case.
+    auto swz = [](int p) {
+        return DH == 64 ? ((p >> 2) & 3) ^ ((p >> 4) * 2) : DH == 128 ? ((p >> 1) & 7) ^ ((p >> 4) * 4) : (p & 15) ^ ((p >> 4) * 8);
+    };
+
+    for_each_pair(a, [&](int b, int len, int hb, uint32_t t0, uint32_t nt, bool whole, int64_t slot) {
+        const int h = hb / a.rtiles, r0 = (hb - h * a.rtiles) * 16, rows = min(16, a.G - r0);
+        const int cnt = (int)nt, key0 = (int)t0 * TK + wave * WK;
+        const int32_t *table = a.c.table + (int64_t)b * a.c.max_pages;
+        const T *q0 = (const T *)a.q + ((int64_t)b * a.H + h * a.G + r0 + min(n16, rows - 1)) * dh;
+        const uint64_t zeros = (uint64_t)(uintptr_t)zero_row;
+        // table entries of the keys of tile i, in the order of rows (lanes 32 .. 63 as lanes 0 .. 31)
+        auto fetch_ids = [&](int i) {
+            const int s = min(key0 + i * TK + key_p, len - 1);
+            lds_gather4(ids0 + (uint32_t)(i % NST) * IDB, (uint64_t)(uintptr_t)(table + a.c.page((uint32_t)s)));
+        };
+        uint32_t row[NL];                                   // rows of the pool that this lane reads of the tile that is being fetched
+        uint64_t scale_at = 0;                              // and the scale that it brings
+        // from the table entries of tile i, which are there; returns which of its rows count
+        auto find_rows = [&](int i) -> uint32_t {
+            const int s = key0 + i * TK + key_p;
+            const int id = *(const __attribute__((address_space(3))) int32_t *)(uintptr_t)(ids0 + (uint32_t)(i % NST) * IDB + lane * 4);
+            int r = -1;
+            scale_at = zeros;
+            if (s < len) {
+                const int pg = (int)a.c.page((uint32_t)s);
+                r = a.c.row_in(id, pg, h, s);
+                if (r < 0) a.c.flag(MOA_DEV_BAD_PAGE);
+                else scale_at = (uint64_t)(uintptr_t)(my_scales + (id * a.c.Hkv + h) * k.blocks + (s - pg * (int)a.c.page.d) / MOA_KVQ_BLOCK);
+            }
+            if (lane < 32) *(__attribute__((address_space(3))) int32_t *)(uintptr_t)(rows0 + key_p * 4) = r;
+            const uint32_t ok = (uint32_t)__ballot(r >= 0);
+#pragma unroll
+            for (int j = 0; j < NL; ++j) row[j] = *(const __attribute__((address_space(3))) uint32_t *)(uintptr_t)(rows0 + (grp * NL + j) * 4);
+            return ok;
+        };
+        auto fetch = [&](const char *pool, uint32_t at) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                  // nobody reads the place any more that is filled now
+#pragma unroll
+            for (int j = 0; j < NL; ++j) {
+                const int piece = (lane % PIECES) ^ swz(RPI * j + grp);
+                const bool in = (int)row[j] >= 0 && (!PAD || 16 * piece < dh);
+                const uint64_t from = in ? (uint64_t)(uintptr_t)pool + (uint64_t)row[j] * (uint32_t)dh + 16 * piece : zeros + 16 * piece;
+                lds_gather16<!PAD>(at + j * 1024, from);
+            }
+        };
+        if (cnt > 0) {
+#pragma unroll
+            for (int i = 0; i < NST; ++i) fetch_ids(i);
+        }
+        // the codes that a lane reads of a key, 16 behind each other, are the operands of two instructions
+        Frag qf[NKS][QP];
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) {
+            const int d = 64 * (ks / 2) + 16 * quad + 8 * (ks & 1);
+            if constexpr (QP == 1) {
+                u32x4 x = {0u, 0u, 0u, 0u};
+                if (!PAD || d < dh) x = *(const u32x4 *)(q0 + d);
+                qf[ks][0].v = __builtin_bit_cast(bf16x8, x);
+            } else {
+                f32x4 x[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+                if (!PAD || d < dh) {
+                    x[0] = *(const f32x4 *)(q0 + d);
+                    x[1] = *(const f32x4 *)(q0 + d + 4);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t part[QP];
+                    split_pair<QP>(x[e / 2][e % 2 * 2], x[e / 2][e % 2 * 2 + 1], part);
+#pragma unroll
+                    for (int i = 0; i < QP; ++i) qf[ks][i].w[e] = part[i];
+                }
+            }
+        }
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+            for (int i = 0; i < QP; ++i) asm volatile("" : "+v"(qf[ks][i].v));       // waited for here, not among the loads below
+        f32x4 acc[NDB];
+        float mref = -INFINITY, lsum = 0.f;                 // reference of the exponent (log2 domain); this lane's part of the sum
+#pragma unroll
+        for (int d = 0; d < NDB; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+        uint32_t ok[NST], any = 0;                          // rows of the tiles that count; whether any did
+        if (cnt > 0) {
+            wait_loads<0>();
+#pragma unroll
+            for (int i = 0; i < NST; ++i) {
+                ok[i] = 0;
+                if (i < cnt) {
+                    ok[i] = find_rows(i);
+                    fetch(a.c.k, lds0 + i * STAGEB);
+                    lds_gather4(scales0 + i * IDB, scale_at);
+                    fetch_ids(i + NST);
+                    fetch(a.c.v, lds0 + i * STAGEB + HALFB);
+                }
+            }
+        }
+        for (int i0 = 0; i0 < cnt; i0 += NST)
+#pragma unroll
+            for (int st = 0; st < NST; ++st) {
+                const int i = i0 + st;
+                if (i >= cnt) break;
+                const uint32_t kb = lds0 + st * STAGEB, vb = kb + HALFB, sb = scales0 + st * IDB, count = ok[st];
+                const bool next = i + NST < cnt;
+                any |= count;
+                if (i + NST <= cnt) wait_loads<BEHIND_K>();
+                else wait_loads<0>();
+                f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                for (int kp = 0; kp < NKS / 2; ++kp)
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {
+                        const int p = 16 * hf + n16;
+                        const u32x4 c = *(const __attribute__((address_space(3))) u32x4 *)(uintptr_t)(kb + p * DH + 16 * ((4 * kp + quad) ^ swz(p)));
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            const bf16x8 kf = widen(c[2 * half], c[2 * half + 1]);
+#pragma unroll
+                            for (int x = QP - 1; x >= 0; --x) s[hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[2 * kp + half][x].v, s[hf], 0, 0, 0);
+                        }
+                    }
+                // score element e: row 16 (e >> 2) + 4 quad + (e & 3) in LDS
+                f32x4 ks[2], vs[2];
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                    ks[hf] = *(const __attribute__((address_space(3))) f32x4 *)(uintptr_t)(sb + (16 * hf + 4 * quad) * 4);
+                    vs[hf] = *(const __attribute__((address_space(3))) f32x4 *)(uintptr_t)(sb + 128 + (16 * hf + 4 * quad) * 4);
+                }
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * (ks[e >> 2][e & 3] * a.scale);
+                if (count != 0xffffffffu) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (!(count >> (16 * (e >> 2) + 4 * quad + (e & 3)) & 1u)) x[e] = -INFINITY;
+                }
+                if (next) {
+                    ok[st] = find_rows(i + NST);
+                    fetch(a.c.k, kb);
+                    lds_gather4(sb, scale_at);
+                    fetch_ids(i + 2 * NST);
+                }
+                // A weight (times its value's scale) as the sum of two or three bf16 numbers: one alone (2^-8) would double the rounding of a
+                // bf16 result.
+                Frag w[WP];
+                float tm = -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) tm = fmaxf(tm, x[e]);
+                if (__ballot(tm > mref)) {
+                    tm = over_lanes<4>(tm, fmaxf);
+                    const float mnew = fmaxf(mref, tm), corr = mnew == -INFINITY ? 1.f : fast_exp2(mref - mnew);
+                    mref = mnew;
+                    lsum *= corr;
+#pragma unroll
+                    for (int d = 0; d < NDB; ++d)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[d][e] *= corr;
+                }
+                const float ms = mref == -INFINITY ? 0.f : mref;
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float p0 = fast_exp2(x[e] - ms), p1 = fast_exp2(x[e + 1] - ms);
+                    lsum += p0 + p1;
+                    uint32_t part[WP];
+                    split_pair<WP>(p0 * vs[e >> 2][e & 3], p1 * vs[e >> 2][(e & 3) + 1], part);
+#pragma unroll
+                    for (int i = 0; i < WP; ++i) w[i].w[e / 2] = part[i];
+                }
+                if (next) wait_loads<BEHIND_V>();
+                else wait_loads<0>();
+#pragma unroll
+                for (int d = 0; d < NDB; ++d) {
+                    // transposing read: lane j of a group of 16 addresses row j >> 1 of the group's eight and dims 8 (j & 1) .. of the 16
+                    const int r = n16 >> 1, p = r < 4 ? 4 * quad + r : 12 + 4 * quad + r;
+                    const i32x2 c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2 *)(uintptr_t)(vb + p * DH + 16 * (d ^ swz(p)) + 8 * (n16 & 1)));
+                    const bf16x8 vf = widen((uint32_t)c[0], (uint32_t)c[1]);
+#pragma unroll
+                    for (int i = WP - 1; i >= 0; --i) acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, w[i].v, acc[d], 0, 0, 0);
+                }
+                if (next) fetch(a.c.v, vb);
+            }
+        wait_loads<0>();
+        float *acc_s = (float *)mine;                              // the stages are free again
+        const float l = over_lanes<4>(lsum, add);
+        if (n16 < rows) {
+#pragma unroll
+            for (int d = 0; d < NDB; ++d)
+                if (!PAD || 16 * d < dh) *(f32x4 *)(acc_s + n16 * dh + 16 * d + 4 * quad) = acc[d];
+            if (quad == 0) {
+                ml_s[(wave * a.HG + n16) * 2] = max_of_keys(mref, any != 0);
+                ml_s[(wave * a.HG + n16) * 2 + 1] = l;
+            }
+        }
+        finish<T, PAD ? 0 : DH>(a, b, len, hb, whole, slot, (const float *)smem, WAVEB / 4, ml_s, fin);
+    });
+}
+
 // ---------------------------------------------------------------- host
+template <typename T, int DH, bool PAD>
+hipError_t launch_mfma(const KvqDecodeArgs &k, int grid, hipStream_t st)
+{
+    constexpr size_t lds = (size_t)WAVES * kvq_wave_bytes(DH);
+    static bool raised[16] = {};
+    const hipError_t e = raise_lds_limit_once(raised, (const void *)k_kvq_decode_mfma<T, DH, PAD>, lds);
+    if (e != hipSuccess) return e;
+    prof_begin(K_KVQ_DECODE_MFMA, st);
+    MOA_KLAUNCH((k_kvq_decode_mfma<T, DH, PAD>), dim3(grid), dim3(64 * WAVES), lds, st, k);
+    prof_end(st);
+    return hipGetLastError();
+}
+
+template <typename T, int DH>
+hipError_t launch_mfma(const KvqDecodeArgs &k, int grid, hipStream_t st)
+{
+    return k.d.c.dh == DH ? launch_mfma<T, DH, false>(k, grid, st) : launch_mfma<T, DH, true>(k, grid, st);
+}
+
 template <typename T, int LPR>
 hipError_t launch_elements(const KvqDecodeArgs &k, int grid, hipStream_t st)
 {
@@ -150,16 +429,30 @@ hipError_t launch_elements(const KvqDecodeArgs &k, int grid, hipStream_t st)
 }
 
 template <typename T>
-hipError_t launch_decode(const KvqDecodeArgs &k, hipStream_t st)
+hipError_t launch_decode(const KvqDecodeArgs &k, bool mfma, hipStream_t st)
 {
     const DecodeArgs &a = k.d;
     const int grid = a.runs ? a.runs : a.c.B * a.HB;
-    const hipError_t e = a.c.dh <= 64 ? launch_elements<T, 16>(k, grid, st) : a.c.dh <= 128 ? launch_elements<T, 32>(k, grid, st) : launch_elements<T, 64>(k, grid, st);
+    hipError_t e;
+    if (mfma) e = a.c.dh <= 64 ? launch_mfma<T, 64>(k, grid, st) : a.c.dh <= 128 ? launch_mfma<T, 128>(k, grid, st) : launch_mfma<T, 256>(k, grid, st);
+    else e = a.c.dh <= 64 ? launch_elements<T, 16>(k, grid, st) : a.c.dh <= 128 ? launch_elements<T, 32>(k, grid, st) : launch_elements<T, 64>(k, grid, st);
     if (e != hipSuccess || !a.runs) return e;
     return launch_decode_join(a, sizeof(T) == 2, st);
 }
 
-KvqPlan plan_of(const moa_kvq_cache_t &c, int H) { return kvq_plan(c.B, c.n_kv_heads, c.head_dim, c.max_pages * c.page_size, H); }
+// whether the matrix cores' form takes such a cache (and queries q, which it also reads 16 bytes at a time)
+bool takes_mfma(const moa_kvq_cache_t &c, const void *q)
+{
+    return c.head_dim % 16 == 0 && !(((uintptr_t)c.k | (uintptr_t)c.v | (uintptr_t)q) & 15);
+}
+KvqPlan plan_of(const moa_kvq_cache_t &c, int H, bool mfma) { return kvq_plan(c.B, c.n_kv_heads, c.head_dim, c.max_pages * c.page_size, H, mfma); }
+
+// enough for either form
+size_t workspace_bytes(const moa_kvq_cache_t &c, int H)
+{
+    const size_t one = plan_of(c, H, false).total(), two = plan_of(c, H, takes_mfma(c, nullptr)).total();
+    return one > two ? one : two;
+}
 
 int32_t check_decode(const moa_kvq_cache_t *c, int32_t H, const char *who)
 {
@@ -186,7 +479,7 @@ int32_t moa_kvq_decode_attn_workspace_bytes(const moa_kvq_cache_t *cache, int32_
     if (!bytes_host) return api_fail(MOA_ERR_NULL, "kvq_decode_attn_workspace_bytes: bytes_host is NULL");
     const int32_t rc = check_decode(cache, n_q_heads, "kvq_decode_attn_workspace_bytes");
     if (rc) return rc;
-    *bytes_host = plan_of(*cache, n_q_heads).total();
+    *bytes_host = workspace_bytes(*cache, n_q_heads);
     return MOA_OK;
 }
 
@@ -197,8 +490,8 @@ int32_t moa_kvq_decode_attn(const moa_kvq_cache_t *cache, int32_t n_q_heads, con
     if (rc) return rc;
     if (!q || !out) return api_fail(MOA_ERR_NULL, "kvq_decode_attn: q / out is NULL");
     if (((uintptr_t)q | (uintptr_t)out) & (cache->dtype == MOA_BF16 ? 1 : 3)) return api_fail(MOA_ERR_SHAPE, "kvq_decode_attn: q / out not aligned to their elements");
-    const KvqPlan p = plan_of(*cache, n_q_heads);
-    const size_t need = p.total();
+    const KvqPlan p = plan_of(*cache, n_q_heads, takes_mfma(*cache, q));
+    const size_t need = workspace_bytes(*cache, n_q_heads);
     if (need && (!ws || (((uintptr_t)ws) & 255) || ws_bytes < need))
         return api_fail(MOA_ERR_WORKSPACE, "kvq_decode_attn: workspace NULL, misaligned or smaller than moa_kvq_decode_attn_workspace_bytes");
     const KvqDecodeArgs k = {{KvDev(kvq_geometry(*cache), dev_status), q, out, n_q_heads, n_q_heads / cache->n_kv_heads, p.HG, p.rtiles, cache->n_kv_heads * p.rtiles,
@@ -207,7 +500,7 @@ int32_t moa_kvq_decode_attn(const moa_kvq_cache_t *cache, int32_t n_q_heads, con
                              cache->k_scale, cache->v_scale, kvq_blocks(cache->page_size)};
     prof_set_site(S_KVQ);
     hipStream_t st = (hipStream_t)stream;
-    const hipError_t e = cache->dtype == MOA_BF16 ? launch_decode<bf16_t>(k, st) : launch_decode<float>(k, st);
+    const hipError_t e = cache->dtype == MOA_BF16 ? launch_decode<bf16_t>(k, p.mfma, st) : launch_decode<float>(k, p.mfma, st);
     return e == hipSuccess ? MOA_OK : api_fail(MOA_ERR_HIP, hipGetErrorString(e));
 }
 

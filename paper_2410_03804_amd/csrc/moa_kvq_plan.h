@@ -6,20 +6,24 @@
 namespace moa {
 
 struct KvqPlan {
+    bool mfma;                         // on the matrix cores, else element by element
     int HG, rtiles, runs;              // query heads in a tile; tiles per KV head; workgroups, 0: one per pair
     size_t part_o, part_ml;            // bytes
     size_t total() const { return part_o + part_ml; }
 };
 
-inline KvqPlan kvq_plan(int B, int Hkv, int dh, int cap, int H)
+// mfma: rows of codes and queries can be read 16 bytes at a time.
+inline KvqPlan kvq_plan(int B, int Hkv, int dh, int cap, int H, bool mfma)
 {
     auto align256 = [](size_t n) { return (n + 255) & ~(size_t)255; };
     KvqPlan p;
-    const int G = H / Hkv;
-    p.HG = G < 4 ? G : 4;
+    const int G = H / Hkv, most = mfma ? 16 : 4;
+    p.mfma = mfma;
+    p.HG = G < most ? G : most;
     p.rtiles = (G + p.HG - 1) / p.HG;
     const int64_t pairs = (int64_t)B * Hkv * p.rtiles;
-    p.runs = cap <= 512 ? 0 : 1024;
+    const int64_t walk = pairs >= 512 ? 1024 : 512;
+    p.runs = cap <= walk ? 0 : mfma ? 512 : 1024;
     p.part_o = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * dh * 4) : 0;
     p.part_ml = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * 2 * 4) : 0;
     return p;
