@@ -137,7 +137,7 @@ __global__ __launch_bounds__(256, 2) void k_kvq_decode(KvqDecodeArgs k)
 
 // ---------------------------------------------------------------- on the matrix cores: head_dim a multiple of 16
 // tiles that a wavefront holds in LDS, and the bytes of that
-constexpr int kvq_stages(int DH) { return 256 / DH; }
+constexpr int kvq_stages(int DH) { return DH == 64 ? 4 : 2; }
 constexpr uint32_t kvq_wave_bytes(int DH) { return kvq_stages(DH) * (2 * WK * DH + 512) + 128; }
 
 // x as the sum of N bf16 numbers, each the rounding of what the ones before leave: to 2^-8, 2^-16, 2^-24 of x
@@ -167,13 +167,55 @@ __device__ __forceinline__ bf16x8 widen(uint32_t c0, uint32_t c1)
 
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 
-// Sixteen query heads of a KV head are the columns of a tile: S^T = K Q^T, O^T += V^T P^T, codes widened to bf16 on their way into the matrix
-// cores.  Every wavefront walks its own 32 keys of each tile of the run, with LDS of its own for NST tiles, so that there is no barrier
-// before the run's end.  Codes go straight into LDS: a tile's keys take the place of those NST tiles before as soon as these have been used,
-// their scales and its values likewise, and its table entries come another NST tiles before that.
+// Where a wavefront's tile lies, and what is to be done behind it.
+struct Place {
+    int b, hb, len, key0;
+    uint32_t ends;                       // 0: the next tile is of the same pair; 1: a part of a pair ends here; 2: a whole one does
+};
+
+// The tiles of a wavefront's run, pair after pair.  Lengths of 64 sequences lie in a register, so that going on to the next sequence waits
+// for nothing.
+struct Walk {
+    const DecodeArgs &a;
+    int b, hb, len, lens_b, lens;
+    uint32_t t, nt, left;                // the next tile of the pair, its tiles, tiles of the run
+    bool from_start;                     // the run has had the pair's first tile
+    __device__ __forceinline__ int length(int of)
+    {
+        if (of - lens_b >= 64) {
+            lens_b = of;
+            const int i = of + ((int)threadIdx.x & 63);
+            lens = i < a.c.B ? a.c.length(i, false) : 0;
+        }
+        return (int)from_lane((uint32_t)lens, of - lens_b);
+    }
+    __device__ __forceinline__ void next(Place &p)
+    {
+        p = Place{b, hb, len, (int)t * WK, 0};
+        if (left == 0) return;           // (no such tile: its table entries are read as if it were the pair's next one, and not used)
+        --left;
+        ++t;
+        p.ends = t == nt ? 1 + from_start : left == 0;
+        if (t < nt || left == 0) return;
+        t = 0;
+        from_start = true;
+        if (++hb < a.HB) return;
+        hb = 0;
+        do len = length(++b);
+        while (len == 0);                // (left > 0: there is one)
+        nt = tiles_of<WK>(len);
+    }
+};
+
+// Sixteen query heads of a KV head are the columns of a tile of 32 keys: S^T = K Q^T, O^T += V^T P^T, codes widened to bf16 on their way into the
+// matrix cores.  A wavefront has LDS of its own for NST tiles, and no barrier.  Codes go straight into LDS: a tile's keys take the place of
+// those NST tiles before as soon as these have been used, their scales and its values likewise, and its table entries come another NST tiles
+// before that.
+// ONE: a workgroup of four wavefronts per pair, a quarter of its tiles each, joined in LDS.  Else a wavefront per run, which is a workgroup: what
+// is fetched goes on from one pair to the next.
 // DH: head_dim as it lies in LDS; the rows in the pool may be shorter (PAD, a multiple of 16): their last pieces are then zeros.
-template <typename T, int DH, bool PAD>
-__global__ __launch_bounds__(256, 2) void k_kvq_decode_mfma(KvqDecodeArgs k)
+template <typename T, int DH, bool PAD, bool ONE>
+__global__ __launch_bounds__(ONE ? 256 : 64, DH == 256 ? 1 : 2) void k_kvq_decode_mfma(KvqDecodeArgs k)
 {
     constexpr int PIECES = DH / 16, RPI = 64 / PIECES, NL = WK / RPI;      // 16-byte pieces of a row; rows of a load, loads of K (or V)
     constexpr int NST = kvq_stages(DH), NKS = DH / 32, NDB = DH / 16;
@@ -181,11 +223,12 @@ __global__ __launch_bounds__(256, 2) void k_kvq_decode_mfma(KvqDecodeArgs k)
     constexpr uint32_t HALFB = WK * DH, STAGEB = 2 * HALFB, IDB = 256, WAVEB = kvq_wave_bytes(DH);
     constexpr int PERTILE = 2 * NL + 2;                          // loads of a tile: keys, scales, table entries for NST tiles later, values
     constexpr int BEHIND_K = (NST - 1) * PERTILE + NL, BEHIND_V = (NST - 1) * PERTILE + NL + 2;
+    constexpr int NW = ONE ? WAVES : 1;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    __shared__ float ml_s[WAVES * 16 * 2], fin[16 * 2];
+    __shared__ float ml_s[ONE ? WAVES * 16 * 2 : 1], fin[ONE ? 16 * 2 : 1];
     const DecodeArgs &a = k.d;
-    const int tid = threadIdx.x, lane = tid & 63, n16 = lane & 15, quad = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lane = threadIdx.x & 63, n16 = lane & 15, quad = lane >> 4;
+    const int wave = ONE ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0;
     const int dh = PAD ? a.c.dh : DH;
     // [stages: K rows, V rows][table entries][scales][row numbers] of this wavefront.  Rows lie in LDS in the order in which the loads
     // bring them: load j has the keys g (32 / RPI) + j of its lane groups g, so that a lane's keys are neighbours.
@@ -196,59 +239,94 @@ __global__ __launch_bounds__(256, 2) void k_kvq_decode_mfma(KvqDecodeArgs k)
     // key of a tile that lies in row p = lane % 32 in LDS
     const int key_p = (lane & 31) % RPI * NL + (lane & 31) / RPI;
     const float *const my_scales = lane < 32 ? k.k_scale : k.v_scale;
+    const uint64_t zeros = (uint64_t)(uintptr_t)zero_row;
     // A piece of row p lies at position piece ^ f(p): reads of K touch 16 rows of one column, the transposing reads of V eight rows of
     // one column in each of two groups, 16 of 256 bytes in every case.
     auto swz = [](int p) {
         return DH == 64 ? ((p >> 2) & 3) ^ ((p >> 4) * 2) : DH == 128 ? ((p >> 1) & 7) ^ ((p >> 4) * 4) : (p & 15) ^ ((p >> 4) * 8);
     };
 
-    for_each_pair(a, [&](int b, int len, int hb, uint32_t t0, uint32_t nt, bool whole, int64_t slot) {
-        const int h = hb / a.rtiles, r0 = (hb - h * a.rtiles) * 16, rows = min(16, a.G - r0);
-        const int cnt = (int)nt, key0 = (int)t0 * TK + wave * WK;
-        const int32_t *table = a.c.table + (int64_t)b * a.c.max_pages;
-        const T *q0 = (const T *)a.q + ((int64_t)b * a.H + h * a.G + r0 + min(n16, rows - 1)) * dh;
-        const uint64_t zeros = (uint64_t)(uintptr_t)zero_row;
-        // table entries of the keys of tile i, in the order of rows (lanes 32 .. 63 as lanes 0 .. 31)
-        auto fetch_ids = [&](int i) {
-            const int s = min(key0 + i * TK + key_p, len - 1);
-            lds_gather4(ids0 + (uint32_t)(i % NST) * IDB, (uint64_t)(uintptr_t)(table + a.c.page((uint32_t)s)));
-        };
-        uint32_t row[NL];                                   // rows of the pool that this lane reads of the tile that is being fetched
-        uint64_t scale_at = 0;                              // and the scale that it brings
-        // from the table entries of tile i, which are there; returns which of its rows count
-        auto find_rows = [&](int i) -> uint32_t {
-            const int s = key0 + i * TK + key_p;
-            const int id = *(const __attribute__((address_space(3))) int32_t *)(uintptr_t)(ids0 + (uint32_t)(i % NST) * IDB + lane * 4);
-            int r = -1;
-            scale_at = zeros;
-            if (s < len) {
-                const int pg = (int)a.c.page((uint32_t)s);
-                r = a.c.row_in(id, pg, h, s);
-                if (r < 0) a.c.flag(MOA_DEV_BAD_PAGE);
-                else scale_at = (uint64_t)(uintptr_t)(my_scales + (id * a.c.Hkv + h) * k.blocks + (s - pg * (int)a.c.page.d) / MOA_KVQ_BLOCK);
-            }
-            if (lane < 32) *(__attribute__((address_space(3))) int32_t *)(uintptr_t)(rows0 + key_p * 4) = r;
-            const uint32_t ok = (uint32_t)__ballot(r >= 0);
-#pragma unroll
-            for (int j = 0; j < NL; ++j) row[j] = *(const __attribute__((address_space(3))) uint32_t *)(uintptr_t)(rows0 + (grp * NL + j) * 4);
-            return ok;
-        };
-        auto fetch = [&](const char *pool, uint32_t at) {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                  // nobody reads the place any more that is filled now
-#pragma unroll
-            for (int j = 0; j < NL; ++j) {
-                const int piece = (lane % PIECES) ^ swz(RPI * j + grp);
-                const bool in = (int)row[j] >= 0 && (!PAD || 16 * piece < dh);
-                const uint64_t from = in ? (uint64_t)(uintptr_t)pool + (uint64_t)row[j] * (uint32_t)dh + 16 * piece : zeros + 16 * piece;
-                lds_gather16<!PAD>(at + j * 1024, from);
-            }
-        };
-        if (cnt > 0) {
-#pragma unroll
-            for (int i = 0; i < NST; ++i) fetch_ids(i);
+    // ---- the run
+    Walk walk{a, 0, 0, 0, 0, 0, 0, 0, 0, true};
+    int cnt = 0;                                            // tiles of this wavefront
+    uint32_t nt_one = 0;
+    if (ONE) {
+        walk.b = (int)blockIdx.x / a.HB;
+        walk.hb = (int)blockIdx.x - walk.b * a.HB;
+        walk.len = (int)uniform((uint32_t)a.c.length(walk.b, walk.hb == 0 && threadIdx.x == 0));
+        nt_one = tiles_of<WK>(walk.len);
+        cnt = ((int)nt_one - wave + NW - 1) / NW;           // tiles wave, wave + NW ..
+    } else {
+        TileList<WK> list;
+        uint32_t begin = 0;
+        if (!list.find(a, blockIdx.x, walk.b, walk.len, begin)) return;
+        const uint32_t f = blockIdx.x * list.per, in = f - begin;
+        walk.nt = tiles_of<WK>(walk.len);
+        walk.hb = (int)(in / walk.nt);
+        walk.t = in - (uint32_t)walk.hb * walk.nt;
+        walk.left = min(list.per, list.total - f);
+        walk.from_start = walk.t == 0;
+        walk.lens_b = walk.b - 64;                          // (nothing there yet)
+        (void)walk.length(walk.b);
+        cnt = (int)walk.left;
+    }
+    int tile_one = wave;
+    auto next_place = [&](Place &p) {
+        if (!ONE) return walk.next(p);
+        p = Place{walk.b, walk.hb, walk.len, min(tile_one, (int)nt_one - 1) * WK, 0};
+        tile_one += NW;
+    };
+
+    Place ahead[NST] = {}, cur[NST] = {};                   // of the tiles whose table entries are, whose rows are on their way
+    auto fetch_ids = [&](int st) {
+        next_place(ahead[st]);
+        const Place &p = ahead[st];
+        const int s = min(p.key0 + key_p, p.len - 1);       // in the order of rows, lanes 32 .. 63 as lanes 0 .. 31
+        lds_gather4(ids0 + (uint32_t)st * IDB, (uint64_t)(uintptr_t)(a.c.table + (int64_t)p.b * a.c.max_pages + a.c.page((uint32_t)s)));
+    };
+    uint32_t row[NL];                                       // rows of the pool that this lane reads of the tile that is being fetched
+    uint64_t scale_at = 0;                                  // and the scale that it brings
+    // from the table entries in stage st, which are there; returns which of its rows count
+    auto find_rows = [&](int st) -> uint32_t {
+        cur[st] = ahead[st];
+        const Place &p = cur[st];
+        const int h = a.rtiles == 1 ? p.hb : p.hb / a.rtiles;
+        const int s = p.key0 + key_p;
+        const int id = *(const __attribute__((address_space(3))) int32_t *)(uintptr_t)(ids0 + (uint32_t)st * IDB + lane * 4);
+        int r = -1;
+        scale_at = zeros;
+        if (s < p.len) {
+            const int pg = (int)a.c.page((uint32_t)s);
+            r = a.c.row_in(id, pg, h, s);
+            if (r < 0) a.c.flag(MOA_DEV_BAD_PAGE);
+            else scale_at = (uint64_t)(uintptr_t)(my_scales + (id * a.c.Hkv + h) * k.blocks + (s - pg * (int)a.c.page.d) / MOA_KVQ_BLOCK);
         }
-        // the codes that a lane reads of a key, 16 behind each other, are the operands of two instructions
-        Frag qf[NKS][QP];
+        if (lane < 32) *(__attribute__((address_space(3))) int32_t *)(uintptr_t)(rows0 + key_p * 4) = r;
+        const uint32_t ok = (uint32_t)__ballot(r >= 0);
+#pragma unroll
+        for (int j = 0; j < NL; ++j) row[j] = *(const __attribute__((address_space(3))) uint32_t *)(uintptr_t)(rows0 + (grp * NL + j) * 4);
+        return ok;
+    };
+    auto fetch = [&](const char *pool, uint32_t at) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                      // nobody reads the place any more that is filled now
+#pragma unroll
+        for (int j = 0; j < NL; ++j) {
+            const int piece = (lane % PIECES) ^ swz(RPI * j + grp);
+            const bool in = (int)row[j] >= 0 && (!PAD || 16 * piece < dh);
+            const uint64_t from = in ? (uint64_t)(uintptr_t)pool + (uint64_t)row[j] * (uint32_t)dh + 16 * piece : zeros + 16 * piece;
+            lds_gather16<!PAD>(at + j * 1024, from);
+        }
+    };
+    if (cnt > 0) {
+#pragma unroll
+        for (int st = 0; st < NST; ++st) fetch_ids(st);
+    }
+
+    // ---- queries: the codes that a lane reads of a key, 16 behind each other, are the operands of two instructions
+    Frag qf[NKS][QP];
+    auto load_queries = [&](int b, int hb) {
+        const int h = a.rtiles == 1 ? hb : hb / a.rtiles, r0 = (hb - h * a.rtiles) * 16, rows = min(16, a.G - r0);
+        const T *q0 = (const T *)a.q + ((int64_t)b * a.H + h * a.G + r0 + min(n16, rows - 1)) * dh;
 #pragma unroll
         for (int ks = 0; ks < NKS; ++ks) {
             const int d = 64 * (ks / 2) + 16 * quad + 8 * (ks & 1);
@@ -274,145 +352,183 @@ __global__ __launch_bounds__(256, 2) void k_kvq_decode_mfma(KvqDecodeArgs k)
 #pragma unroll
         for (int ks = 0; ks < NKS; ++ks)
 #pragma unroll
-            for (int i = 0; i < QP; ++i) asm volatile("" : "+v"(qf[ks][i].v));       // waited for here, not among the loads below
-        f32x4 acc[NDB];
-        float mref = -INFINITY, lsum = 0.f;                 // reference of the exponent (log2 domain); this lane's part of the sum
-#pragma unroll
-        for (int d = 0; d < NDB; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < QP; ++i) asm volatile("" : "+v"(qf[ks][i].v));       // waited for here, not among the loads behind
+    };
+    load_queries(ONE ? walk.b : ahead[0].b, ONE ? walk.hb : ahead[0].hb);
 
-        uint32_t ok[NST], any = 0;                          // rows of the tiles that count; whether any did
-        if (cnt > 0) {
-            wait_loads<0>();
+    f32x4 acc[NDB];
+    float mref = -INFINITY, lsum = 0.f;                     // reference of the exponent (log2 domain); this lane's part of the sum
+    uint32_t ok[NST], any = 0;                              // rows of the tiles that count; whether any did
 #pragma unroll
-            for (int i = 0; i < NST; ++i) {
-                ok[i] = 0;
-                if (i < cnt) {
-                    ok[i] = find_rows(i);
-                    fetch(a.c.k, lds0 + i * STAGEB);
-                    lds_gather4(scales0 + i * IDB, scale_at);
-                    fetch_ids(i + NST);
-                    fetch(a.c.v, lds0 + i * STAGEB + HALFB);
-                }
+    for (int d = 0; d < NDB; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (cnt > 0) {
+        wait_loads<0>();
+#pragma unroll
+        for (int st = 0; st < NST; ++st) {
+            ok[st] = 0;
+            if (st < cnt) {
+                ok[st] = find_rows(st);
+                fetch(a.c.k, lds0 + st * STAGEB);
+                lds_gather4(scales0 + st * IDB, scale_at);
+                fetch_ids(st);
+                fetch(a.c.v, lds0 + st * STAGEB + HALFB);
             }
         }
-        for (int i0 = 0; i0 < cnt; i0 += NST)
+    }
+    for (int i0 = 0; i0 < cnt; i0 += NST)
 #pragma unroll
-            for (int st = 0; st < NST; ++st) {
-                const int i = i0 + st;
-                if (i >= cnt) break;
-                const uint32_t kb = lds0 + st * STAGEB, vb = kb + HALFB, sb = scales0 + st * IDB, count = ok[st];
-                const bool next = i + NST < cnt;
-                any |= count;
-                if (i + NST <= cnt) wait_loads<BEHIND_K>();
-                else wait_loads<0>();
-                f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        for (int st = 0; st < NST; ++st) {
+            const int i = i0 + st;
+            if (i >= cnt) break;
+            const uint32_t kb = lds0 + st * STAGEB, vb = kb + HALFB, sb = scales0 + st * IDB, count = ok[st];
+            const Place at = cur[st];
+            const bool next = i + NST < cnt;
+            any |= count;
+            if (i + NST <= cnt) wait_loads<BEHIND_K>();
+            else wait_loads<0>();
+            f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-                for (int kp = 0; kp < NKS / 2; ++kp)
-#pragma unroll
-                    for (int hf = 0; hf < 2; ++hf) {
-                        const int p = 16 * hf + n16;
-                        const u32x4 c = *(const __attribute__((address_space(3))) u32x4 *)(uintptr_t)(kb + p * DH + 16 * ((4 * kp + quad) ^ swz(p)));
-#pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            const bf16x8 kf = widen(c[2 * half], c[2 * half + 1]);
-#pragma unroll
-                            for (int x = QP - 1; x >= 0; --x) s[hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[2 * kp + half][x].v, s[hf], 0, 0, 0);
-                        }
-                    }
-                // score element e: row 16 (e >> 2) + 4 quad + (e & 3) in LDS
-                f32x4 ks[2], vs[2];
+            for (int kp = 0; kp < NKS / 2; ++kp)
 #pragma unroll
                 for (int hf = 0; hf < 2; ++hf) {
-                    ks[hf] = *(const __attribute__((address_space(3))) f32x4 *)(uintptr_t)(sb + (16 * hf + 4 * quad) * 4);
-                    vs[hf] = *(const __attribute__((address_space(3))) f32x4 *)(uintptr_t)(sb + 128 + (16 * hf + 4 * quad) * 4);
-                }
-                float x[8];
+                    const int p = 16 * hf + n16;
+                    const u32x4 c = *(const __attribute__((address_space(3))) u32x4 *)(uintptr_t)(kb + p * DH + 16 * ((4 * kp + quad) ^ swz(p)));
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * (ks[e >> 2][e & 3] * a.scale);
-                if (count != 0xffffffffu) {
+                    for (int half = 0; half < 2; ++half) {
+                        const bf16x8 kf = widen(c[2 * half], c[2 * half + 1]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (!(count >> (16 * (e >> 2) + 4 * quad + (e & 3)) & 1u)) x[e] = -INFINITY;
+                        for (int x = QP - 1; x >= 0; --x) s[hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[2 * kp + half][x].v, s[hf], 0, 0, 0);
+                    }
                 }
-                if (next) {
-                    ok[st] = find_rows(i + NST);
-                    fetch(a.c.k, kb);
-                    lds_gather4(sb, scale_at);
-                    fetch_ids(i + 2 * NST);
-                }
-                // A weight (times its value's scale) as the sum of two or three bf16 numbers: one alone (2^-8) would double the rounding of a
-                // bf16 result.
-                Frag w[WP];
-                float tm = -INFINITY;
+            // score element e: row 16 (e >> 2) + 4 quad + (e & 3) in LDS
+            f32x4 ks[2], vs[2];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) tm = fmaxf(tm, x[e]);
-                if (__ballot(tm > mref)) {
-                    tm = over_lanes<4>(tm, fmaxf);
-                    const float mnew = fmaxf(mref, tm), corr = mnew == -INFINITY ? 1.f : fast_exp2(mref - mnew);
-                    mref = mnew;
-                    lsum *= corr;
+            for (int hf = 0; hf < 2; ++hf) {
+                ks[hf] = *(const __attribute__((address_space(3))) f32x4 *)(uintptr_t)(sb + (16 * hf + 4 * quad) * 4);
+                vs[hf] = *(const __attribute__((address_space(3))) f32x4 *)(uintptr_t)(sb + 128 + (16 * hf + 4 * quad) * 4);
+            }
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * (ks[e >> 2][e & 3] * a.scale);
+            if (count != 0xffffffffu) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (!(count >> (16 * (e >> 2) + 4 * quad + (e & 3)) & 1u)) x[e] = -INFINITY;
+            }
+            if (next) {
+                ok[st] = find_rows(st);
+                fetch(a.c.k, kb);
+                lds_gather4(sb, scale_at);
+                fetch_ids(st);
+            }
+            // A weight (times its value's scale) as the sum of two or three bf16 numbers: one alone (2^-8) would double the rounding of a
+            // bf16 result.
+            Frag w[WP];
+            float tm = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) tm = fmaxf(tm, x[e]);
+            if (__ballot(tm > mref)) {
+                tm = over_lanes<4>(tm, fmaxf);
+                const float mnew = fmaxf(mref, tm), corr = mnew == -INFINITY ? 1.f : fast_exp2(mref - mnew);
+                mref = mnew;
+                lsum *= corr;
+#pragma unroll
+                for (int d = 0; d < NDB; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[d][e] *= corr;
+            }
+            const float ms = mref == -INFINITY ? 0.f : mref;
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const float p0 = fast_exp2(x[e] - ms), p1 = fast_exp2(x[e + 1] - ms);
+                lsum += p0 + p1;
+                uint32_t part[WP];
+                split_pair<WP>(p0 * vs[e >> 2][e & 3], p1 * vs[e >> 2][(e & 3) + 1], part);
+#pragma unroll
+                for (int i = 0; i < WP; ++i) w[i].w[e / 2] = part[i];
+            }
+            if (next) wait_loads<BEHIND_V>();
+            else wait_loads<0>();
+#pragma unroll
+            for (int d = 0; d < NDB; ++d) {
+                // transposing read: lane j of a group of 16 addresses row j >> 1 of the group's eight and dims 8 (j & 1) .. of the 16
+                const int r = n16 >> 1, p = r < 4 ? 4 * quad + r : 12 + 4 * quad + r;
+                const i32x2 c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2 *)(uintptr_t)(vb + p * DH + 16 * (d ^ swz(p)) + 8 * (n16 & 1)));
+                const bf16x8 vf = widen((uint32_t)c[0], (uint32_t)c[1]);
+#pragma unroll
+                for (int i = WP - 1; i >= 0; --i) acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, w[i].v, acc[d], 0, 0, 0);
+            }
+            if (next) fetch(a.c.v, vb);
+            if (ONE || !at.ends) continue;
+            // ---- the pair, or the run's part of it, ends: a lane has 4 dims of every 16 of one head
+            const int h = a.rtiles == 1 ? at.hb : at.hb / a.rtiles, r0 = (at.hb - h * a.rtiles) * 16, rows = min(16, a.G - r0);
+            const float l = over_lanes<4>(lsum, add), m = max_of_keys(mref, any != 0);
+            if (n16 < rows) {
+                if (at.ends == 2) {
+                    const float inv = inverse_sum(m, l);
+                    T *out = (T *)a.out + ((int64_t)at.b * a.H + h * a.G + r0 + n16) * dh;
 #pragma unroll
                     for (int d = 0; d < NDB; ++d)
+                        if (!PAD || 16 * d < dh) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[d][e] *= corr;
+                            for (int e = 0; e < 4; ++e) moa::st(out + 16 * d + 4 * quad + e, acc[d][e] * inv);
+                        }
+                    if (m == -INFINITY && l == 0.f) a.c.flag(MOA_DEV_EMPTY_KEYS);
+                } else {
+                    const int64_t slot = ((int64_t)blockIdx.x + (int64_t)at.b * a.HB + at.hb) * a.HG + n16;
+#pragma unroll
+                    for (int d = 0; d < NDB; ++d)
+                        if (!PAD || 16 * d < dh) *(f32x4 *)(a.part_o + slot * dh + 16 * d + 4 * quad) = acc[d];
+                    if (quad == 0) {
+                        a.part_ml[slot * 2] = m;
+                        a.part_ml[slot * 2 + 1] = l;
+                    }
                 }
-                const float ms = mref == -INFINITY ? 0.f : mref;
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const float p0 = fast_exp2(x[e] - ms), p1 = fast_exp2(x[e + 1] - ms);
-                    lsum += p0 + p1;
-                    uint32_t part[WP];
-                    split_pair<WP>(p0 * vs[e >> 2][e & 3], p1 * vs[e >> 2][(e & 3) + 1], part);
-#pragma unroll
-                    for (int i = 0; i < WP; ++i) w[i].w[e / 2] = part[i];
-                }
-                if (next) wait_loads<BEHIND_V>();
-                else wait_loads<0>();
-#pragma unroll
-                for (int d = 0; d < NDB; ++d) {
-                    // transposing read: lane j of a group of 16 addresses row j >> 1 of the group's eight and dims 8 (j & 1) .. of the 16
-                    const int r = n16 >> 1, p = r < 4 ? 4 * quad + r : 12 + 4 * quad + r;
-                    const i32x2 c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2 *)(uintptr_t)(vb + p * DH + 16 * (d ^ swz(p)) + 8 * (n16 & 1)));
-                    const bf16x8 vf = widen((uint32_t)c[0], (uint32_t)c[1]);
-#pragma unroll
-                    for (int i = WP - 1; i >= 0; --i) acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, w[i].v, acc[d], 0, 0, 0);
-                }
-                if (next) fetch(a.c.v, vb);
             }
-        wait_loads<0>();
-        float *acc_s = (float *)mine;                              // the stages are free again
-        const float l = over_lanes<4>(lsum, add);
-        if (n16 < rows) {
+            if (i + 1 >= cnt) return;
 #pragma unroll
-            for (int d = 0; d < NDB; ++d)
-                if (!PAD || 16 * d < dh) *(f32x4 *)(acc_s + n16 * dh + 16 * d + 4 * quad) = acc[d];
-            if (quad == 0) {
-                ml_s[(wave * a.HG + n16) * 2] = max_of_keys(mref, any != 0);
-                ml_s[(wave * a.HG + n16) * 2 + 1] = l;
-            }
+            for (int d = 0; d < NDB; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+            mref = -INFINITY;
+            lsum = 0.f;
+            any = 0;
+            load_queries(cur[(st + 1) % NST].b, cur[(st + 1) % NST].hb);
         }
-        finish<T, PAD ? 0 : DH>(a, b, len, hb, whole, slot, (const float *)smem, WAVEB / 4, ml_s, fin);
-    });
+    if (!ONE) return;
+    wait_loads<0>();
+    const int h = a.rtiles == 1 ? walk.hb : walk.hb / a.rtiles, rows = min(16, a.G - (walk.hb - h * a.rtiles) * 16);
+    float *acc_s = (float *)mine;                                  // the stages are free again
+    const float l = over_lanes<4>(lsum, add);
+    if (n16 < rows) {
+#pragma unroll
+        for (int d = 0; d < NDB; ++d)
+            if (!PAD || 16 * d < dh) *(f32x4 *)(acc_s + n16 * dh + 16 * d + 4 * quad) = acc[d];
+        if (quad == 0) {
+            ml_s[(wave * a.HG + n16) * 2] = max_of_keys(mref, any != 0);
+            ml_s[(wave * a.HG + n16) * 2 + 1] = l;
+        }
+    }
+    finish<T, PAD ? 0 : DH>(a, walk.b, walk.len, walk.hb, true, 0, (const float *)smem, WAVEB / 4, ml_s, fin);
 }
 
 // ---------------------------------------------------------------- host
-template <typename T, int DH, bool PAD>
-hipError_t launch_mfma(const KvqDecodeArgs &k, int grid, hipStream_t st)
+template <typename T, int DH, bool PAD, bool ONE>
+hipError_t launch_mfma(const KvqDecodeArgs &k, hipStream_t st)
 {
-    constexpr size_t lds = (size_t)WAVES * kvq_wave_bytes(DH);
+    constexpr size_t lds = (size_t)(ONE ? WAVES : 1) * kvq_wave_bytes(DH);
     static bool raised[16] = {};
-    const hipError_t e = raise_lds_limit_once(raised, (const void *)k_kvq_decode_mfma<T, DH, PAD>, lds);
+    const hipError_t e = raise_lds_limit_once(raised, (const void *)k_kvq_decode_mfma<T, DH, PAD, ONE>, lds);
     if (e != hipSuccess) return e;
     prof_begin(K_KVQ_DECODE_MFMA, st);
-    MOA_KLAUNCH((k_kvq_decode_mfma<T, DH, PAD>), dim3(grid), dim3(64 * WAVES), lds, st, k);
+    MOA_KLAUNCH((k_kvq_decode_mfma<T, DH, PAD, ONE>), dim3(ONE ? k.d.c.B * k.d.HB : k.d.runs), dim3(ONE ? 64 * WAVES : 64), lds, st, k);
     prof_end(st);
     return hipGetLastError();
 }
 
 template <typename T, int DH>
-hipError_t launch_mfma(const KvqDecodeArgs &k, int grid, hipStream_t st)
+hipError_t launch_mfma(const KvqDecodeArgs &k, hipStream_t st)
 {
-    return k.d.c.dh == DH ? launch_mfma<T, DH, false>(k, grid, st) : launch_mfma<T, DH, true>(k, grid, st);
+    if (k.d.c.dh == DH) return k.d.runs ? launch_mfma<T, DH, false, false>(k, st) : launch_mfma<T, DH, false, true>(k, st);
+    return k.d.runs ? launch_mfma<T, DH, true, false>(k, st) : launch_mfma<T, DH, true, true>(k, st);
 }
 
 template <typename T, int LPR>
@@ -434,10 +550,10 @@ hipError_t launch_decode(const KvqDecodeArgs &k, bool mfma, hipStream_t st)
     const DecodeArgs &a = k.d;
     const int grid = a.runs ? a.runs : a.c.B * a.HB;
     hipError_t e;
-    if (mfma) e = a.c.dh <= 64 ? launch_mfma<T, 64>(k, grid, st) : a.c.dh <= 128 ? launch_mfma<T, 128>(k, grid, st) : launch_mfma<T, 256>(k, grid, st);
+    if (mfma) e = a.c.dh <= 64 ? launch_mfma<T, 64>(k, st) : a.c.dh <= 128 ? launch_mfma<T, 128>(k, st) : launch_mfma<T, 256>(k, st);
     else e = a.c.dh <= 64 ? launch_elements<T, 16>(k, grid, st) : a.c.dh <= 128 ? launch_elements<T, 32>(k, grid, st) : launch_elements<T, 64>(k, grid, st);
     if (e != hipSuccess || !a.runs) return e;
-    return launch_decode_join(a, sizeof(T) == 2, st);
+    return launch_decode_join(a, sizeof(T) == 2, mfma ? WK : TK, st);
 }
 
 // whether the matrix cores' form takes such a cache (and queries q, which it also reads 16 bytes at a time)
@@ -462,8 +578,8 @@ int32_t check_decode(const moa_kvq_cache_t *c, int32_t H, const char *who)
     if ((int64_t)c->B * H > (1 << 20)) return api_fail(MOA_ERR_SHAPE, "kvq_decode_attn: more than 2^20 pairs of sequence and query head");
     const int64_t cap = (int64_t)c->max_pages * c->page_size;
     // tiles are counted in 32 bits
-    if ((int64_t)c->B * H * ((cap + TK - 1) / TK) > INT32_MAX / 2)
-        return api_fail(MOA_ERR_SHAPE, "kvq_decode_attn: B * n_q_heads * ceil(capacity / 128) above 2^30");
+    if ((int64_t)c->B * H * ((cap + WK - 1) / WK) > INT32_MAX / 2)
+        return api_fail(MOA_ERR_SHAPE, "kvq_decode_attn: B * n_q_heads * ceil(capacity / 32) above 2^30");
     return MOA_OK;
 }
 

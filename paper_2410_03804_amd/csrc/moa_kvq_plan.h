@@ -23,7 +23,7 @@ inline KvqPlan kvq_plan(int B, int Hkv, int dh, int cap, int H, bool mfma)
     p.rtiles = (G + p.HG - 1) / p.HG;
     const int64_t pairs = (int64_t)B * Hkv * p.rtiles;
     const int64_t walk = pairs >= 512 ? 1024 : 512;
-    p.runs = cap <= walk ? 0 : mfma ? 512 : 1024;
+    p.runs = cap <= walk ? 0 : !mfma ? 1024 : dh <= 128 ? 2048 : 1024;
     p.part_o = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * dh * 4) : 0;
     p.part_ml = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * 2 * 4) : 0;
     return p;
