@@ -18,7 +18,7 @@ if not _LIB_PATH.exists():
     raise ImportError(f"{_LIB_PATH} is missing: build it with `python {_LIB_PATH.with_name('build.py')}` (there is no fallback path)")
 _lib = C.CDLL(str(_LIB_PATH))
 try:
-    from ._argcheck import dev as _dev, dev_on as _dev_on, room_on as _room_on  # built with the library: csrc/argcheck.c
+    from ._argcheck import dev as _dev, dev_on as _dev_on, room_on as _room_on, rows_on as _rows_on  # built with the library: csrc/argcheck.c
 except ImportError as e:
     raise ImportError(f"{_LIB_PATH.with_name('_argcheck.abi3.so')}, the argument check built with the library, does not load ({e}): "
                       f"build both with `python {_LIB_PATH.with_name('build.py')}` (there is no fallback path)") from e
@@ -597,23 +597,6 @@ def _device_of(t, stream):
     if torch._C._cuda_getDevice() != i or (stream is not None and stream.device_index != i):
         raise ValueError("the tensors' device must be the current one, and the stream's")
     return i, torch._C._cuda_getCurrentRawStream(i) if stream is None else stream.cuda_stream
-
-
-def _rows_on(t, dtype, heads, dh, name, at):
-    """Address and row stride of a tensor [T, heads, dh] whose rows may lie apart (a part of a projection's output)."""
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name}: expected a torch tensor")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dh:
-        raise ValueError(f"{name}: must be [T, {heads}, {dh}]")
-    if t.dtype != dtype:
-        raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
-    step, of_head, of_elem = t.stride()
-    few = t.shape[0] <= 1                              # a stride that is never taken may be any number
-    if not t.is_cuda or (of_elem != 1 and dh > 1) or (of_head != dh and heads > 1) or (step < heads * dh and not few):
-        raise ValueError(f"{name}: must be a CUDA tensor whose heads lie behind each other")
-    if t.get_device() != at:
-        raise ValueError(f"{name}: must be on the same device as the others")
-    return t.data_ptr(), heads * dh if few else step
 
 
 def _page_args(table, length, page_size, free, n_free, i):

@@ -24,19 +24,24 @@ struct RopeNormArgs {
     const int32_t *pos;              // [T]
     int dh, half;                    // elements of a head, pairs that are rotated
     float eps;
-    double log_theta;
+    double power[7];                 // theta^(-2^i / half): the frequency of pair c is the product of those of c's bits
 };
 
-// cos and sin of the pairs of `tokens` tokens from t0 on, [tokens][half]
+// cos and sin of the pairs of `tokens` tokens from t0 on, [tokens][half].  The angle in turns, and in double precision until what is left of it
+// is at most an eighth of one, from there in single: as good as a cosine rounded from double precision to a unit in the last place, and a
+// fifth of the instructions (8192 tokens of 40 heads, exp and sincospi in double: 44 us, 119 in the kernel below).
 __device__ __forceinline__ void angles(const RopeNormArgs &a, int64_t t0, int tokens, float2 *cs)
 {
     for (int i = threadIdx.x; i < tokens * a.half; i += blockDim.x) {
         const int t = i / a.half, c = i - t * a.half;
-        // (in turns: what is left of them after the whole ones is exact)
-        const double turns = (double)a.pos[t0 + t] * (exp((double)c / (double)a.half * -a.log_theta) * 0.15915494309189533577);
-        double sn, cn;
-        sincospi(2.0 * (turns - rint(turns)), &sn, &cn);
-        cs[i] = make_float2((float)cn, (float)sn);
+        double f = 0.15915494309189533577;                  // 1 / (2 pi)
+#pragma unroll
+        for (int k = 0; k < 7; ++k) f *= c >> k & 1 ? a.power[k] : 1.0;
+        const double turns = (double)a.pos[t0 + t] * f, quarters = rint(4.0 * turns);
+        float sn, cn;
+        sincospif((float)(2.0 * fma(-0.25, quarters, turns)), &sn, &cn);
+        const int q = (int)(quarters - 4.0 * floor(0.25 * quarters));
+        cs[i] = q == 0 ? make_float2(cn, sn) : q == 1 ? make_float2(-sn, cn) : q == 2 ? make_float2(-cn, -sn) : make_float2(sn, -cn);
     }
 }
 
@@ -91,9 +96,139 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope(RopeNormArgs a)
     }
 }
 
+// ---------------------------------------------------------------- rows in pieces of 16 bytes
+// A head is spread over LPR lanes, two pieces each: the ones that are rotated against each other, so that no lane needs another's elements, or two
+// that pass.  A workgroup has TPB tokens, whose angles are one or two a thread.
+template <typename T, int LPR, int TPB>
+__global__ __launch_bounds__(256) void k_qk_norm_rope_pieces(RopeNormArgs a)
+{
+    constexpr int VE = 16 / sizeof(T), U = 2;
+    __shared__ __attribute__((aligned(16))) float2 cs[TPB * 128];
+    const int64_t t0 = (int64_t)blockIdx.x * TPB;
+    const int tokens = (int)(a.T - t0 < TPB ? a.T - t0 : TPB), R = a.heads[0] + a.heads[1], n = tokens * R;
+    const int c = threadIdx.x % LPR, pairs = a.dh / (2 * VE), turned = a.half / VE;
+    const bool on = c < pairs, turn = c < turned;
+    const int pa = turn ? c : turned + c, step = turn ? turned : pairs - turned;      // pieces: pa and pa + step
+    struct Row { const T *x; T *y; int t, w; };
+    auto row_of = [&](int r) {
+        const int t = r / R, hh = r - t * R, w = hh >= a.heads[0], h = w ? hh - a.heads[0] : hh;
+        return Row{(const T *)a.x[w] + (t0 + t) * a.ldx[w] + (int64_t)h * a.dh, (T *)a.y[w] + (t0 + t) * a.ldy[w] + (int64_t)h * a.dh, t, w};
+    };
+    u32x4 x[U][2];
+    auto load = [&](int r, u32x4 (&v)[2]) {
+        v[0] = v[1] = u32x4{0u, 0u, 0u, 0u};
+        if (r >= n || !on) return;
+        const T *p = row_of(r).x;
+        v[0] = *(const u32x4 *)(p + pa * VE);
+        v[1] = *(const u32x4 *)(p + (pa + step) * VE);
+    };
+    auto value = [](const u32x4 &v, int e) {
+        return sizeof(T) == 4 ? __uint_as_float(v[e]) : __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
+    };
+    constexpr int RP = 256 / LPR;                        // rows at a time
+    const int first = threadIdx.x / LPR;
+#pragma unroll
+    for (int u = 0; u < U; ++u) load(first + u * RP, x[u]);
+    u32x4 g[2][2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        g[w][0] = g[w][1] = u32x4{0u, 0u, 0u, 0u};
+        if (!a.g[w] || !on) continue;
+        g[w][0] = *(const u32x4 *)((const T *)a.g[w] + pa * VE);
+        g[w][1] = *(const u32x4 *)((const T *)a.g[w] + (pa + step) * VE);
+    }
+    if (a.half) {
+        angles(a, t0, tokens, cs);
+        __syncthreads();
+    }
+    for (int r0 = first; r0 < n; r0 += U * RP) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int r = r0 + u * RP;
+            float y[2][VE];
+            float ss = 0.f;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < VE; ++e) {
+                    y[i][e] = value(x[u][i], e);
+                    ss = fmaf(y[i][e], y[i][e], ss);
+                }
+            load(r + U * RP, x[u]);
+#pragma unroll
+            for (int o = LPR / 2; o >= 1; o >>= 1) ss += __shfl_xor(ss, o);
+            if (r >= n || !on) continue;
+            const Row at = row_of(r);
+            if (a.g[at.w]) {
+                const float inv = 1.f / sqrtf(ss / (float)a.dh + a.eps);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) y[i][e] = y[i][e] * inv * (at.w ? value(g[1][i], e) : value(g[0][i], e));
+            }
+            if (turn) {
+                const f32x4 *f = (const f32x4 *)(cs + at.t * a.half + c * VE);
+#pragma unroll
+                for (int e = 0; e < VE; e += 2) {
+                    const f32x4 f2 = f[e / 2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float lo = y[0][e + i], hi = y[1][e + i], cn = f2[2 * i], sn = f2[2 * i + 1];
+                        y[0][e + i] = fmaf(lo, cn, -hi * sn);
+                        y[1][e + i] = fmaf(hi, cn, lo * sn);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                u32x4 o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (sizeof(T) == 4) o[e] = __float_as_uint(y[i][e]);
+                    else o[e] = pack_bf16x2(y[i][2 * e], y[i][2 * e + 1]);
+                }
+                u32x4 *const to = (u32x4 *)(at.y + (pa + i * step) * VE);
+                // (of many tokens no cache holds the results until they are read: 42.6 us without, 36.9 with, where reads said so too 38.8)
+                if constexpr (TPB > 1) __builtin_nontemporal_store(o, to);
+                else *to = o;
+            }
+        }
+    }
+}
+
+template <typename T, int LPR>
+hipError_t launch_pieces(const RopeNormArgs &a, hipStream_t st)
+{
+    const bool many = a.T >= 2048;
+    prof_begin(K_QK_NORM_ROPE, st);
+    if (many) MOA_KLAUNCH((k_qk_norm_rope_pieces<T, LPR, 4>), dim3((unsigned)((a.T + 3) / 4)), dim3(256), 0, st, a);
+    else MOA_KLAUNCH((k_qk_norm_rope_pieces<T, LPR, 1>), dim3((unsigned)a.T), dim3(256), 0, st, a);
+    prof_end(st);
+    return hipGetLastError();
+}
+
+// every address in 16 bytes, and pairs of pieces that are rotated or pass
+template <typename T>
+bool in_pieces(const RopeNormArgs &a)
+{
+    constexpr int VE = 16 / sizeof(T);
+    uintptr_t bits = 0;
+    int64_t elems = 0;
+    for (int w = 0; w < 2; ++w)
+        if (a.heads[w]) {
+            bits |= (uintptr_t)a.x[w] | (uintptr_t)a.y[w] | (uintptr_t)a.g[w];
+            elems |= a.ldx[w] | a.ldy[w];
+        }
+    return a.dh % (2 * VE) == 0 && a.half % VE == 0 && !(bits & 15) && elems % VE == 0;
+}
+
 template <typename T>
 hipError_t launch(const RopeNormArgs &a, hipStream_t st)
 {
+    if (in_pieces<T>(a)) {
+        const int pairs = a.dh * (int)sizeof(T) / 32;
+        return pairs <= 4 ? launch_pieces<T, 4>(a, st) : pairs <= 8 ? launch_pieces<T, 8>(a, st) : pairs <= 16 ? launch_pieces<T, 16>(a, st) : launch_pieces<T, 32>(a, st);
+    }
     prof_begin(K_QK_NORM_ROPE, st);
     MOA_KLAUNCH(k_qk_norm_rope<T>, dim3((unsigned)a.T), dim3(256), 0, st, a);
     prof_end(st);
@@ -131,8 +266,9 @@ int32_t moa_qk_norm_rope(int32_t dtype, const void *q, int64_t q_stride, int32_t
     if (n_kv_heads) bits |= (uintptr_t)k | (uintptr_t)k_out;
     bits |= (uintptr_t)gq | (uintptr_t)gk;
     if ((bits & (es - 1)) || ((uintptr_t)pos & 3)) return api_fail(MOA_ERR_SHAPE, "qk_norm_rope: pointers must be aligned to their elements");
-    const RopeNormArgs a = {{q, k}, {q_out, k_out}, {gq, gk}, {q_stride, k_stride}, {q_out_stride, k_out_stride}, {n_q_heads, n_kv_heads}, T, pos,
-                            head_dim, rot_dim / 2, rms_eps, rot_dim ? log((double)rope_theta) : 0.0};
+    RopeNormArgs a = {{q, k}, {q_out, k_out}, {gq, gk}, {q_stride, k_stride}, {q_out_stride, k_out_stride}, {n_q_heads, n_kv_heads}, T, pos,
+                            head_dim, rot_dim / 2, rms_eps, {}};
+    for (int i = 0; i < 7 && rot_dim; ++i) a.power[i] = exp(-log((double)rope_theta) * ((1 << i) / (0.5 * rot_dim)));
     prof_set_site(S_QK_NORM_ROPE);
     const hipError_t e = dtype == MOA_BF16 ? launch<bf16_t>(a, (hipStream_t)stream) : launch<float>(a, (hipStream_t)stream);
     return e == hipSuccess ? MOA_OK : api_fail(MOA_ERR_HIP, hipGetErrorString(e));
