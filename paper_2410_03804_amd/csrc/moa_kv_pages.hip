@@ -10,7 +10,7 @@ namespace moa {
 
 namespace {
 
-constexpr int PT = 1024, PW = PT / 64;             // threads, wavefronts
+constexpr int PT = 1024, PW = PT / 64, PU = 4;     // threads, wavefronts, table entries a thread looks at
 
 // Sums over the workgroup's threads in their order.  Two sets of LDS in turn, so that one barrier a sum is enough.
 struct BlockScan {
@@ -121,15 +121,37 @@ __global__ __launch_bounds__(PT) void k_kv_reserve(ReserveArgs a)
         first_s[tid] = p0;
         need_s[tid] = 0;
         __syncthreads();
-        auto entry = [&](uint32_t i, int &s) -> int32_t * {
-            s = last_upto<uint32_t>(items_s, PT, i);
-            return a.table + (int64_t)(b0 + s) * a.max_pages + first_s[s] + (int)(i - items_s[s]);
+        // PU of them a thread, one behind the other: their sequences and table entries; which of them name no page
+        uint32_t lacks = 0;
+        auto look_at = [&](uint32_t i0, int (&s)[PU], int32_t *(&e)[PU]) {
+            const uint32_t i1 = i0 + PU * tid;
+            lacks = 0;
+            if (i1 >= item.all) return;
+            s[0] = last_upto<uint32_t>(items_s, PT, i1);
+#pragma unroll
+            for (int u = 0; u < PU; ++u) {
+                const uint32_t i = i1 + u;
+                if (u > 0) s[u] = s[u - 1];
+                if (i >= item.all) continue;
+                while (s[u] + 1 < PT && items_s[s[u] + 1] <= i) ++s[u];
+                e[u] = a.table + (int64_t)(b0 + s[u]) * a.max_pages + first_s[s[u]] + (int)(i - items_s[s[u]]);
+            }
+            int32_t id[PU];
+#pragma unroll
+            for (int u = 0; u < PU; ++u) id[u] = i1 + u < item.all ? *e[u] : 0;
+#pragma unroll
+            for (int u = 0; u < PU; ++u) {
+                if (id[u] < 0) lacks |= 1u << u;
+                else if (id[u] >= a.n_pages) a.flag(MOA_DEV_BAD_PAGE);
+            }
         };
-        for (uint32_t i = tid; i < item.all; i += PT) {
-            int s;
-            const int32_t id = *entry(i, s);
-            if (id < 0) atomicAdd(&need_s[s], 1u);
-            else if (id >= a.n_pages) a.flag(MOA_DEV_BAD_PAGE);
+        int s[PU];
+        int32_t *e[PU];
+        for (uint32_t i0 = 0; i0 < item.all; i0 += PT * PU) {
+            look_at(i0, s, e);
+#pragma unroll
+            for (int u = 0; u < PU; ++u)
+                if (lacks >> u & 1) atomicAdd(&need_s[s[u]], 1u);
         }
         __syncthreads();
         // in their order, as long as the free pages last; who lacks none goes on in any case
@@ -142,21 +164,20 @@ __global__ __launch_bounds__(PT) void k_kv_reserve(ReserveArgs a)
         refused |= give.all != lack.all;
         // (the barriers of the sums stand between got_s and its use)
         uint32_t rank = needed;
-        for (uint32_t i0 = 0; i0 < item.all; i0 += PT) {
-            const uint32_t i = i0 + tid;
-            int s = 0;
-            int32_t *e = nullptr;
-            bool lacks = false;
-            if (i < item.all) {
-                e = entry(i, s);
-                lacks = *e < 0;
-            }
-            const BlockScan::Sum r = scan(lacks ? 1u : 0u);
-            if (lacks && got_s[s]) {
-                const int32_t id = a.free_pages[left - 1 - (int)(rank + r.before)];
-                if ((uint32_t)id >= (uint32_t)a.n_pages) a.flag(MOA_DEV_BAD_PAGE);
-                *e = id;
-            }
+        for (uint32_t i0 = 0; i0 < item.all; i0 += PT * PU) {
+            if (item.all > PT * PU) look_at(i0, s, e);         // (else as it was left)
+            const BlockScan::Sum r = scan(__popc(lacks));
+            uint32_t at = rank + r.before;
+#pragma unroll
+            for (int u = 0; u < PU; ++u)
+                if (lacks >> u & 1) {
+                    if (got_s[s[u]]) {
+                        const int32_t id = a.free_pages[left - 1 - (int)at];
+                        if ((uint32_t)id >= (uint32_t)a.n_pages) a.flag(MOA_DEV_BAD_PAGE);
+                        *e[u] = id;
+                    }
+                    ++at;
+                }
             rank += r.all;
         }
         needed += lack.all;
@@ -203,7 +224,7 @@ struct ReleaseArgs {
 // The table as one list of entries, walked from its end: what goes back first lies deepest in the list of free pages.
 __global__ __launch_bounds__(PT) void k_kv_release(ReleaseArgs a)
 {
-    constexpr int U = 4;
+    constexpr int U = PU;
     __shared__ uint32_t sums[2][PW];
     const int tid = threadIdx.x;
     BlockScan scan{sums};

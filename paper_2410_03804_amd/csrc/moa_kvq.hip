@@ -83,9 +83,11 @@ __device__ __forceinline__ float wave_max(float x)
     return x;
 }
 
-// One wavefront encodes what a call brings of one block of one KV head, of the keys or of the values.
-// VE: elements that are read and encoded at a time, 16 bytes' worth, or 1 where rows are not in such pieces.
-template <typename T, int VE>
+// One wavefront encodes what a call brings of one block of one KV head, of the keys or of the values: its rows are read once, into registers,
+// while the table's entry and the block's scale are on their way.
+// VE: elements that are read and encoded at a time, 16 bytes' worth, or 1 where rows are not in such pieces; IT: such pieces that a lane has at
+// most, 0: rows are read twice instead.
+template <typename T, int VE, int IT>
 __device__ __forceinline__ void encode_block(const KvqAppendArgs &a, int b, int h, bool values, int held, NewRows in, int gb)
 {
     const KvDev &c = a.c.c;
@@ -93,14 +95,10 @@ __device__ __forceinline__ void encode_block(const KvqAppendArgs &a, int b, int 
     const int pg = (int)a.c.blocks((uint32_t)gb), r0 = (gb - pg * (int)a.c.blocks.d) * BLK;
     const int s0 = pg * ps + r0, from = max(s0, held), rows = min(min(s0 + BLK, (pg + 1) * ps), held + in.n) - from;
     const int id = c.table[(int64_t)b * c.max_pages + pg];
-    if (!a.c.is_page(id)) {
-        if (lane == 0) c.flag(MOA_DEV_BAD_PAGE);
-        return;
-    }
     const T *src = (const T *)(values ? a.v_new : a.k_new) + b * a.seq_stride + h * a.head_stride;
     const int64_t row_stride = values ? a.v_row_stride : a.k_row_stride;
     const int pieces = (int)a.pieces.d, items = rows * pieces;
-    auto load = [&](int it, float (&x)[VE]) {
+    auto load = [&](int it, u32x4 &x) {
         const int i = (int)a.pieces((uint32_t)it), p = it - i * pieces, at = from - held + i;
         int row = at;
         if (a.path) {
@@ -111,31 +109,53 @@ __device__ __forceinline__ void encode_block(const KvqAppendArgs &a, int b, int 
             }
         }
         const T *p0 = src + (in.first + row) * row_stride + p * VE;
-        if constexpr (VE == 1) x[0] = ld(p0);
-        else {
-            const u32x4 w = *(const u32x4 *)p0;
-#pragma unroll
-            for (int e = 0; e < VE; ++e)
-                x[e] = sizeof(T) == 4 ? __uint_as_float(w[e]) : __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
-        }
+        if constexpr (VE == 1) x[0] = __float_as_uint(ld(p0));
+        else x = *(const u32x4 *)p0;
+    };
+    auto value = [](const u32x4 &x, int e) {
+        return VE == 1 || sizeof(T) == 4 ? __uint_as_float(x[e]) : __uint_as_float(e & 1 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16);
     };
     float most = 0.f;
-    for (int it = lane; it < items; it += 64) {
-        float x[VE];
-        load(it, x);
+    auto measure = [&](const u32x4 &x) {
 #pragma unroll
-        for (int e = 0; e < VE; ++e) most = fmaxf(most, fabsf(x[e]) < INFINITY ? fabsf(x[e]) : 0.f);     // (NaN and infinity are held as NaN by any scale)
+        for (int e = 0; e < VE; ++e) {
+            const float v = fabsf(value(x, e));
+            most = fmaxf(most, v < INFINITY ? v : 0.f);                       // (NaN and infinity are held as NaN by any scale)
+        }
+    };
+    u32x4 held_x[IT ? IT : 1];
+    if constexpr (IT > 0) {
+#pragma unroll
+        for (int k = 0; k < IT; ++k) {
+            held_x[k] = u32x4{0u, 0u, 0u, 0u};
+            if (64 * k < items && lane + 64 * k < items) load(lane + 64 * k, held_x[k]);
+        }
+    }
+    if (!a.c.is_page(id)) {
+        if (lane == 0) c.flag(MOA_DEV_BAD_PAGE);
+        return;
     }
     float *const scale_at = (values ? a.c.v_scale : a.c.k_scale) + a.c.block_in(id, h, r0);
+    const float old = s0 < held ? *scale_at : 0.f;
+    if constexpr (IT > 0) {
+#pragma unroll
+        for (int k = 0; k < IT; ++k) measure(held_x[k]);
+    } else
+#pragma unroll 1
+        for (int it = lane; it < items; it += 64) {
+            u32x4 x;
+            load(it, x);
+            measure(x);
+        }
     char *const pool = values ? c.v : c.k;
     const int64_t row0 = (int64_t)(id * c.Hkv + h) * ps;
     float scale = smallest_scale(wave_max(most));
     if (s0 < held) {
-        const float old = *scale_at;
         if (scale > old) {
             // rows that the block holds already, in the new scale
             const float f = old / scale;
             unsigned char *p = (unsigned char *)pool + (row0 + r0) * dh;
+#pragma unroll 1
             for (int i = lane; i < (from - s0) * dh; i += 64) p[i] = (unsigned char)code_pair(code_value<0>(p[i]) * f, 0.f, 0, false);
         } else scale = old;
     }
@@ -143,13 +163,12 @@ __device__ __forceinline__ void encode_block(const KvqAppendArgs &a, int b, int 
     // (a scale that this call did not make may be no power of two)
     const bool exact = (__float_as_uint(scale) & 0x807fffffu) == 0 && scale >= 0x1p-126f && scale <= 0x1p126f;
     const float inv = exact ? 1.f / scale : 0.f;
-    for (int it = lane; it < items; it += 64) {
+    unsigned char *const to0 = (unsigned char *)pool + (row0 + r0 + from - s0) * dh;
+    auto store = [&](int it, const u32x4 &v, bool divide) {
         float x[VE];
-        load(it, x);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) x[e] = exact ? x[e] * inv : x[e] / scale;
-        const int i = (int)a.pieces((uint32_t)it), p = it - i * pieces;
-        unsigned char *to = (unsigned char *)pool + (row0 + r0 + from - s0 + i) * dh + p * VE;
+        for (int e = 0; e < VE; ++e) x[e] = divide ? value(v, e) / scale : value(v, e) * inv;
+        unsigned char *to = to0 + (int64_t)it * VE;                             // (rows of a block lie behind each other)
         if constexpr (VE == 1) *to = (unsigned char)code_pair(x[0], 0.f, 0, false);
         else {
             uint32_t w[VE / 4];
@@ -158,11 +177,22 @@ __device__ __forceinline__ void encode_block(const KvqAppendArgs &a, int b, int 
             if constexpr (VE == 8) *(u32x2 *)to = u32x2{w[0], w[1]};
             else *(uint32_t *)to = w[0];
         }
-    }
+    };
+    if (IT > 0 && exact) {
+#pragma unroll
+        for (int k = 0; k < IT; ++k)
+            if (lane + 64 * k < items) store(lane + 64 * k, held_x[k], false);
+    } else
+#pragma unroll 1
+        for (int it = lane; it < items; it += 64) {
+            u32x4 x;
+            load(it, x);
+            store(it, x, !exact);
+        }
 }
 
 // ONE: a workgroup per sequence, which may then also move its length on.  Else gridDim.x of them per sequence.
-template <typename T, int VE, int THREADS, bool ONE>
+template <typename T, int VE, int IT, int THREADS, bool ONE>
 __global__ __launch_bounds__(THREADS) void k_kvq_append(KvqAppendArgs a)
 {
     const KvDev &c = a.c.c;
@@ -179,7 +209,7 @@ __global__ __launch_bounds__(THREADS) void k_kvq_append(KvqAppendArgs a)
         const int gb0 = block_of(held), units = (block_of(held + in.n - 1) - gb0 + 1) * c.Hkv * 2;
         for (int u = blockIdx.x * (THREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); u < units; u += gridDim.x * (THREADS / 64)) {
             const int j = u / (2 * c.Hkv), hv = u - j * 2 * c.Hkv;
-            encode_block<T, VE>(a, b, hv >> 1, hv & 1, held, in, gb0 + j);
+            encode_block<T, VE, IT>(a, b, hv >> 1, hv & 1, held, in, gb0 + j);
         }
     }
     if (ONE) {
@@ -196,16 +226,16 @@ __global__ __launch_bounds__(256) void k_kvq_append_len(KvqAppendArgs a)
     a.c.c.len[b] = held + new_rows(a, b, held, false).n;
 }
 
-template <typename T, int VE>
+template <typename T, int VE, int IT>
 hipError_t launch_append(const KvqAppendArgs &a, hipStream_t st)
 {
     const int64_t units = ((int64_t)a.M / BLK + 2) * a.c.c.Hkv * 2;
-    const bool one = units <= 64;
+    const bool one = units <= 128;
     prof_begin(K_KVQ_APPEND, st);
-    if (one) MOA_KLAUNCH((k_kvq_append<T, VE, 1024, true>), dim3(1, 1, a.c.c.B), dim3(1024), 0, st, a);
+    if (one) MOA_KLAUNCH((k_kvq_append<T, VE, IT, 1024, true>), dim3(1, 1, a.c.c.B), dim3(1024), 0, st, a);
     else {
         const int64_t blocks = (units + 3) / 4, most = 4096 / a.c.c.B + 1;
-        MOA_KLAUNCH((k_kvq_append<T, VE, 256, false>), dim3((unsigned)(blocks < most ? blocks : most), 1, a.c.c.B), dim3(256), 0, st, a);
+        MOA_KLAUNCH((k_kvq_append<T, VE, IT, 256, false>), dim3((unsigned)(blocks < most ? blocks : most), 1, a.c.c.B), dim3(256), 0, st, a);
     }
     prof_end(st);
     if (!one) {
@@ -224,8 +254,16 @@ int32_t append(KvqAppendArgs &a, int64_t strides, hipStream_t st, int dtype)
                         !(((uintptr_t)a.c.c.k | (uintptr_t)a.c.c.v) & (ve - 1));
     a.pieces = FastDiv((uint32_t)(pieces ? dh / ve : dh));
     prof_set_site(S_KVQ);
-    const hipError_t e = dtype == MOA_BF16 ? pieces ? launch_append<bf16_t, 8>(a, st) : launch_append<bf16_t, 1>(a, st)
-                                           : pieces ? launch_append<float, 4>(a, st) : launch_append<float, 1>(a, st);
+    // pieces of a block's new rows a lane.  (One where it can be: the kernel's code is fetched while it runs, once.)
+    const int per_lane = ((a.M < BLK ? a.M : BLK) * (int)a.pieces.d + 63) / 64;
+    const hipError_t e = dtype == MOA_BF16 ? !pieces         ? launch_append<bf16_t, 1, 0>(a, st)
+                                             : per_lane <= 1 ? launch_append<bf16_t, 8, 1>(a, st)
+                                             : per_lane <= 4 ? launch_append<bf16_t, 8, 4>(a, st)
+                                                             : launch_append<bf16_t, 8, 0>(a, st)
+                         : !pieces         ? launch_append<float, 1, 0>(a, st)
+                         : per_lane <= 1   ? launch_append<float, 4, 1>(a, st)
+                         : per_lane <= 4   ? launch_append<float, 4, 4>(a, st)
+                                           : launch_append<float, 4, 0>(a, st);
     return e == hipSuccess ? MOA_OK : api_fail(MOA_ERR_HIP, hipGetErrorString(e));
 }
 
@@ -237,10 +275,14 @@ struct KvqReadArgs {
     FastDiv pieces;
 };
 
-// VE codes at a time: 16, or 1 where rows are not in such pieces.
+// VE codes at a time, 16 bytes of results, or 1 where rows are not in such pieces.  HBM bounds it: 16 sequences of 100 to 1500 tokens, 79 MB, 23 us
+// with 16 codes a load and 32 bytes of results behind each other, 21.8 with 16 bytes, 16.8 when the stores say that nothing of it is read
+// again soon, 15 with two of them a thread instead of four.
+constexpr int READ_U = 2;
 template <typename T, int VE>
 __global__ __launch_bounds__(256) void k_kvq_read(KvqReadArgs a)
 {
+    constexpr int U = READ_U;
     const KvDev &c = a.c.c;
     const int b = blockIdx.z, h = blockIdx.y >> 1, pieces = (int)a.pieces.d;
     const bool values = blockIdx.y & 1, first = blockIdx.x + blockIdx.y == 0 && threadIdx.x == 0;
@@ -250,36 +292,44 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqReadArgs a)
     const float *scales = values ? a.c.v_scale : a.c.k_scale;
     T *out = (T *)(values ? a.v_out : a.k_out) + ((int64_t)b * c.Hkv + h) * a.P * c.dh;
     const uint32_t items = (uint32_t)n * pieces;
-    for (uint32_t it = blockIdx.x * 256 + threadIdx.x; it < items; it += gridDim.x * 256) {
-        const int s = (int)a.pieces(it), p = (int)it - s * pieces, pg = (int)c.page((uint32_t)s), r = s - pg * (int)c.page.d;
-        const int id = c.table[(int64_t)b * c.max_pages + pg];
-        if (!a.c.is_page(id)) {
-            c.flag(MOA_DEV_BAD_PAGE);
-            continue;
+    for (uint32_t it0 = blockIdx.x * (256 * U) + threadIdx.x; it0 < items; it0 += gridDim.x * (256 * U)) {
+        int id[U], r[U];
+        u32x2 w[U];
+        float scale[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t it = min(it0 + 256 * u, items - 1);
+            const int s = (int)a.pieces(it), pg = (int)c.page((uint32_t)s);
+            r[u] = s - pg * (int)c.page.d;
+            id[u] = c.table[(int64_t)b * c.max_pages + pg];
         }
-        const float scale = scales[a.c.block_in(id, h, r)];
-        const unsigned char *from = pool + ((int64_t)(id * c.Hkv + h) * c.page.d + r) * c.dh + p * VE;
-        T *to = out + (int64_t)s * c.dh + p * VE;
-        if constexpr (VE == 1) st(to, code_value<0>(*from) * scale);
-        else {
-            const u32x4 w = *(const u32x4 *)from;
-            float x[16];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                x[4 * q] = code_value<0>(w[q]) * scale;
-                x[4 * q + 1] = code_value<1>(w[q]) * scale;
-                x[4 * q + 2] = code_value<2>(w[q]) * scale;
-                x[4 * q + 3] = code_value<3>(w[q]) * scale;
+        for (int u = 0; u < U; ++u) {
+            const uint32_t it = it0 + 256 * u;
+            if (it >= items || !a.c.is_page(id[u])) continue;
+            const int p = (int)(it - a.pieces(it) * pieces);
+            const unsigned char *from = pool + ((int64_t)(id[u] * c.Hkv + h) * c.page.d + r[u]) * c.dh + p * VE;
+            scale[u] = scales[a.c.block_in(id[u], h, r[u])];
+            if constexpr (VE == 8) w[u] = *(const u32x2 *)from;
+            else if constexpr (VE == 4) w[u][0] = *(const uint32_t *)from;
+            else w[u][0] = *from;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t it = it0 + 256 * u;
+            if (it >= items) continue;
+            if (!a.c.is_page(id[u])) {
+                c.flag(MOA_DEV_BAD_PAGE);
+                continue;
             }
-            if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) *(f32x4 *)(to + 4 * q) = f32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
-            } else {
-#pragma unroll
-                for (int q = 0; q < 2; ++q)
-                    *(u32x4 *)(to + 8 * q) = u32x4{pack_bf16x2(x[8 * q], x[8 * q + 1]), pack_bf16x2(x[8 * q + 2], x[8 * q + 3]),
-                                                   pack_bf16x2(x[8 * q + 4], x[8 * q + 5]), pack_bf16x2(x[8 * q + 6], x[8 * q + 7])};
-            }
+            T *to = out + (int64_t)it * VE;                                     // (rows of a head lie behind each other)
+            const float sc = scale[u];
+            if constexpr (VE == 1) st(to, code_value<0>(w[u][0]) * sc);
+            else if constexpr (VE == 4)
+                __builtin_nontemporal_store(f32x4{code_value<0>(w[u][0]) * sc, code_value<1>(w[u][0]) * sc, code_value<2>(w[u][0]) * sc, code_value<3>(w[u][0]) * sc}, (f32x4 *)to);
+            else
+                __builtin_nontemporal_store(u32x4{pack_bf16x2(code_value<0>(w[u][0]) * sc, code_value<1>(w[u][0]) * sc), pack_bf16x2(code_value<2>(w[u][0]) * sc, code_value<3>(w[u][0]) * sc),
+                                     pack_bf16x2(code_value<0>(w[u][1]) * sc, code_value<1>(w[u][1]) * sc), pack_bf16x2(code_value<2>(w[u][1]) * sc, code_value<3>(w[u][1]) * sc)}, (u32x4 *)to);
         }
     }
 }
@@ -287,7 +337,7 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqReadArgs a)
 template <typename T, int VE>
 hipError_t launch_read(const KvqReadArgs &a, hipStream_t st)
 {
-    const int64_t blocks = ((int64_t)a.P * a.pieces.d + 1023) / 1024;
+    const int64_t blocks = ((int64_t)a.P * a.pieces.d + 256 * READ_U - 1) / (256 * READ_U);
     prof_begin(K_KVQ_READ, st);
     MOA_KLAUNCH((k_kvq_read<T, VE>), dim3((unsigned)(blocks < 1024 ? blocks : 1024), a.c.c.Hkv * 2, a.c.c.B), dim3(256), 0, st, a);
     prof_end(st);
@@ -351,12 +401,13 @@ int32_t moa_kvq_read(const moa_kvq_cache_t *cache, int32_t P_cap, void *k_out, v
     if (((uintptr_t)k_out | (uintptr_t)v_out) & (es - 1)) return api_fail(MOA_ERR_SHAPE, "kvq_read: k_out / v_out not aligned to their elements");
     if (P_cap < 1 || P_cap > (1 << 30) || (int64_t)P_cap * cache->head_dim > INT32_MAX) return api_fail(MOA_ERR_SHAPE, "kvq_read: P_cap outside [1, 2^30], or P_cap * head_dim above 2^31 - 1");
     if (cache->B > 65535 || cache->n_kv_heads > 32767) return api_fail(MOA_ERR_SHAPE, "kvq_read: more than 65535 sequences or 32767 KV heads");
-    const bool pieces = cache->head_dim % 16 == 0 && !(((uintptr_t)k_out | (uintptr_t)v_out | (uintptr_t)cache->k | (uintptr_t)cache->v) & 15);
-    KvqReadArgs a = {KvqDev(*cache, dev_status), P_cap, (char *)k_out, (char *)v_out, FastDiv((uint32_t)(pieces ? cache->head_dim / 16 : cache->head_dim))};
+    const int ve = 16 / es;
+    const bool pieces = cache->head_dim % ve == 0 && !(((uintptr_t)k_out | (uintptr_t)v_out) & 15) && !(((uintptr_t)cache->k | (uintptr_t)cache->v) & (ve - 1));
+    const KvqReadArgs a = {KvqDev(*cache, dev_status), P_cap, (char *)k_out, (char *)v_out, FastDiv((uint32_t)(pieces ? cache->head_dim / ve : cache->head_dim))};
     prof_set_site(S_KVQ);
     hipStream_t st = (hipStream_t)stream;
-    const hipError_t e = cache->dtype == MOA_BF16 ? pieces ? launch_read<bf16_t, 16>(a, st) : launch_read<bf16_t, 1>(a, st)
-                                                  : pieces ? launch_read<float, 16>(a, st) : launch_read<float, 1>(a, st);
+    const hipError_t e = cache->dtype == MOA_BF16 ? pieces ? launch_read<bf16_t, 8>(a, st) : launch_read<bf16_t, 1>(a, st)
+                                                  : pieces ? launch_read<float, 4>(a, st) : launch_read<float, 1>(a, st);
     return e == hipSuccess ? MOA_OK : api_fail(MOA_ERR_HIP, hipGetErrorString(e));
 }
 
