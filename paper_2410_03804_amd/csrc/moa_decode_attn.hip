@@ -401,7 +401,7 @@ __global__ __launch_bounds__(256, DH == 256 || CT == 2 ? 1 : 2) void k_decode_at
 // where most slots are in use and is paid for where few are.  16 sequences of 2048 tokens, 8b heads, us: 7.2 in a capacity of
 // 2112, 19.3 of 16384, 48.5 of 65536; 64 of 1000: none in a capacity of 1024, 36 of 8192, 91 of 32768.  (Without accounts 4 in any.)
 constexpr int ACC_SLOTS = 256;
-template <typename T, int KEYS>
+template <typename T>
 __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
 {
     __shared__ float sm[2][32][8], fin[32][2];
@@ -444,14 +444,14 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a)
     }
     uint32_t all = 0, before = 0;
     for (int b0 = 0; b0 < a.c.B; b0 += 64) {
-        const uint32_t upto = wave_scan(b0 + lane < a.c.B ? tiles_of<KEYS>(a.c.length(b0 + lane, false)) : 0u);
+        const uint32_t upto = wave_scan(b0 + lane < a.c.B ? tiles_of(a.c.length(b0 + lane, false)) : 0u);
         if (b > b0) before = all + from_lane(upto, min(b - b0, 64) - 1);
         all += from_lane(upto, 63);
     }
-    TileList<KEYS> list;
+    TileList list;
     list.set(a, all);
     const int len = a.c.length(b, !accounts && h + r == 0 && tid == 0);
-    const uint32_t nt = tiles_of<KEYS>(len);
+    const uint32_t nt = tiles_of(len);
     // the runs that tiles of row tile rt of this KV head are in, and the first's place among the partial results
     auto runs_of = [&](int rt, uint32_t &w0, uint32_t &ns, int64_t &slot0) {
         const uint32_t hb = (uint32_t)(h * a.rtiles + rt), f0 = before * (uint32_t)a.HB + hb * nt;
@@ -643,7 +643,7 @@ hipError_t launch_decode(const DecodeArgs &a, bool mfma, bool wide, hipStream_t 
     else if constexpr (sizeof(T) == 4)
         e = a.HG == 2 ? launch_rows<T, 2, true>(a, grid, st) : a.HG == 4 ? launch_rows<T, 4, true>(a, grid, st) : launch_rows<T, 8, true>(a, grid, st);
     if (e != hipSuccess || !a.runs) return e;
-    return launch_decode_join(a, sizeof(T) == 2, TK, st);
+    return launch_decode_join(a, sizeof(T) == 2, st);
 }
 
 int32_t check_decode(const moa_kv_cache_t *c, int32_t H, const char *who)
@@ -661,20 +661,15 @@ int32_t check_decode(const moa_kv_cache_t *c, int32_t H, const char *who)
 
 }  // namespace
 
-hipError_t launch_decode_join(const DecodeArgs &a, bool bf16, int keys, hipStream_t st)
+hipError_t launch_decode_join(const DecodeArgs &a, bool bf16, hipStream_t st)
 {
     // (a dimension of a launch has less than 2^32 threads)
     const int64_t accounts = a.raw ? (int64_t)a.c.B * a.c.Hkv * ((a.c.cap + ACC_SLOTS - 1) / ACC_SLOTS) : 0;
     const int64_t wide_x = accounts < (1 << 20) ? accounts : 1 << 20, y = accounts > wide_x ? (accounts + wide_x - 1) / wide_x : 1;
     const dim3 grid((unsigned)(a.c.B * a.H + wide_x), (unsigned)y);
     prof_begin(K_DECODE_JOIN, st);
-    if (keys == TK) {
-        if (bf16) MOA_KLAUNCH((k_decode_join<bf16_t, TK>), grid, dim3(256), 0, st, a);
-        else MOA_KLAUNCH((k_decode_join<float, TK>), grid, dim3(256), 0, st, a);
-    } else {
-        if (bf16) MOA_KLAUNCH((k_decode_join<bf16_t, WK>), grid, dim3(256), 0, st, a);
-        else MOA_KLAUNCH((k_decode_join<float, WK>), grid, dim3(256), 0, st, a);
-    }
+    if (bf16) MOA_KLAUNCH(k_decode_join<bf16_t>, grid, dim3(256), 0, st, a);
+    else MOA_KLAUNCH(k_decode_join<float>, grid, dim3(256), 0, st, a);
     prof_end(st);
     return hipGetLastError();
 }

@@ -25,8 +25,8 @@ struct DecodeArgs {
     float *raw;                   // [B, HB, cap32, HG] scores, where accounts are kept; else NULL
 };
 
-// the second launch (moa_decode_attn.hip): joins the partial results, and brings accounts up to date; keys: of a tile, TK or WK
-hipError_t launch_decode_join(const DecodeArgs &a, bool bf16, int keys, hipStream_t st);
+// the second launch (moa_decode_attn.hip): joins the partial results, and brings accounts up to date
+hipError_t launch_decode_join(const DecodeArgs &a, bool bf16, hipStream_t st);
 
 namespace {
 
@@ -71,7 +71,6 @@ __device__ __forceinline__ float max_of_keys(float m, bool any) { return any && 
 __device__ __forceinline__ float inverse_sum(float m, float l) { return l != 0.f ? 1.f / l : m == -INFINITY ? 0.f : __builtin_nanf(""); }
 
 // Where the tiles of the sequences lie in the list of all tiles: every wavefront works this out for itself.
-template <int KEYS = TK>
 struct TileList {
     uint32_t total, per;          // tiles in all, of a run
     __device__ __forceinline__ void set(const DecodeArgs &a, uint32_t all)       // all: tiles of the sequences, for one KV head
@@ -84,8 +83,8 @@ struct TileList {
     {
         const int lane = threadIdx.x & 63;
         int mine = lane < a.c.B ? a.c.length(lane, false) : 0;
-        uint32_t upto = wave_scan(tiles_of<KEYS>(mine)), all = from_lane(upto, 63);
-        for (int i = lane + 64; i < (a.c.B + 63) / 64 * 64; i += 64) all += from_lane(wave_scan(i < a.c.B ? tiles_of<KEYS>(a.c.length(i, false)) : 0u), 63);
+        uint32_t upto = wave_scan(tiles_of(mine)), all = from_lane(upto, 63);
+        for (int i = lane + 64; i < (a.c.B + 63) / 64 * 64; i += 64) all += from_lane(wave_scan(i < a.c.B ? tiles_of(a.c.length(i, false)) : 0u), 63);
         set(a, all);
         const uint32_t f = w * per;
         if (f >= total) return false;
@@ -96,12 +95,12 @@ struct TileList {
                 const int at = __ffsll((unsigned long long)past) - 1;
                 b = b0 + at;
                 len = (int)from_lane((uint32_t)mine, at);
-                begin = (base + from_lane(upto, at) - tiles_of<KEYS>(len)) * (uint32_t)a.HB;
+                begin = (base + from_lane(upto, at) - tiles_of(len)) * (uint32_t)a.HB;
                 return true;
             }
             base += from_lane(upto, 63);
             mine = b0 + 64 + lane < a.c.B ? a.c.length(b0 + 64 + lane, false) : 0;
-            upto = wave_scan(tiles_of<KEYS>(mine));
+            upto = wave_scan(tiles_of(mine));
         }
     }
 };
@@ -167,7 +166,7 @@ __device__ __forceinline__ void for_each_pair(const DecodeArgs &a, const F &proc
         len = (int)uniform((uint32_t)a.c.length(b, hb == 0 && threadIdx.x == 0));
         cnt = tiles_of(len);
     } else {
-        TileList<> list;
+        TileList list;
         if (!list.find(a, blockIdx.x, b, len, begin)) return;
         f = blockIdx.x * list.per;
         end = min(f + list.per, list.total);

@@ -149,9 +149,16 @@ __global__ __launch_bounds__(PT) void k_kv_reserve(ReserveArgs a)
         int32_t *e[PU];
         for (uint32_t i0 = 0; i0 < item.all; i0 += PT * PU) {
             look_at(i0, s, e);
+            // (one addition a thread and sequence: the entries of a long prompt would else all add to the same place)
+            uint32_t sum = 0;
 #pragma unroll
-            for (int u = 0; u < PU; ++u)
-                if (lacks >> u & 1) atomicAdd(&need_s[s[u]], 1u);
+            for (int u = 0; u < PU; ++u) {
+                sum += lacks >> u & 1;
+                if (sum && (u + 1 == PU || i0 + PU * tid + u + 1 >= item.all || s[u + 1 < PU ? u + 1 : u] != s[u])) {
+                    atomicAdd(&need_s[s[u]], sum);
+                    sum = 0;
+                }
+            }
         }
         __syncthreads();
         // in their order, as long as the free pages last; who lacks none goes on in any case

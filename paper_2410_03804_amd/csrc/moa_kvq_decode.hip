@@ -167,10 +167,54 @@ __device__ __forceinline__ bf16x8 widen(uint32_t c0, uint32_t c1)
 
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 
+// The list of all tiles of 32 keys of all pairs, dealt to the runs so that none has more than one more than another.  A pair takes up one more
+// place than it has tiles, since going on to it costs a wavefront up to a tile's time (its queries are waited for, its predecessor's result is
+// written): 64 ragged sequences up to 8192, some of which are short, 105 us without and 94 with.
+struct PlaceList {
+    uint32_t total;                      // places
+    static __device__ __forceinline__ uint32_t of(int len) { return tiles_of<WK>(len) + (len > 0); }
+    // the first place of run w (of the one behind the last: total), and the run of place f; runs beyond the places have none
+    __device__ __forceinline__ uint32_t first(const DecodeArgs &a, uint32_t w) const
+    {
+        return total < (uint32_t)a.runs ? min(w, total) : (uint32_t)((uint64_t)w * total >> a.runs_log2);
+    }
+    __device__ __forceinline__ uint32_t run_of(const DecodeArgs &a, uint32_t f) const
+    {
+        return total < (uint32_t)a.runs ? f : (uint32_t)((((uint64_t)(f + 1) << a.runs_log2) - 1) / total);
+    }
+    // the sequence that place f of run w's first is in, its length and its first place; false where the run has none
+    __device__ __forceinline__ bool find(const DecodeArgs &a, uint32_t w, int &b, int &len, uint32_t &begin, uint32_t &f, uint32_t &n)
+    {
+        const int lane = threadIdx.x & 63;
+        int mine = lane < a.c.B ? a.c.length(lane, false) : 0;
+        uint32_t upto = wave_scan(of(mine)), all = from_lane(upto, 63);
+        for (int i = lane + 64; i < (a.c.B + 63) / 64 * 64; i += 64) all += from_lane(wave_scan(i < a.c.B ? of(a.c.length(i, false)) : 0u), 63);
+        total = all * (uint32_t)a.HB;
+        f = first(a, w);
+        n = first(a, w + 1) - f;
+        if (n == 0) return false;
+        uint32_t base = 0;
+        for (int b0 = 0;; b0 += 64) {
+            const uint64_t past = __ballot(f < (base + upto) * (uint32_t)a.HB);
+            if (past) {
+                const int at = __ffsll((unsigned long long)past) - 1;
+                b = b0 + at;
+                len = (int)from_lane((uint32_t)mine, at);
+                begin = (base + from_lane(upto, at) - of(len)) * (uint32_t)a.HB;
+                return true;
+            }
+            base += from_lane(upto, 63);
+            mine = b0 + 64 + lane < a.c.B ? a.c.length(b0 + 64 + lane, false) : 0;
+            upto = wave_scan(of(mine));
+        }
+    }
+};
+
 // Where a wavefront's tile lies, and what is to be done behind it.
+enum { GOES_ON = 0, PART_ENDS = 1, PAIR_ENDS = 2, NO_TILE = 3 };
 struct Place {
     int b, hb, len, key0;
-    uint32_t ends;                       // 0: the next tile is of the same pair; 1: a part of a pair ends here; 2: a whole one does
+    int ends;
 };
 
 // The tiles of a wavefront's run, pair after pair.  Lengths of 64 sequences lie in a register, so that going on to the next sequence waits
@@ -178,7 +222,7 @@ struct Place {
 struct Walk {
     const DecodeArgs &a;
     int b, hb, len, lens_b, lens;
-    uint32_t t, nt, left;                // the next tile of the pair, its tiles, tiles of the run
+    uint32_t t, nt, left;                // the next tile of the pair, its tiles, places of the list that are left of the run
     bool from_start;                     // the run has had the pair's first tile
     __device__ __forceinline__ int length(int of)
     {
@@ -191,12 +235,17 @@ struct Walk {
     }
     __device__ __forceinline__ void next(Place &p)
     {
-        p = Place{b, hb, len, (int)t * WK, 0};
-        if (left == 0) return;           // (no such tile: its table entries are read as if it were the pair's next one, and not used)
+        // (behind the last tile: table entries are read as if it were the pair's next one, and not used)
+        p = Place{b, hb, len, (int)t * WK, NO_TILE};
+        if (left == 0) return;
         --left;
         ++t;
-        p.ends = t == nt ? 1 + from_start : left == 0;
-        if (t < nt || left == 0) return;
+        p.ends = t == nt ? from_start ? PAIR_ENDS : PART_ENDS : left == 0 ? PART_ENDS : GOES_ON;
+        if (t < nt || left <= 1) {
+            left = t < nt ? left : 0;    // (the one that is left is the next pair's beginning)
+            return;
+        }
+        --left;
         t = 0;
         from_start = true;
         if (++hb < a.HB) return;
@@ -223,7 +272,6 @@ __global__ __launch_bounds__(ONE ? 256 : 64, DH == 256 ? 1 : 2) void k_kvq_decod
     constexpr uint32_t HALFB = WK * DH, STAGEB = 2 * HALFB, IDB = 256, WAVEB = kvq_wave_bytes(DH);
     constexpr int PERTILE = 2 * NL + 2;                          // loads of a tile: keys, scales, table entries for NST tiles later, values
     constexpr int BEHIND_K = (NST - 1) * PERTILE + NL, BEHIND_V = (NST - 1) * PERTILE + NL + 2;
-    constexpr int NW = ONE ? WAVES : 1;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     __shared__ float ml_s[ONE ? WAVES * 16 * 2 : 1], fin[ONE ? 16 * 2 : 1];
     const DecodeArgs &a = k.d;
@@ -248,41 +296,40 @@ __global__ __launch_bounds__(ONE ? 256 : 64, DH == 256 ? 1 : 2) void k_kvq_decod
 
     // ---- the run
     Walk walk{a, 0, 0, 0, 0, 0, 0, 0, 0, true};
-    int cnt = 0;                                            // tiles of this wavefront
-    uint32_t nt_one = 0;
+    uint32_t tile_one = (uint32_t)wave;
     if (ONE) {
         walk.b = (int)blockIdx.x / a.HB;
         walk.hb = (int)blockIdx.x - walk.b * a.HB;
         walk.len = (int)uniform((uint32_t)a.c.length(walk.b, walk.hb == 0 && threadIdx.x == 0));
-        nt_one = tiles_of<WK>(walk.len);
-        cnt = ((int)nt_one - wave + NW - 1) / NW;           // tiles wave, wave + NW ..
-    } else {
-        TileList<WK> list;
-        uint32_t begin = 0;
-        if (!list.find(a, blockIdx.x, walk.b, walk.len, begin)) return;
-        const uint32_t f = blockIdx.x * list.per, in = f - begin;
         walk.nt = tiles_of<WK>(walk.len);
-        walk.hb = (int)(in / walk.nt);
-        walk.t = in - (uint32_t)walk.hb * walk.nt;
-        walk.left = min(list.per, list.total - f);
+    } else {
+        PlaceList list;
+        uint32_t begin = 0, f = 0;
+        if (!list.find(a, blockIdx.x, walk.b, walk.len, begin, f, walk.left)) return;
+        const uint32_t in = f - begin, places = PlaceList::of(walk.len);
+        walk.nt = tiles_of<WK>(walk.len);
+        walk.hb = (int)uniform(in / places);
+        walk.t = in - (uint32_t)walk.hb * places;
+        if (walk.t == 0) --walk.left;                       // the pair's beginning
+        else --walk.t;
         walk.from_start = walk.t == 0;
+        if (walk.left == 0) return;
         walk.lens_b = walk.b - 64;                          // (nothing there yet)
         (void)walk.length(walk.b);
-        cnt = (int)walk.left;
     }
-    int tile_one = wave;
     auto next_place = [&](Place &p) {
         if (!ONE) return walk.next(p);
-        p = Place{walk.b, walk.hb, walk.len, min(tile_one, (int)nt_one - 1) * WK, 0};
-        tile_one += NW;
+        p = Place{walk.b, walk.hb, walk.len, (int)min(tile_one, walk.nt - 1) * WK, tile_one < walk.nt ? GOES_ON : NO_TILE};
+        tile_one += WAVES;                                  // (tiles wave, wave + WAVES ..)
     };
+    const bool some = !ONE || tile_one < walk.nt;           // whether there is a tile at all
 
     Place ahead[NST] = {}, cur[NST] = {};                   // of the tiles whose table entries are, whose rows are on their way
     auto fetch_ids = [&](int st) {
         next_place(ahead[st]);
         const Place &p = ahead[st];
         const int s = min(p.key0 + key_p, p.len - 1);       // in the order of rows, lanes 32 .. 63 as lanes 0 .. 31
-        lds_gather4(ids0 + (uint32_t)st * IDB, (uint64_t)(uintptr_t)(a.c.table + (int64_t)p.b * a.c.max_pages + a.c.page((uint32_t)s)));
+        lds_gather4(uniform(ids0 + (uint32_t)st * IDB), (uint64_t)(uintptr_t)(a.c.table + (int64_t)p.b * a.c.max_pages + a.c.page((uint32_t)s)));
     };
     uint32_t row[NL];                                       // rows of the pool that this lane reads of the tile that is being fetched
     uint64_t scale_at = 0;                                  // and the scale that it brings
@@ -314,10 +361,10 @@ __global__ __launch_bounds__(ONE ? 256 : 64, DH == 256 ? 1 : 2) void k_kvq_decod
             const int piece = (lane % PIECES) ^ swz(RPI * j + grp);
             const bool in = (int)row[j] >= 0 && (!PAD || 16 * piece < dh);
             const uint64_t from = in ? (uint64_t)(uintptr_t)pool + (uint64_t)row[j] * (uint32_t)dh + 16 * piece : zeros + 16 * piece;
-            lds_gather16<!PAD>(at + j * 1024, from);
+            lds_gather16<!PAD>(uniform(at + j * 1024), from);
         }
     };
-    if (cnt > 0) {
+    if (some) {
 #pragma unroll
         for (int st = 0; st < NST; ++st) fetch_ids(st);
     }
@@ -361,30 +408,33 @@ __global__ __launch_bounds__(ONE ? 256 : 64, DH == 256 ? 1 : 2) void k_kvq_decod
     uint32_t ok[NST], any = 0;                              // rows of the tiles that count; whether any did
 #pragma unroll
     for (int d = 0; d < NDB; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (cnt > 0) {
+#pragma unroll
+    for (int st = 0; st < NST; ++st) {
+        ok[st] = 0;
+        cur[st].ends = NO_TILE;
+    }
+    if (some) {
         wait_loads<0>();
 #pragma unroll
         for (int st = 0; st < NST; ++st) {
-            ok[st] = 0;
-            if (st < cnt) {
+            if (ahead[st].ends != NO_TILE) {
                 ok[st] = find_rows(st);
                 fetch(a.c.k, lds0 + st * STAGEB);
-                lds_gather4(scales0 + st * IDB, scale_at);
+                lds_gather4(uniform(scales0 + st * IDB), scale_at);
                 fetch_ids(st);
                 fetch(a.c.v, lds0 + st * STAGEB + HALFB);
             }
         }
     }
-    for (int i0 = 0; i0 < cnt; i0 += NST)
+    while (cur[0].ends != NO_TILE)
 #pragma unroll
         for (int st = 0; st < NST; ++st) {
-            const int i = i0 + st;
-            if (i >= cnt) break;
+            if (cur[st].ends == NO_TILE) break;
             const uint32_t kb = lds0 + st * STAGEB, vb = kb + HALFB, sb = scales0 + st * IDB, count = ok[st];
             const Place at = cur[st];
-            const bool next = i + NST < cnt;
+            const bool next = ahead[st].ends != NO_TILE;         // the tile that takes this one's place
             any |= count;
-            if (i + NST <= cnt) wait_loads<BEHIND_K>();
+            if (cur[(st + NST - 1) % NST].ends != NO_TILE) wait_loads<BEHIND_K>();
             else wait_loads<0>();
             f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
@@ -418,9 +468,9 @@ __global__ __launch_bounds__(ONE ? 256 : 64, DH == 256 ? 1 : 2) void k_kvq_decod
             if (next) {
                 ok[st] = find_rows(st);
                 fetch(a.c.k, kb);
-                lds_gather4(sb, scale_at);
+                lds_gather4(uniform(sb), scale_at);
                 fetch_ids(st);
-            }
+            } else cur[st].ends = NO_TILE;
             // A weight (times its value's scale) as the sum of two or three bf16 numbers: one alone (2^-8) would double the rounding of a
             // bf16 result.
             Frag w[WP];
@@ -459,12 +509,12 @@ __global__ __launch_bounds__(ONE ? 256 : 64, DH == 256 ? 1 : 2) void k_kvq_decod
                 for (int i = WP - 1; i >= 0; --i) acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, w[i].v, acc[d], 0, 0, 0);
             }
             if (next) fetch(a.c.v, vb);
-            if (ONE || !at.ends) continue;
+            if (ONE || at.ends == GOES_ON) continue;
             // ---- the pair, or the run's part of it, ends: a lane has 4 dims of every 16 of one head
             const int h = a.rtiles == 1 ? at.hb : at.hb / a.rtiles, r0 = (at.hb - h * a.rtiles) * 16, rows = min(16, a.G - r0);
             const float l = over_lanes<4>(lsum, add), m = max_of_keys(mref, any != 0);
             if (n16 < rows) {
-                if (at.ends == 2) {
+                if (at.ends == PAIR_ENDS) {
                     const float inv = inverse_sum(m, l);
                     T *out = (T *)a.out + ((int64_t)at.b * a.H + h * a.G + r0 + n16) * dh;
 #pragma unroll
@@ -485,7 +535,7 @@ __global__ __launch_bounds__(ONE ? 256 : 64, DH == 256 ? 1 : 2) void k_kvq_decod
                     }
                 }
             }
-            if (i + 1 >= cnt) return;
+            if (cur[(st + 1) % NST].ends == NO_TILE) return;
 #pragma unroll
             for (int d = 0; d < NDB; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
             mref = -INFINITY;
@@ -508,6 +558,108 @@ __global__ __launch_bounds__(ONE ? 256 : 64, DH == 256 ? 1 : 2) void k_kvq_decod
         }
     }
     finish<T, PAD ? 0 : DH>(a, walk.b, walk.len, walk.hb, true, 0, (const float *)smem, WAVEB / 4, ml_s, fin);
+}
+
+// ---------------------------------------------------------------- the second launch
+// A workgroup joins the partial results of one or more query heads of a pair: as many as leave 512 workgroups, where there are so many pairs.
+// Us, a workgroup a head against one a pair: 512 pairs of 4 heads, five parts each, 8.4 and 4.8; 64 pairs of 8 heads, 32 parts, 5.2 and 9.0.
+constexpr int JT = 512;
+template <typename T>
+__global__ __launch_bounds__(JT) void k_kvq_join(DecodeArgs a, int per, int chunks)      // heads of a workgroup; such workgroups of a pair
+{
+    __shared__ __attribute__((aligned(16))) float part[4 * JT];
+    __shared__ float m_s[16], inv_s[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, dh = a.c.dh;
+    const int pair = (int)blockIdx.x / chunks, first = ((int)blockIdx.x - pair * chunks) * per;          // of the tile's heads
+    const int b = pair / a.HB, hb = pair - b * a.HB, h = hb / a.rtiles, t0 = (hb - h * a.rtiles) * 16, r0 = t0 + first, rows = min(per, min(16, a.G - t0) - first);
+    if (rows <= 0) return;
+    uint32_t all = 0, before = 0;
+    for (int b0 = 0; b0 < a.c.B; b0 += 64) {
+        const uint32_t upto = wave_scan(b0 + lane < a.c.B ? PlaceList::of(a.c.length(b0 + lane, false)) : 0u);
+        if (b > b0) before = all + from_lane(upto, min(b - b0, 64) - 1);
+        all += from_lane(upto, 63);
+    }
+    const PlaceList list{all * (uint32_t)a.HB};
+    const int len = a.c.length(b, hb + first == 0 && tid == 0);
+    const uint32_t nt = tiles_of<WK>(len);
+    T *const out = (T *)a.out + ((int64_t)b * a.H + h * a.G + r0) * dh;
+    if (nt == 0) {
+        for (int i = tid; i < rows * dh; i += JT) st(out + i, 0.f);
+        if (tid == 0) a.c.flag(MOA_DEV_EMPTY_KEYS);
+        return;
+    }
+    // the runs that its tiles are in, and the first one's place among the partial results
+    const uint32_t f0 = before * (uint32_t)a.HB + (uint32_t)hb * (nt + 1) + 1, w0 = list.run_of(a, f0), ns = list.run_of(a, f0 + nt - 1) - w0 + 1;
+    if (ns == 1) return;                                         // the first launch had all of it
+    const int64_t slot0 = (int64_t)w0 + (int64_t)b * a.HB + hb;
+    const float *ml = a.part_ml + (slot0 * a.HG + first) * 2, *po = a.part_o + (slot0 * a.HG + first) * dh;
+    // a group of E threads adds up every so many-th of them, four elements a thread; the first ones are loaded while the sums are unknown
+    const uint32_t E = (uint32_t)(rows * dh) / 4, groups = E < JT ? JT / E : 1, step = groups;
+    const uint32_t g = (uint32_t)tid / E;
+    constexpr int U = 4;
+    const bool on = g < groups;
+    uint32_t c = (uint32_t)tid - g * E;
+    auto load = [&](uint32_t s) { return on && c < E && s < ns ? *(const f32x4 *)(po + (int64_t)s * a.HG * dh + 4 * c) : f32x4{0.f, 0.f, 0.f, 0.f}; };
+    f32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = load(g + u * step);
+    for (int r = wave; r < rows; r += JT / 64) {
+        float m = -INFINITY, l = 0.f;
+        for (uint32_t s = lane; s < ns; s += 64) m = fmaxf(m, ml[(s * a.HG + r) * 2]);
+        m = over_lanes<0>(m, fmaxf);
+        const float ms = m == -INFINITY ? 0.f : m;
+        for (uint32_t s = lane; s < ns; s += 64) l += ml[(s * a.HG + r) * 2 + 1] * fast_exp2(ml[(s * a.HG + r) * 2] - ms);
+        l = over_lanes<0>(l, add);
+        if (lane == 0) {
+            if (m == -INFINITY && l == 0.f) a.c.flag(MOA_DEV_EMPTY_KEYS);
+            m_s[r] = ms;
+            inv_s[r] = inverse_sum(m, l);
+        }
+    }
+    __syncthreads();
+    for (;;) {                                                   // (more than once where a pair has more than 4 JT elements)
+        const int r = min((int)(4 * c) / dh, rows - 1);
+        const float ms = m_s[r];
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        for (uint32_t s = g; s < ns; s += U * step) {
+            f32x4 y[U];
+            float w[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t su = s + u * step;
+                w[u] = su < ns ? fast_exp2(ml[(su * a.HG + r) * 2] - ms) : 0.f;
+                y[u] = x[u];
+                x[u] = load(su + U * step);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = fmaf(y[u][i], w[u], o[i]);
+        }
+        if (groups > 1) {
+            *(f32x4 *)(part + 4 * tid) = o;
+            __syncthreads();
+            if ((uint32_t)tid >= E) return;
+            for (uint32_t k = 1; k < groups; ++k) {
+                const f32x4 y = *(const f32x4 *)(part + 4 * (k * E + tid));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] += y[i];
+            }
+        }
+        if (on && c < E) {
+            const float inv = inv_s[r];
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) out[4 * c + i] = o[i] * inv;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) st(out + 4 * c + i, o[i] * inv);
+            }
+        }
+        if (groups > 1 || (c += JT) >= E) return;
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = load(g + u * step);
+    }
 }
 
 // ---------------------------------------------------------------- host
@@ -553,7 +705,12 @@ hipError_t launch_decode(const KvqDecodeArgs &k, bool mfma, hipStream_t st)
     if (mfma) e = a.c.dh <= 64 ? launch_mfma<T, 64>(k, st) : a.c.dh <= 128 ? launch_mfma<T, 128>(k, st) : launch_mfma<T, 256>(k, st);
     else e = a.c.dh <= 64 ? launch_elements<T, 16>(k, grid, st) : a.c.dh <= 128 ? launch_elements<T, 32>(k, grid, st) : launch_elements<T, 64>(k, grid, st);
     if (e != hipSuccess || !a.runs) return e;
-    return launch_decode_join(a, sizeof(T) == 2, mfma ? WK : TK, st);
+    if (!mfma) return launch_decode_join(a, sizeof(T) == 2, st);
+    prof_begin(K_KVQ_JOIN, st);
+    const int pairs = a.c.B * a.HB, heads = (int)((int64_t)pairs * a.HG / 512), per = heads < 1 ? 1 : heads < a.HG ? heads : a.HG, chunks = (a.HG + per - 1) / per;
+    MOA_KLAUNCH(k_kvq_join<T>, dim3(pairs * chunks), dim3(JT), 0, st, a, per, chunks);
+    prof_end(st);
+    return hipGetLastError();
 }
 
 // whether the matrix cores' form takes such a cache (and queries q, which it also reads 16 bytes at a time)
