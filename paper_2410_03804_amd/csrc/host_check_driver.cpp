@@ -122,6 +122,53 @@ static void kv_cache()
     EXPECT(moa_kv_append(nullptr, fake(12), fake(13), 1, nullptr, nullptr, nullptr, nullptr) == MOA_ERR_NULL);
 }
 
+// the cache held in 8 bits, pages, norm and rotation: as above
+static void kvq_cache()
+{
+    moa_kvq_cache_t c = {MOA_BF16, 8, 128, 4, 1000, 16, 100, fake(1), fake(2), (float *)fake(3), (float *)fake(4), (const int32_t *)fake(5), (int32_t *)fake(6)};
+    auto launched = [](int32_t rc) { return rc == MOA_ERR_HIP || rc == MOA_OK; };
+    size_t n = 0;
+    for (const int dtype : {MOA_BF16, MOA_F32})
+        for (const int dh : {1, 33, 64, 80, 128, 256})
+            for (const int page : {1, 7, 16, 4096}) {
+                moa_kvq_cache_t d = c;
+                d.dtype = dtype;
+                d.head_dim = dh;
+                d.page_size = page;
+                for (const int H : {8, 16, 32, 64, 160}) {
+                    EXPECT(moa_kvq_decode_attn_workspace_bytes(&d, H, &n) == MOA_OK);
+                    EXPECT(launched(moa_kvq_decode_attn(&d, H, fake(8), fake(9), (int32_t *)fake(10), n ? fake(11) : nullptr, n, nullptr)));
+                    if (n) EXPECT(moa_kvq_decode_attn(&d, H, fake(8), fake(9), nullptr, fake(11), n - 1, nullptr) == MOA_ERR_WORKSPACE);
+                }
+                for (const int M : {1, 5, 60, 5000}) {
+                    EXPECT(launched(moa_kvq_append(&d, fake(12), fake(13), M, nullptr, nullptr, nullptr, nullptr)));
+                    EXPECT(launched(moa_kvq_append_rows(&d, fake(12), 8 * dh, fake(13), 24 * dh, M, (const int32_t *)fake(14), nullptr, nullptr, nullptr)));
+                    EXPECT(launched(moa_kvq_read(&d, M, fake(12), fake(13), nullptr, nullptr)));
+                }
+                for (const int rot : {0, dh / 2 * 2, dh / 4 * 2})
+                    for (const int T : {1, 3, 5000}) {
+                        EXPECT(launched(moa_qk_norm_rope(dtype, fake(1), 24 * dh, 16, fake(2), 24 * dh, 4, T, dh, fake(3), nullptr, 1e-6f, (const int32_t *)fake(4), 1e4f, rot,
+                                                         fake(5), 16 * dh, fake(6), 4 * dh, nullptr)));
+                        EXPECT(launched(moa_qk_norm_rope(dtype, nullptr, 0, 0, fake(2), INT64_MAX / 8 / (T + 1), 4, T, dh, nullptr, nullptr, 0.f, (const int32_t *)fake(4), 1e4f, rot,
+                                                         nullptr, 0, fake(6), 4 * dh, nullptr)));
+                    }
+            }
+    EXPECT(moa_kvq_append_rows(&c, fake(12), INT64_MAX, fake(13), 1024, 5, (const int32_t *)fake(14), nullptr, nullptr, nullptr) == MOA_ERR_SHAPE);
+    EXPECT(moa_kvq_append_rows(&c, fake(12), INT64_MIN, fake(13), 1024, 5, (const int32_t *)fake(14), nullptr, nullptr, nullptr) == MOA_ERR_SHAPE);
+    c.n_pages = INT32_MAX;
+    EXPECT(moa_kvq_read(&c, 5, fake(12), fake(13), nullptr, nullptr) == MOA_ERR_SHAPE);
+    int32_t *p = (int32_t *)fake(1);
+    for (const int B : {1, 1024, 1025, 1 << 20})
+        for (const int T : {0, 1, 8192, 8193, 1 << 21}) {
+            EXPECT(launched(moa_kv_reserve(B, 1000, 16, 100, p, p, nullptr, p, p, p, T, p, p, p, p, nullptr, nullptr)));
+            EXPECT(launched(moa_kv_release(B, 1000, 16, 100, p, p, p, p, nullptr, nullptr)));
+        }
+    EXPECT(moa_kv_reserve(INT32_MAX, 1000, 16, 100, p, p, nullptr, p, p, p, 1, p, p, p, p, nullptr, nullptr) == MOA_ERR_SHAPE);
+    EXPECT(moa_kv_reserve(4, INT32_MAX, INT32_MAX, 1, p, p, nullptr, p, p, p, 1, p, p, p, p, nullptr, nullptr) == MOA_ERR_SHAPE);
+    EXPECT(moa_kv_release(1 << 20, 1000, 1, 1 << 30, p, p, p, p, nullptr, nullptr) == MOA_ERR_SHAPE);
+    EXPECT(moa_qk_norm_rope(MOA_F32, fake(1), INT64_MAX, 1, nullptr, 0, 0, 5, 64, nullptr, nullptr, 0.f, p, 1e4f, 64, fake(2), 64, nullptr, 0, nullptr) == MOA_ERR_SHAPE);
+}
+
 // a whole step with fake device pointers: the checks-only pass over every stage, under each schedule and regime
 static void whole_step(int dtype, int B, int M, int P_cap, int64_t T_lsa, int layers, int schedule, bool with_sa, bool folded, bool packed,
                        bool tiny_ws)
@@ -198,6 +245,7 @@ int main()
     workspace_and_shapes();
     single_entry_points();
     kv_cache();
+    kvq_cache();
     for (int schedule = MOA_SCHED_GROUPED; schedule <= MOA_SCHED_SEQUENTIAL; ++schedule) {
         whole_step(MOA_BF16, 1, 60, 1084, 60, 1, schedule, false, true, true, false);       // the headline step
         whole_step(MOA_BF16, 1, 60, 1084, 60, 3, schedule, true, false, false, false);      // Self-Attention layer in front, more layers
