@@ -407,7 +407,7 @@ int32_t moa_kv_release(int32_t B, int32_t n_pages, int32_t page_size, int32_t ma
  *   pairs (c, c + rot_dim/2), c < rot_dim/2, are rotated by pos[t] * rope_theta^(-2c/rot_dim); dims from rot_dim on are y.
  * rot_dim = 0: the norm alone.  In single precision, the angle in double, rounded once.  q_out may be q with the same stride, k_out k; other
  * overlaps are not allowed.  0 heads: q (or k) is not looked at.  T = 0 is a no-op.  MOA_ERR_SHAPE: head_dim outside [1, 256], rot_dim odd or beyond
- * head_dim, strides smaller than the heads take, T > 2^24. */
+ * head_dim, strides smaller than the heads take, T > 2^23.  Squares are summed in single precision (elements up to 1e18). */
 int32_t moa_qk_norm_rope(int32_t dtype, const void *q, int64_t q_stride, int32_t n_q_heads, const void *k, int64_t k_stride,
                          int32_t n_kv_heads, int64_t T, int32_t head_dim, const void *gq, const void *gk, float rms_eps,
                          const int32_t *pos /*[T]*/, float rope_theta, int32_t rot_dim, void *q_out, int64_t q_out_stride,
@@ -419,7 +419,8 @@ int32_t moa_qk_norm_rope(int32_t dtype, const void *q, int64_t q_stride, int32_t
  *   k, v             [n_pages, Hkv, page_size, dh] codes;
  *   k_scale, v_scale [n_pages, Hkv, ceil(page_size / MOA_KVQ_BLOCK)] fp32, positive and finite; of blocks that hold no row they do not matter;
  *   table, len       as in moa_kv_cache_t; `dtype` is that of the rows given, of queries and of results.
- * Limits as there.  No accounts, and so no eviction by them.
+ * Limits as there, and M (or T) <= 2^24, times n_kv_heads <= 2^29, for the append, P_cap * head_dim < 2^31 for the read, B * n_q_heads * ceil(cap / 32)
+ * <= 2^30 for the attention.  No accounts, and so no eviction by them.
  *
  * moa_kvq_append puts rows into the cache as moa_kv_append does (k_new, v_new [B, Hkv, M, dh], path, n_new; len grows).  moa_kvq_append_rows takes them
  *   packed: row tok_off[b] + i of T, heads behind each other, k_stride (v_stride) elements from row to row, for i < tok_off[b + 1] - tok_off[b], or

@@ -638,29 +638,31 @@ def qk_norm_rope(q, k, q_out, k_out, pos, rope_theta=10000.0, rot_dim=None, gq=N
     if some is None:
         raise ValueError("q and k: one of them must be given")
     i, st = _device_of(some, stream)
-    T, _, dh = some.shape
-    dt = some.dtype
+    T, dt, dh = some.shape[0], some.dtype, some.shape[-1]
     if dt not in (torch.float32, torch.bfloat16):
         raise ValueError(f"q: dtype {dt}, expected float32 or bfloat16")
-    if q is not None and k is not None and k.shape[0] != T:
-        raise ValueError("q and k: must have the same number of rows")
-    at = []
-    for x, y, names in ((q, q_out, ("q", "q_out")), (k, k_out, ("k", "k_out"))):
-        if x is None:
-            at.append((None, 0, 0, None, 0))
-            continue
-        heads = x.shape[1]
-        xp, xs = _rows_on(x, dt, heads, dh, names[0], i)
-        if y is None or y.shape != x.shape:
-            raise ValueError(f"{names[1]}: must be as {names[0]}")
-        yp, ys = _rows_on(y, dt, heads, dh, names[1], i)
-        at.append((xp, xs, _int32(heads, "heads"), yp, ys))
-    (qp, qs, H, qop, qos), (kp, ks, Hkv, kop, kos) = at
-    rot = dh if rot_dim is None else _int32(rot_dim, "rot_dim")
+    qp, qs, H, qop, qos = _heads_in_and_out(q, q_out, T, dt, dh, "q", i)
+    kp, ks, Hkv, kop, kos = _heads_in_and_out(k, k_out, T, dt, dh, "k", i)
     rc = _lib.moa_qk_norm_rope(F32 if dt == torch.float32 else BF16, qp, qs, H, kp, ks, Hkv, T, _int32(dh, "dh"), _dev_on(gq, dt, dh, "gq", i),
-                               _dev_on(gk, dt, dh, "gk", i), float(rms_eps), _dev_on(pos, torch.int32, T, "pos", i), float(rope_theta), rot, qop, qos, kop, kos, st)
+                               _dev_on(gk, dt, dh, "gk", i), rms_eps, _dev_on(pos, torch.int32, T, "pos", i), rope_theta,
+                               dh if rot_dim is None else _int32(rot_dim, "rot_dim"), qop, qos, kop, kos, st)
     if rc:
         _check(rc)
+
+
+def _heads_in_and_out(x, y, T, dtype, dh, name, at):
+    """(address, row stride, heads, address, row stride) of x [T, heads, dh] and of what it becomes."""
+    if x is None:
+        return None, 0, 0, None, 0
+    shape = x.shape
+    if len(shape) != 3 or shape[0] != T:
+        raise ValueError("q and k: must be [T, heads, dh] with the same number of rows")
+    heads = shape[1]
+    xp, xs = _rows_on(x, dtype, heads, dh, name, at)
+    if y is None or y.shape != shape:
+        raise ValueError(f"{name}_out: must be as {name}")
+    yp, ys = _rows_on(y, dtype, heads, dh, name + "_out", at)
+    return xp, xs, _int32(heads, "heads"), yp, ys
 
 
 class QuantKVCache:

@@ -371,7 +371,8 @@ int32_t moa_kvq_append(const moa_kvq_cache_t *cache, const void *k_new, const vo
 {
     const int32_t rc = check_append(cache, k_new, v_new, "kvq_append");
     if (rc) return rc;
-    if (M < 1 || M > (1 << 24) || (int64_t)M * cache->head_dim > INT32_MAX) return api_fail(MOA_ERR_SHAPE, "kvq_append: M outside [1, 2^24], or M * head_dim above 2^31 - 1");
+    if (M < 1 || M > (1 << 24) || (int64_t)M * cache->head_dim > INT32_MAX || (int64_t)M * cache->n_kv_heads > (1 << 29))
+        return api_fail(MOA_ERR_SHAPE, "kvq_append: M outside [1, 2^24], M * head_dim above 2^31 - 1, or M * n_kv_heads above 2^29");
     const int64_t dh = cache->head_dim;
     KvqAppendArgs a = {KvqDev(*cache, dev_status), (const char *)k_new, (const char *)v_new, cache->n_kv_heads * M * dh, M * dh, dh, dh, M, path, n_new, nullptr, FastDiv(1)};
     return append(a, 0, (hipStream_t)stream, cache->dtype);
@@ -385,7 +386,8 @@ int32_t moa_kvq_append_rows(const moa_kvq_cache_t *cache, const void *k_new, int
     if (rc) return rc;
     if (!tok_off) return api_fail(MOA_ERR_NULL, "kvq_append_rows: tok_off is NULL");
     const int64_t dh = cache->head_dim, width = cache->n_kv_heads * dh;
-    if (T < 0 || T > (1 << 24)) return api_fail(MOA_ERR_SHAPE, "kvq_append_rows: T outside [0, 2^24]");
+    if (T < 0 || T > (1 << 24) || (int64_t)T * cache->n_kv_heads > (1 << 29))
+        return api_fail(MOA_ERR_SHAPE, "kvq_append_rows: T outside [0, 2^24], or T * n_kv_heads above 2^29");
     if (k_stride < width || v_stride < width) return api_fail(MOA_ERR_SHAPE, "kvq_append_rows: rows closer to each other than n_kv_heads * head_dim elements");
     if (k_stride > INT64_MAX / 8 / (T + 1) || v_stride > INT64_MAX / 8 / (T + 1)) return api_fail(MOA_ERR_SHAPE, "kvq_append_rows: strides beyond the address space");
     KvqAppendArgs a = {KvqDev(*cache, dev_status), (const char *)k_new, (const char *)v_new, 0, dh, k_stride, v_stride, T, nullptr, n_new, tok_off, FastDiv(1)};

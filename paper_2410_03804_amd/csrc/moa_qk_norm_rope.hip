@@ -247,8 +247,8 @@ int32_t moa_qk_norm_rope(int32_t dtype, const void *q, int64_t q_stride, int32_t
                          void *q_out, int64_t q_out_stride, void *k_out, int64_t k_out_stride, void *stream)
 {
     if (dtype != MOA_F32 && dtype != MOA_BF16) return api_fail(MOA_ERR_DTYPE, "qk_norm_rope: dtype is neither MOA_F32 nor MOA_BF16");
-    if (head_dim < 1 || head_dim > 256 || n_q_heads < 0 || n_kv_heads < 0 || n_q_heads > (1 << 20) || n_kv_heads > (1 << 20) || T < 0 || T > (1 << 24))
-        return api_fail(MOA_ERR_SHAPE, "qk_norm_rope: dimensions (1 <= head_dim <= 256, heads within 2^20, T within 2^24)");
+    if (head_dim < 1 || head_dim > 256 || n_q_heads < 0 || n_kv_heads < 0 || n_q_heads > (1 << 20) || n_kv_heads > (1 << 20) || T < 0 || T > (1 << 23))
+        return api_fail(MOA_ERR_SHAPE, "qk_norm_rope: dimensions (1 <= head_dim <= 256, heads within 2^20, T within 2^23)");
     if (rot_dim < 0 || rot_dim > head_dim || rot_dim % 2) return api_fail(MOA_ERR_SHAPE, "qk_norm_rope: rot_dim must be even and at most head_dim");
     if (T == 0 || n_q_heads + n_kv_heads == 0) return MOA_OK;
     if ((n_q_heads && (!q || !q_out)) || (n_kv_heads && (!k || !k_out))) return api_fail(MOA_ERR_NULL, "qk_norm_rope: q / k / q_out / k_out is NULL");

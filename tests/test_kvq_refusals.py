@@ -63,6 +63,9 @@ def test_append_arguments():
     assert append(cache(), M=0) == SHAPE and append(cache(), M=(1 << 24) + 1) == SHAPE and append(cache(head_dim=256), M=1 << 24) == SHAPE
     assert append(cache(), k=FAKE + 1) == SHAPE and append(cache(dtype=moa.F32), v=FAKE + 2) == SHAPE
     assert append(cache(B=70000, n_kv_heads=1)) == SHAPE
+    # blocks of all heads are counted in 32 bits
+    many = dict(n_kv_heads=256, head_dim=8, n_pages=4)
+    assert append(cache(**many), M=(1 << 21) + 1) == SHAPE and append_rows(cache(**many), T=(1 << 21) + 1, ks=2048, vs=2048) == SHAPE
     assert append_rows(cache(), k=None) == NULL and append_rows(cache(), off=None) == NULL
     assert append_rows(cache(), T=-1) == SHAPE and append_rows(cache(), T=(1 << 24) + 1) == SHAPE
     assert append_rows(cache(), ks=1023) == SHAPE and append_rows(cache(), vs=-1024) == SHAPE and append_rows(cache(), ks=1 << 60) == SHAPE
@@ -123,7 +126,7 @@ def rope(dtype=moa.BF16, H=32, Hkv=8, T=5, dh=128, theta=1e4, eps=1e-6, rot=128,
 
 def test_norm_and_rotation_arguments():
     assert rope(dtype=2) == DTYPE
-    for kw in (dict(dh=0, rot=0), dict(dh=257), dict(H=-1), dict(Hkv=-1), dict(T=-1), dict(T=(1 << 24) + 1), dict(H=(1 << 20) + 1), dict(rot=-2), dict(rot=130),
+    for kw in (dict(dh=0, rot=0), dict(dh=257), dict(H=-1), dict(Hkv=-1), dict(T=-1), dict(T=(1 << 23) + 1), dict(H=(1 << 20) + 1), dict(rot=-2), dict(rot=130),
                dict(rot=127), dict(qs=4095), dict(ks=1023), dict(qos=4095), dict(kos=0), dict(qs=1 << 61), dict(q=FAKE + 1), dict(ko=FAKE + 1),
                dict(gq=FAKE + 1), dict(pos=FAKE + 2), dict(dtype=moa.F32, k=FAKE + 2)):
         assert rope(**kw) == SHAPE, kw
