@@ -277,3 +277,15 @@ def test_pages_beyond_4_gib():
         assert np.array_equal(U.host(out)[0, h, 250:256], U.VALUES[U.encode(x[h, :6])])
         s = U.smallest_scale(x[h, 6:])
         assert np.array_equal(U.host(out)[0, h, 256:260], U.VALUES[U.encode(x[h, 6:] / s)] * s)
+    # and decoded over: the rows in front of these are zeros, so that weights and values are those of the last ten
+    q, got = torch.randn(1, Hkv, dh, device="cuda").to(torch.bfloat16), torch.zeros(1, Hkv, dh, dtype=torch.bfloat16, device="cuda")
+    moa.kvq_decode_attn(cache, q, got, U.workspace(moa.kvq_decode_attn_workspace_bytes(cache, Hkv)))
+    for h in (0, 63):
+        keys = U.host(out)[0, h, :260]
+        sc = keys @ U.host(q)[0, h] / 16.0
+        p = np.exp(sc - sc.max())
+        want = (p / p.sum()) @ U.host(other)[0, h, :260]
+        # (dh + 8) u of the largest score's sum, twice, 260 u and 2^-15 of the sum of p |v|; then rounded to bf16
+        eps = 2 * (dh + 8) * 2.0 ** -24 * np.max(np.abs(keys) @ np.abs(U.host(q)[0, h]) / 16.0) + 324 * 2.0 ** -24 + 2.0 ** -15
+        tol = 2.0 ** -8 * np.abs(want) + eps * ((p / p.sum()) @ np.abs(U.host(other)[0, h, :260]))
+        assert np.all(np.abs(U.host(got)[0, h] - want) <= tol)

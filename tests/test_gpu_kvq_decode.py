@@ -209,6 +209,28 @@ def test_on_another_stream_and_captured():
     assert c.status.item() == 0
 
 
+def test_two_graphs_share_a_workspace():
+    """Replayed one behind the other, on inputs of their own."""
+    cs = [U.QCache(B8, lens, 16, seed=20 + i) for i, lens in enumerate(([1500, 300], [900, 2100]))]
+    caches, qs = [c.moa() for c in cs], [queries(c) for c in cs]
+    ws = U.workspace(max(moa.kvq_decode_attn_workspace_bytes(c, 32) for c in caches))
+    outs = [torch.zeros_like(q) for q in qs]
+    graphs = [torch.cuda.CUDAGraph() for _ in cs]
+    for c, q, out, g in zip(caches, qs, outs, graphs):
+        with torch.cuda.graph(g):
+            moa.kvq_decode_attn(c, q, out, ws)
+    for step in range(3):
+        for q in qs:
+            q.mul_(1.25)
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for c, q, out in zip(cs, qs, outs):
+            want, tol = U.decode_reference(c, q)
+            U.check(out, want, tol, f"replay {step}")
+        ws.random_(0, 256)
+
+
 def test_random_calls():
     rng = np.random.default_rng(15)
     for i in range(25):
