@@ -388,10 +388,10 @@ int32_t moa_kv_evict(const moa_kv_cache_t *cache, int32_t budget, int32_t recent
  * moa_kv_release: entries behind the page of slot len[b] - 1 that name a page lose it (-1); the pages go back, so that the first of them by
  *   sequence and slot is the next one to be taken.  For a sequence that is done, set its len to 0 first; behind moa_kv_evict or a rejected draft
  *   it gives back what they left.  A page that several sequences share is for the caller to take out of all tables but one: *n_free never
- *   passes n_pages (what would is dropped, MOA_DEV_BAD_PAGE), but a page that is in the list twice is handed out twice.  The whole table is read, by
- *   one workgroup.
+ *   passes n_pages (what would is dropped, MOA_DEV_BAD_PAGE), but a page that is in the list twice is handed out twice.  The whole table
+ *   is read.
  * Calls on one list (or one table) are to be ordered by the caller, as by one stream.
- * Both are one launch of one workgroup; reserve writes pos and slot by a second one beyond 8192 rows or 1024 sequences.  Limits: B <= 2^20, T <=
+ * Both are one launch of one workgroup, beyond 1024 sequences or 8192 rows three (beyond 16384 table entries, two).  Limits: B <= 2^20, T <=
  * 2^21, max_pages * page_size <= 2^30, n_pages * page_size and B * max_pages < 2^31 (MOA_ERR_SHAPE). */
 int32_t moa_kv_reserve(int32_t B, int32_t n_pages, int32_t page_size, int32_t max_pages, const int32_t *len /*[B]*/,
                        const int32_t *n_new /*[B]*/, const int32_t *seen /*[B] or NULL*/, int32_t *table, int32_t *free_pages,

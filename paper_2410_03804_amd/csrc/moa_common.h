@@ -127,7 +127,7 @@ enum KernelId {
     K_RMSNORM, K_ROPE, K_SWIGLU, K_ADD_OUT, K_TREE_EXPAND, K_TREE_FINALIZE, K_TOPK_LOGPROB,
     K_LM_HEAD, K_LM_HEAD_REDUCE, K_TOPK_MERGE, K_MSG_TREE, K_MSG_ACCEPT, K_LSA_FUSED, K_LSA_FUSED_PK, K_LSA_PACK, K_LIN_F32_LATENCY, K_LIN_F32_TILE, K_ATTN_F32, K_LIN_BF16, K_ATTN_LONG, K_ATTN_FUSED16,
     K_KV_APPEND, K_KV_APPEND_LEN, K_KV_EVICT_SELECT, K_KV_EVICT_MOVE, K_DECODE_ATTN, K_DECODE_ATTN_MFMA, K_DECODE_JOIN,
-    K_KV_RESERVE, K_KV_SLOTS, K_KV_RELEASE, K_QK_NORM_ROPE, K_KVQ_APPEND, K_KVQ_APPEND_LEN, K_KVQ_READ, K_KVQ_DECODE, K_KVQ_DECODE_MFMA, K_KVQ_JOIN, K_COUNT
+    K_KV_RESERVE, K_KV_RESERVE_COUNT, K_KV_RESERVE_SUM, K_KV_RESERVE_WRITE, K_KV_RELEASE, K_KV_RELEASE_LIST, K_KV_RELEASE_TABLE, K_QK_NORM_ROPE, K_KVQ_APPEND, K_KVQ_APPEND_LEN, K_KVQ_READ, K_KVQ_DECODE, K_KVQ_DECODE_MFMA, K_KVQ_JOIN, K_COUNT
 };
 enum SiteId {
     S_NONE = 0, S_TREE_BUILD, S_LSA_QKV, S_LSA_ATTN, S_LSA_OPROJ, S_APPEND_KV, S_APPEND_LEN, S_CA_QPROJ, S_CA_CORE,

@@ -37,7 +37,7 @@ const char *const kKernelNames[K_COUNT] = {
     "k_linear_splitk_reduce", "k_scatter_copy", "k_attn_generic", "k_attn_mfma", "k_attn_merge", "k_lsa_attn", "k_lsa_attn_mfma", "k_step_small", "k_attn_fused", "k_probe_read", "k_probe_mfma",
     "k_rmsnorm", "k_rope", "k_swiglu", "k_add_out", "k_tree_expand", "k_tree_finalize", "k_topk_slices", "k_lm_head_argmax", "k_lm_head_reduce", "k_topk_merge", "k_msg_tree", "k_msg_accept", "k_lsa_fused", "k_lsa_fused_pk", "k_lsa_pack_weights", "k_linear_f32_latency", "k_linear_f32_tile", "k_attn_f32", "k_linear_bf16", "k_attn_long<128>", "k_attn_fused16<128, 8>",
     "k_kv_append", "k_kv_append_len", "k_kv_evict_select", "k_kv_evict_move", "k_decode_attn", "k_decode_attn_mfma", "k_decode_join",
-    "k_kv_reserve", "k_kv_slots", "k_kv_release", "k_qk_norm_rope", "k_kvq_append", "k_kvq_append_len", "k_kvq_read", "k_kvq_decode", "k_kvq_decode_mfma", "k_kvq_join"};
+    "k_kv_reserve", "k_kv_reserve_count", "k_kv_reserve_sum", "k_kv_reserve_write", "k_kv_release", "k_kv_release_list", "k_kv_release_table", "k_qk_norm_rope", "k_kvq_append", "k_kvq_append_len", "k_kvq_read", "k_kvq_decode", "k_kvq_decode_mfma", "k_kvq_join"};
 const char *const kSiteNames[S_COUNT] = {
     "none", "tree_build", "lsa.qkv_proj", "lsa.layer_attn", "lsa.o_proj", "ca_append.kv_proj", "ca_append.lengths",
     "ca.q_proj", "ca.core", "ca.o_proj", "verify.qkv_proj", "verify.core", "verify.o_proj", "tree_accept",

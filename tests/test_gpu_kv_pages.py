@@ -102,17 +102,19 @@ class Pages:
         self.t_len.copy_(i32(self.len))
 
 
+@pytest.mark.parametrize("pad", [0, 8192])
 @pytest.mark.parametrize("page", [1, 16, 40])
 @pytest.mark.parametrize("B", [1, 2, 63, 64, 300])
-def test_a_batch_s_life(B, page):
-    """Prompts, decoded tokens, drafts that are mostly rejected, sequences that end, until the pool runs out now and then."""
+def test_a_batch_s_life(B, page, pad):
+    """Prompts, decoded tokens, drafts that are mostly rejected, sequences that end, until the pool runs out now and then.  pad: rows of the
+    batch that no token comes to use; beyond 8192 rows it is several launches."""
     mp = -(-400 // page)
     s = Pages(B, max(8, B * mp // 3), page, mp, seed=B * 100 + page)
     rng = s.rng
     for step in range(12):
         n = rng.integers(0, 120, B) if step % 4 == 0 else np.ones(B, int) if step % 2 else rng.integers(0, 9, B)
         n = np.minimum(n, s.cap - s.len)
-        got = s.reserve(n, int(n.sum()) + int(rng.integers(0, 5)), seen=rng.integers(0, 10 ** 6, B) if step % 3 == 0 else None, alias=step % 5 == 2)
+        got = s.reserve(n, int(n.sum()) + pad + int(rng.integers(0, 5)), seen=rng.integers(0, 10 ** 6, B) if step % 3 == 0 else None, alias=step % 5 == 2)
         accepted = np.minimum(got, rng.integers(0, 5, B)) if step % 2 == 0 and step else np.asarray(got)
         s.grow(accepted)
         if step % 3 == 2:
@@ -125,23 +127,24 @@ def test_a_batch_s_life(B, page):
     assert len(set(s.stack)) == len(s.stack) and np.all(s.table == -1)
 
 
-@pytest.mark.parametrize("B,T", [(3000, 9000), (1025, 1025), (1024, 8192), (1024, 8193), (2500, 500), (7, 40000)])
+@pytest.mark.parametrize("B,T", [(3000, 9000), (1025, 1025), (1024, 8192), (1024, 8193), (2500, 500), (7, 40000), (1, 100000), (2100, 2000)])
 def test_many_sequences_and_many_rows(B, T):
     page = 16
-    s = Pages(B, 3 * B + T // page, page, 40 if B > 7 else 600, seed=T)
+    s = Pages(B, 3 * B + T // page, page, 40 if B > 7 else 600 if B > 1 else 7000, seed=T)
     n = s.rng.integers(0, 2 * T // B + 1, B)
     s.reserve(n, T)
     s.release()                                  # what was taken, back in its order
     s.reserve(n, T)
 
 
-def test_pages_run_out_in_order():
+@pytest.mark.parametrize("pad", [0, 9000])
+def test_pages_run_out_in_order(pad):
     s = Pages(6, 10, 16, 8, seed=1, free=4)
-    assert s.reserve([30, 16, 20, 0, 1, 0], 67) == [30, 16, 0, 0, 0, 0]      # 2 + 1; two are wanted, one is left; then who needs one waits too
+    assert s.reserve([30, 16, 20, 0, 1, 0], 67 + pad) == [30, 16, 0, 0, 0, 0]      # 2 + 1; two are wanted, one is left; then who needs one waits too
     s.grow([30, 16, 0, 0, 0, 0])
-    assert s.reserve([2, 1, 0, 0, 0, 0], 8) == [2, 1, 0, 0, 0, 0]            # the first has room in its page, the second takes the last one
+    assert s.reserve([2, 1, 0, 0, 0, 0], 8 + pad) == [2, 1, 0, 0, 0, 0]            # the first has room in its page, the second takes the last one
     s.grow([2, 1, 0, 0, 0, 0])
-    assert s.reserve([1, 15, 0, 0, 0, 0], 17) == [0, 15, 0, 0, 0, 0]         # none is left; who lacks none goes on
+    assert s.reserve([1, 15, 0, 0, 0, 0], 17 + pad) == [0, 15, 0, 0, 0, 0]         # none is left; who lacks none goes on
 
 
 def test_the_same_room_asked_for_twice_takes_no_more():
@@ -151,6 +154,48 @@ def test_the_same_room_asked_for_twice_takes_no_more():
     left = len(s.stack)
     s.reserve(n, 58)
     assert len(s.stack) == left
+
+
+def test_a_batch_too_small_for_a_prompt_of_a_large_one():
+    """Rows run out in the middle of a sequence whose pages were counted, and of more than one round of sequences."""
+    for alias in (False, True):
+        s = Pages(1500, 4000, 16, 9, seed=8)
+        n = s.rng.integers(0, 20, 1500)
+        n[1100] = 130
+        T = int(n[:1100].sum()) + 20
+        got = s.reserve(n, T, alias=alias)
+        assert got[1100] == 20 and not any(got[1101:])
+        s = Pages(3, 700, 16, 900, seed=9)
+        assert s.reserve([9000, 200, 5], 9100, alias=alias) == [9000, 100, 0]
+        s.release()
+        assert len(s.stack) == 700
+
+
+def test_numbers_outside_their_ranges_in_a_large_batch():
+    s = Pages(4, 50, 16, 4, seed=3)
+    s.reserve([-3, 70, 5, 2], 9000)
+    s.grow([-2, 100, 3, 0])
+    s.reserve([1, 1, 1, 1], 9000)
+    s.table[1, 0], s.table[2, 1] = 50, 10 ** 9
+    s.t_table.copy_(i32(s.table))
+    s.grow([2, -100, 0, 0])
+    s.reserve([5, 20, 20, 0], 9000)
+    big = Pages(40, 30, 16, 500, seed=4)                      # two launches of the release
+    big.table[3, 7], big.table[20, 499], big.table[20, 2] = 30, 10 ** 9, 17
+    big.stack.remove(17)
+    big.free[:29].copy_(i32(big.stack))
+    big.n_free.fill_(29)
+    big.t_table.copy_(i32(big.table))
+    big.grow([-4] + [0] * 39)
+    big.release(status=moa.DEV_BAD_PAGE | moa.DEV_BAD_LENGTH)
+    for claim, left in ((-7, 2), (31, 30), (30, 30)):
+        big.n_free.fill_(claim)
+        big.t_len.zero_()
+        big.t_table[5, 100:102] = i32([4, 9])
+        moa.kv_release(big.t_table, big.t_len, 16, big.free, big.n_free, dev_status=big.status)
+        assert big.n_free.item() == left and torch.all(big.t_table == -1)
+        assert big.status.item() == (moa.DEV_BAD_LENGTH if claim != 30 else 0) | (moa.DEV_BAD_PAGE if claim >= 30 else 0)
+        big.status.zero_()
 
 
 def test_numbers_outside_their_ranges():
