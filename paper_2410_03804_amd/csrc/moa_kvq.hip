@@ -229,7 +229,8 @@ __global__ __launch_bounds__(256) void k_kvq_append_len(KvqAppendArgs a)
 template <typename T, int VE, int IT>
 hipError_t launch_append(const KvqAppendArgs &a, hipStream_t st)
 {
-    const int64_t units = ((int64_t)a.M / BLK + 2) * a.c.c.Hkv * 2;
+    // blocks that the rows of a sequence can be in
+    const int64_t units = ((int64_t)a.M * (int)a.c.blocks.d / (int)a.c.c.page.d + 3) * a.c.c.Hkv * 2;
     const bool one = units <= 128;
     prof_begin(K_KVQ_APPEND, st);
     if (one) MOA_KLAUNCH((k_kvq_append<T, VE, IT, 1024, true>), dim3(1, 1, a.c.c.B), dim3(1024), 0, st, a);

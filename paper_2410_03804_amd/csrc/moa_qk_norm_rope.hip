@@ -96,13 +96,14 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope(RopeNormArgs a)
     }
 }
 
-// ---------------------------------------------------------------- rows in pieces of 16 bytes
+// ---------------------------------------------------------------- rows in pieces of W words of 4 bytes: 4, or 2 where the rotated pairs do not lie in pieces of 16 bytes
 // A head is spread over LPR lanes, two pieces each: the ones that are rotated against each other, so that no lane needs another's elements, or two
 // that pass.  A workgroup has TPB tokens, whose angles are one or two a thread.
-template <typename T, int LPR, int TPB>
+template <typename T, int W, int LPR, int TPB>
 __global__ __launch_bounds__(256) void k_qk_norm_rope_pieces(RopeNormArgs a)
 {
-    constexpr int VE = 16 / sizeof(T), U = 2;
+    typedef __attribute__((ext_vector_type(W))) uint32_t Piece;
+    constexpr int VE = 4 * W / sizeof(T), U = 2;
     __shared__ __attribute__((aligned(16))) float2 cs[TPB * 128];
     const int64_t t0 = (int64_t)blockIdx.x * TPB;
     const int tokens = (int)(a.T - t0 < TPB ? a.T - t0 : TPB), R = a.heads[0] + a.heads[1], n = tokens * R;
@@ -114,28 +115,28 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope_pieces(RopeNormArgs a)
         const int t = r / R, hh = r - t * R, w = hh >= a.heads[0], h = w ? hh - a.heads[0] : hh;
         return Row{(const T *)a.x[w] + (t0 + t) * a.ldx[w] + (int64_t)h * a.dh, (T *)a.y[w] + (t0 + t) * a.ldy[w] + (int64_t)h * a.dh, t, w};
     };
-    u32x4 x[U][2];
-    auto load = [&](int r, u32x4 (&v)[2]) {
-        v[0] = v[1] = u32x4{0u, 0u, 0u, 0u};
+    Piece x[U][2];
+    auto load = [&](int r, Piece (&v)[2]) {
+        v[0] = v[1] = Piece{};
         if (r >= n || !on) return;
         const T *p = row_of(r).x;
-        v[0] = *(const u32x4 *)(p + pa * VE);
-        v[1] = *(const u32x4 *)(p + (pa + step) * VE);
+        v[0] = *(const Piece *)(p + pa * VE);
+        v[1] = *(const Piece *)(p + (pa + step) * VE);
     };
-    auto value = [](const u32x4 &v, int e) {
+    auto value = [](const Piece &v, int e) {
         return sizeof(T) == 4 ? __uint_as_float(v[e]) : __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
     };
     constexpr int RP = 256 / LPR;                        // rows at a time
     const int first = threadIdx.x / LPR;
 #pragma unroll
     for (int u = 0; u < U; ++u) load(first + u * RP, x[u]);
-    u32x4 g[2][2];
+    Piece g[2][2];
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-        g[w][0] = g[w][1] = u32x4{0u, 0u, 0u, 0u};
+        g[w][0] = g[w][1] = Piece{};
         if (!a.g[w] || !on) continue;
-        g[w][0] = *(const u32x4 *)((const T *)a.g[w] + pa * VE);
-        g[w][1] = *(const u32x4 *)((const T *)a.g[w] + (pa + step) * VE);
+        g[w][0] = *(const Piece *)((const T *)a.g[w] + pa * VE);
+        g[w][1] = *(const Piece *)((const T *)a.g[w] + (pa + step) * VE);
     }
     if (a.half) {
         angles(a, t0, tokens, cs);
@@ -181,13 +182,13 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope_pieces(RopeNormArgs a)
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                u32x4 o;
+                Piece o;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
+                for (int e = 0; e < W; ++e) {
                     if constexpr (sizeof(T) == 4) o[e] = __float_as_uint(y[i][e]);
                     else o[e] = pack_bf16x2(y[i][2 * e], y[i][2 * e + 1]);
                 }
-                u32x4 *const to = (u32x4 *)(at.y + (pa + i * step) * VE);
+                Piece *const to = (Piece *)(at.y + (pa + i * step) * VE);
                 // (of many tokens no cache holds the results until they are read: 42.6 us without, 36.9 with, where reads said so too 38.8)
                 if constexpr (TPB > 1) __builtin_nontemporal_store(o, to);
                 else *to = o;
@@ -196,22 +197,22 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope_pieces(RopeNormArgs a)
     }
 }
 
-template <typename T, int LPR>
+template <typename T, int W, int LPR>
 hipError_t launch_pieces(const RopeNormArgs &a, hipStream_t st)
 {
     const bool many = a.T >= 2048;
     prof_begin(K_QK_NORM_ROPE, st);
-    if (many) MOA_KLAUNCH((k_qk_norm_rope_pieces<T, LPR, 4>), dim3((unsigned)((a.T + 3) / 4)), dim3(256), 0, st, a);
-    else MOA_KLAUNCH((k_qk_norm_rope_pieces<T, LPR, 1>), dim3((unsigned)a.T), dim3(256), 0, st, a);
+    if (many) MOA_KLAUNCH((k_qk_norm_rope_pieces<T, W, LPR, 4>), dim3((unsigned)((a.T + 3) / 4)), dim3(256), 0, st, a);
+    else MOA_KLAUNCH((k_qk_norm_rope_pieces<T, W, LPR, 1>), dim3((unsigned)a.T), dim3(256), 0, st, a);
     prof_end(st);
     return hipGetLastError();
 }
 
-// every address in 16 bytes, and pairs of pieces that are rotated or pass
-template <typename T>
+// every address in pieces of W words, and pairs of pieces that are rotated or pass
+template <typename T, int W>
 bool in_pieces(const RopeNormArgs &a)
 {
-    constexpr int VE = 16 / sizeof(T);
+    constexpr int VE = 4 * W / sizeof(T);
     uintptr_t bits = 0;
     int64_t elems = 0;
     for (int w = 0; w < 2; ++w)
@@ -219,16 +220,31 @@ bool in_pieces(const RopeNormArgs &a)
             bits |= (uintptr_t)a.x[w] | (uintptr_t)a.y[w] | (uintptr_t)a.g[w];
             elems |= a.ldx[w] | a.ldy[w];
         }
-    return a.dh % (2 * VE) == 0 && a.half % VE == 0 && !(bits & 15) && elems % VE == 0;
+    return a.dh % (2 * VE) == 0 && a.half % VE == 0 && !(bits & (4 * W - 1)) && elems % VE == 0;
+}
+
+template <typename T, int W>
+hipError_t launch_width(const RopeNormArgs &a, hipStream_t st)
+{
+    constexpr int MOST = 256 * sizeof(T) / (8 * W);      // pairs of pieces that a head can have
+    const int pairs = a.dh * (int)sizeof(T) / (8 * W);
+    if (pairs <= 4) return launch_pieces<T, W, 4>(a, st);
+    if (pairs <= 8) return launch_pieces<T, W, 8>(a, st);
+    if constexpr (MOST > 16)
+        if (pairs > 16) {
+            if constexpr (MOST > 32)
+                if (pairs > 32) return launch_pieces<T, W, 64>(a, st);
+            return launch_pieces<T, W, 32>(a, st);
+        }
+    return launch_pieces<T, W, 16>(a, st);
 }
 
 template <typename T>
 hipError_t launch(const RopeNormArgs &a, hipStream_t st)
 {
-    if (in_pieces<T>(a)) {
-        const int pairs = a.dh * (int)sizeof(T) / 32;
-        return pairs <= 4 ? launch_pieces<T, 4>(a, st) : pairs <= 8 ? launch_pieces<T, 8>(a, st) : pairs <= 16 ? launch_pieces<T, 16>(a, st) : launch_pieces<T, 32>(a, st);
-    }
+    if (in_pieces<T, 4>(a)) return launch_width<T, 4>(a, st);
+    // (16145 tokens of 8 heads of 80 dims, 40 of them rotated: 44 us in the kernel for any sizes)
+    if (in_pieces<T, 2>(a)) return launch_width<T, 2>(a, st);
     prof_begin(K_QK_NORM_ROPE, st);
     MOA_KLAUNCH(k_qk_norm_rope<T>, dim3((unsigned)a.T), dim3(256), 0, st, a);
     prof_end(st);

@@ -76,7 +76,8 @@ class Case:
 @pytest.mark.parametrize("norm", [True, False])
 @pytest.mark.parametrize("T", [1, 2, 3, 17, 260])
 @pytest.mark.parametrize("heads", [(4, 2, 64, "f32"), (32, 8, 128, "bf16"), (32, 4, 128, "bf16"), (6, 2, 80, "bf16"), (6, 2, 80, "f32"), (3, 1, 256, "bf16"),
-                                   (2, 1, 256, "f32"), (5, 1, 34, "bf16"), (7, 3, 16, "bf16"), (1, 1, 2, "f32"), (5, 2, 96, "f32"), (64, 8, 128, "f32")], ids=str)
+                                   (2, 1, 256, "f32"), (5, 1, 34, "bf16"), (7, 3, 16, "bf16"), (1, 1, 2, "f32"), (5, 2, 96, "f32"), (64, 8, 128, "f32"),
+                                   (3, 2, 72, "bf16"), (3, 2, 248, "bf16"), (3, 2, 20, "f32"), (3, 2, 252, "f32"), (3, 2, 8, "bf16")], ids=str)
 def test_sizes(heads, T, norm):
     Case(*heads, T, seed=T, norm=norm).run(what=f"{heads} {T}")
 
@@ -86,6 +87,13 @@ def test_sizes(heads, T, norm):
 def test_a_part_of_the_dims_is_rotated(dtype, rot):
     Case(8, 2, 128, dtype, 50, seed=rot).run(rot=rot, what=f"{dtype} {rot}")
     Case(8, 2, 128, dtype, 50, seed=rot, norm=False).run(rot=rot, what=f"{dtype} {rot} no norm")
+
+
+@pytest.mark.parametrize("heads,rot", [((6, 2, 80, "bf16"), 40), ((6, 2, 80, "bf16"), 8), ((6, 2, 80, "f32"), 20), ((6, 2, 80, "f32"), 36), ((3, 1, 256, "bf16"), 72), ((3, 1, 256, "f32"), 4),
+                                       ((3, 1, 64, "bf16"), 0), ((9, 2, 12, "f32"), 4)], ids=str)
+@pytest.mark.parametrize("T", [5, 2300])
+def test_parts_in_pieces_of_every_width(heads, rot, T):
+    Case(*heads, T, seed=rot).run(rot=rot, what=f"{heads} {rot}")
 
 
 @pytest.mark.parametrize("dh", [1, 3, 33, 129, 255])
