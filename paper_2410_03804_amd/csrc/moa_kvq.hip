@@ -231,7 +231,8 @@ hipError_t launch_append(const KvqAppendArgs &a, hipStream_t st)
 {
     // blocks that the rows of a sequence can be in
     const int64_t units = ((int64_t)a.M * (int)a.c.blocks.d / (int)a.c.c.page.d + 3) * a.c.c.Hkv * 2;
-    const bool one = units <= 128;
+    // A workgroup's round of 16 blocks is about 2.5 us, the other launch 4; of a path's nodes few are accepted.
+    const bool one = units <= (a.path ? 128 : 48);
     prof_begin(K_KVQ_APPEND, st);
     if (one) MOA_KLAUNCH((k_kvq_append<T, VE, IT, 1024, true>), dim3(1, 1, a.c.c.B), dim3(1024), 0, st, a);
     else {

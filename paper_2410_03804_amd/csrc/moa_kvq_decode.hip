@@ -169,19 +169,19 @@ typedef int i32x2 __attribute__((ext_vector_type(2)));
 
 // The list of all tiles of 32 keys of all pairs, dealt to the runs so that none has more than one more than another.  A pair takes up one more
 // place than it has tiles, since going on to it costs a wavefront up to a tile's time (its queries are waited for, its predecessor's result is
-// written): 64 ragged sequences up to 8192, some of which are short, 105 us without and 94 with.
+// written): 64 ragged sequences up to 8192, some of which are short, 105 us without and 94 with.  (At least two or four places a run: one
+// sequence of 1084 5.6 us without, 7.5 and 10; of 27000 with 2 KV heads 6.9, 10.8 and 14.4.)
 struct PlaceList {
-    uint32_t total;                      // places
+    uint32_t total, log2;                // places; runs that they are dealt to: a.runs, or as many as leave none without
     static __device__ __forceinline__ uint32_t of(int len) { return tiles_of<WK>(len) + (len > 0); }
-    // the first place of run w (of the one behind the last: total), and the run of place f; runs beyond the places have none
-    __device__ __forceinline__ uint32_t first(const DecodeArgs &a, uint32_t w) const
+    __device__ __forceinline__ void set(const DecodeArgs &a, uint32_t all)       // all: places of the sequences, for one KV head
     {
-        return total < (uint32_t)a.runs ? min(w, total) : (uint32_t)((uint64_t)w * total >> a.runs_log2);
+        total = all * (uint32_t)a.HB;
+        log2 = min((uint32_t)a.runs_log2, 31u - (uint32_t)__clz((int)max(total, 1u)));
     }
-    __device__ __forceinline__ uint32_t run_of(const DecodeArgs &a, uint32_t f) const
-    {
-        return total < (uint32_t)a.runs ? f : (uint32_t)((((uint64_t)(f + 1) << a.runs_log2) - 1) / total);
-    }
+    // the first place of run w (of the one behind the last: total), and the run of place f
+    __device__ __forceinline__ uint32_t first(uint32_t w) const { return (uint32_t)((uint64_t)w * total >> log2); }
+    __device__ __forceinline__ uint32_t run_of(uint32_t f) const { return (uint32_t)((((uint64_t)(f + 1) << log2) - 1) / total); }
     // the sequence that place f of run w's first is in, its length and its first place; false where the run has none
     __device__ __forceinline__ bool find(const DecodeArgs &a, uint32_t w, int &b, int &len, uint32_t &begin, uint32_t &f, uint32_t &n)
     {
@@ -189,10 +189,10 @@ struct PlaceList {
         int mine = lane < a.c.B ? a.c.length(lane, false) : 0;
         uint32_t upto = wave_scan(of(mine)), all = from_lane(upto, 63);
         for (int i = lane + 64; i < (a.c.B + 63) / 64 * 64; i += 64) all += from_lane(wave_scan(i < a.c.B ? of(a.c.length(i, false)) : 0u), 63);
-        total = all * (uint32_t)a.HB;
-        f = first(a, w);
-        n = first(a, w + 1) - f;
-        if (n == 0) return false;
+        set(a, all);
+        f = first(w);
+        n = first(w + 1) - f;
+        if (w >> log2 || n == 0) return false;
         uint32_t base = 0;
         for (int b0 = 0;; b0 += 64) {
             const uint64_t past = __ballot(f < (base + upto) * (uint32_t)a.HB);
@@ -568,7 +568,7 @@ template <typename T>
 __global__ __launch_bounds__(JT) void k_kvq_join(DecodeArgs a, int per, int chunks)      // heads of a workgroup; such workgroups of a pair
 {
     __shared__ __attribute__((aligned(16))) float part[4 * JT];
-    __shared__ float m_s[16], inv_s[16];
+    __shared__ float m_s[16], inv_s[16], parts_s[2][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, dh = a.c.dh;
     const int pair = (int)blockIdx.x / chunks, first = ((int)blockIdx.x - pair * chunks) * per;          // of the tile's heads
     const int b = pair / a.HB, hb = pair - b * a.HB, h = hb / a.rtiles, t0 = (hb - h * a.rtiles) * 16, r0 = t0 + first, rows = min(per, min(16, a.G - t0) - first);
@@ -579,7 +579,8 @@ __global__ __launch_bounds__(JT) void k_kvq_join(DecodeArgs a, int per, int chun
         if (b > b0) before = all + from_lane(upto, min(b - b0, 64) - 1);
         all += from_lane(upto, 63);
     }
-    const PlaceList list{all * (uint32_t)a.HB};
+    PlaceList list;
+    list.set(a, all);
     const int len = a.c.length(b, hb + first == 0 && tid == 0);
     const uint32_t nt = tiles_of<WK>(len);
     T *const out = (T *)a.out + ((int64_t)b * a.H + h * a.G + r0) * dh;
@@ -589,7 +590,7 @@ __global__ __launch_bounds__(JT) void k_kvq_join(DecodeArgs a, int per, int chun
         return;
     }
     // the runs that its tiles are in, and the first one's place among the partial results
-    const uint32_t f0 = before * (uint32_t)a.HB + (uint32_t)hb * (nt + 1) + 1, w0 = list.run_of(a, f0), ns = list.run_of(a, f0 + nt - 1) - w0 + 1;
+    const uint32_t f0 = before * (uint32_t)a.HB + (uint32_t)hb * (nt + 1) + 1, w0 = list.run_of(f0), ns = list.run_of(f0 + nt - 1) - w0 + 1;
     if (ns == 1) return;                                         // the first launch had all of it
     const int64_t slot0 = (int64_t)w0 + (int64_t)b * a.HB + hb;
     const float *ml = a.part_ml + (slot0 * a.HG + first) * 2, *po = a.part_o + (slot0 * a.HG + first) * dh;
@@ -603,33 +604,52 @@ __global__ __launch_bounds__(JT) void k_kvq_join(DecodeArgs a, int per, int chun
     f32x4 x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) x[u] = load(g + u * step);
-    for (int r = wave; r < rows; r += JT / 64) {
+    // maxima and sums, by as many wavefronts a head as there are
+    constexpr int JW = JT / 64;
+    const int share = rows < JW ? JW / rows : 1;                 // wavefronts of a head
+    for (int rw = wave; rw < rows * share; rw += JW) {
+        const int r = rw / share;
         float m = -INFINITY, l = 0.f;
-        for (uint32_t s = lane; s < ns; s += 64) m = fmaxf(m, ml[(s * a.HG + r) * 2]);
-        m = over_lanes<0>(m, fmaxf);
-        const float ms = m == -INFINITY ? 0.f : m;
-        for (uint32_t s = lane; s < ns; s += 64) l += ml[(s * a.HG + r) * 2 + 1] * fast_exp2(ml[(s * a.HG + r) * 2] - ms);
-        l = over_lanes<0>(l, add);
-        if (lane == 0) {
-            if (m == -INFINITY && l == 0.f) a.c.flag(MOA_DEV_EMPTY_KEYS);
-            m_s[r] = ms;
-            inv_s[r] = inverse_sum(m, l);
+        for (uint32_t s = (uint32_t)(rw - r * share) * 64 + lane; s < ns; s += 64 * share) {
+            const float mn = ml[(s * a.HG + r) * 2], ln = ml[(s * a.HG + r) * 2 + 1], top = fmaxf(m, mn), ms = top == -INFINITY ? 0.f : top;
+            l = l * fast_exp2(m - ms) + ln * fast_exp2(mn - ms);
+            m = top;
         }
+        const float top = over_lanes<0>(m, fmaxf), ms = top == -INFINITY ? 0.f : top;
+        l = over_lanes<0>(l * fast_exp2(m - ms), add);
+        if (lane == 0) {
+            parts_s[0][rw] = top;
+            parts_s[1][rw] = l;
+        }
+    }
+    __syncthreads();
+    if (tid < rows) {
+        float m = -INFINITY, l = 0.f;
+        for (int k = 0; k < share; ++k) m = fmaxf(m, parts_s[0][tid * share + k]);
+        const float ms = m == -INFINITY ? 0.f : m;
+        for (int k = 0; k < share; ++k) l += parts_s[1][tid * share + k] * fast_exp2(parts_s[0][tid * share + k] - ms);
+        if (m == -INFINITY && l == 0.f) a.c.flag(MOA_DEV_EMPTY_KEYS);
+        m_s[tid] = ms;
+        inv_s[tid] = inverse_sum(m, l);
     }
     __syncthreads();
     for (;;) {                                                   // (more than once where a pair has more than 4 JT elements)
         const int r = min((int)(4 * c) / dh, rows - 1);
         const float ms = m_s[r];
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        auto top_of = [&](uint32_t s) { return s < ns ? ml[(s * a.HG + r) * 2] : -INFINITY; };
+        float t[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) t[u] = top_of(g + u * step);
         for (uint32_t s = g; s < ns; s += U * step) {
             f32x4 y[U];
             float w[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const uint32_t su = s + u * step;
-                w[u] = su < ns ? fast_exp2(ml[(su * a.HG + r) * 2] - ms) : 0.f;
+                w[u] = fast_exp2(t[u] - ms);
                 y[u] = x[u];
-                x[u] = load(su + U * step);
+                t[u] = top_of(s + (U + u) * step);
+                x[u] = load(s + (U + u) * step);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u)

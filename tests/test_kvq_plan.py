@@ -72,25 +72,27 @@ def test_workspace_of_a_plan(plan):
 
 
 def places(lens, HB, runs):
-    """The list of places dealt to runs as the kernel has it (PlaceList): for every pair with keys, (first run, runs, whole)."""
+    """The list of places dealt to runs as the kernel has it (PlaceList)."""
     total = sum((-(-n // 32) + 1) * HB for n in lens if n)
-    first = (lambda w: min(w, total)) if total < runs else (lambda w: w * total // runs)
-    run_of = (lambda f: f) if total < runs else (lambda f: ((f + 1) * runs - 1) // total)
-    return total, first, run_of
+    log2 = min(runs.bit_length() - 1, max(total, 1).bit_length() - 1)
+    first = lambda w: w * total >> log2
+    run_of = lambda f: (((f + 1) << log2) - 1) // total
+    return total, 1 << log2, first, run_of
 
 
 def test_places_and_runs_are_each_other_s_inverse():
     rng = random.Random(3)
     for _ in range(300):
         lens, HB, runs = [rng.choice([0, 1, 32, 33, rng.randint(0, 5000)]) for _ in range(rng.randint(1, 40))], rng.randint(1, 9), rng.choice([1024, 2048])
-        total, first, run_of = places(lens, HB, runs)
+        total, dealt, first, run_of = places(lens, HB, runs)
+        assert 1 <= dealt <= runs
         of = {}
-        for w in range(runs):
+        for w in range(dealt):
             for f in range(first(w), first(w + 1)):
                 of[f] = w
         assert sorted(of) == list(range(total)) and all(run_of(f) == w for f, w in of.items())
-        sizes = [first(w + 1) - first(w) for w in range(runs)]
-        assert max(sizes) - min(sizes) <= 1
+        sizes = [first(w + 1) - first(w) for w in range(dealt)]
+        assert max(sizes) - min(sizes) <= 1 and (min(sizes) >= 1 or total < 1)
         # the runs of a pair are one behind the other, so that the second launch finds a partial result in each; no two pairs' have the same number
         f, pair, slots = 0, 0, set()
         for n in lens:
