@@ -424,11 +424,25 @@ __global__ __launch_bounds__(PT) void k_kv_release_list(ReleaseArgs a, int per) 
         if (blockIdx.x == 0 && tid == 0 && a.dev_status) atomicOr(a.dev_status, MOA_DEV_BAD_LENGTH);
         have = have < 0 ? 0 : a.n_pages;
     }
+    // a wavefront takes up to 64 of the rows behind at a time, whose first entries that go its lanes look up together
     uint32_t behind = 0;
-    for (int b = b1 + __builtin_amdgcn_readfirstlane(tid >> 6); b < a.B; b += PW) {
-        const int32_t *row = a.table + (int64_t)b * a.max_pages;
+    const int share = min((a.B - b1 + PW - 1) / PW, 64);
+    for (int w0 = b1 + share * __builtin_amdgcn_readfirstlane(tid >> 6); w0 < a.B; w0 += share * PW) {
+        const int rows = min(share, a.B - w0), mine = lane < rows ? first_gone(a, w0 + lane, false) : a.max_pages;
+        int lowest = mine;
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) lowest = min(lowest, __shfl_xor(lowest, o));
+        for (int e0 = 0; e0 < a.max_pages - lowest; e0 += 256)
 #pragma unroll 4
-        for (int p = first_gone(a, b, false) + lane; p < a.max_pages; p += 64) behind += (uint32_t)row[p] < (uint32_t)a.n_pages;
+            for (int k = 0; k < rows; ++k) {
+                const int32_t *row = a.table + (int64_t)(w0 + k) * a.max_pages;
+                const int p0 = __builtin_amdgcn_readlane(mine, k) + e0 + lane;
+                int32_t id[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) id[u] = p0 + 64 * u < a.max_pages ? row[p0 + 64 * u] : -1;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) behind += (uint32_t)id[u] < (uint32_t)a.n_pages;
+            }
     }
     uint32_t count = (uint32_t)have + scan(behind).all;
     for (int b = b1 - 1; b >= b0; --b) {
@@ -446,33 +460,39 @@ __global__ __launch_bounds__(PT) void k_kv_release_list(ReleaseArgs a, int per) 
     }
 }
 
-__global__ __launch_bounds__(256) void k_kv_release_table(ReleaseArgs a)
+__global__ __launch_bounds__(PT) void k_kv_release_table(ReleaseArgs a)
 {
-    const int b = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6))), lane = threadIdx.x & 63;
-    if (b >= a.B) return;
+    __shared__ uint32_t all_s;
+    const int b = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * PW + (threadIdx.x >> 6))), lane = threadIdx.x & 63;
     auto flag = [&](int bit) {
         if (a.dev_status) atomicOr(a.dev_status, bit);
     };
-    int32_t *row = a.table + (int64_t)b * a.max_pages;
-    uint32_t count = 0;
-    bool bad = false;
+    if (threadIdx.x == 0) all_s = 0;
+    __syncthreads();
+    if (b < a.B) {
+        int32_t *row = a.table + (int64_t)b * a.max_pages;
+        uint32_t count = 0;
+        bool bad = false;
 #pragma unroll 4
-    for (int p = first_gone(a, b, lane == 0) + lane; p < a.max_pages; p += 64) {
-        const int32_t id = row[p];
-        if (id < 0) continue;
-        row[p] = -1;
-        bad |= id >= a.n_pages;
-        count += id < a.n_pages;
+        for (int p = first_gone(a, b, lane == 0) + lane; p < a.max_pages; p += 64) {
+            const int32_t id = row[p];
+            if (id < 0) continue;
+            row[p] = -1;
+            bad |= id >= a.n_pages;
+            count += id < a.n_pages;
+        }
+        if (bad) flag(MOA_DEV_BAD_PAGE);
+        count = from_last_lane(wave_scan(count));
+        if (lane == 0 && count) atomicAdd(&all_s, count);
     }
-    if (bad) flag(MOA_DEV_BAD_PAGE);
-    count = from_last_lane(wave_scan(count));
-    if (lane) return;
+    __syncthreads();
     // Whole numbers: their order is of no account.  A list that claimed to hold less than nothing holds nothing, and no list holds more than
     // there are pages, whoever comes last.
-    if (count == 0 && b > 0) return;
+    const int all = (int)all_s;
+    if (threadIdx.x || (all == 0 && blockIdx.x)) return;
     (void)atomicMax(a.n_free, 0);
-    if (atomicAdd(a.n_free, (int)count) + (int)count > a.n_pages) {
-        if (count) flag(MOA_DEV_BAD_PAGE);
+    if (atomicAdd(a.n_free, all) + all > a.n_pages) {
+        if (all) flag(MOA_DEV_BAD_PAGE);
         (void)atomicMin(a.n_free, a.n_pages);
     }
 }
@@ -551,7 +571,7 @@ int32_t moa_kv_release(int32_t B, int32_t n_pages, int32_t page_size, int32_t ma
         MOA_KLAUNCH(k_kv_release_list, dim3((B + per - 1) / per), dim3(PT), 0, st, a, per);
         prof_end(st);
         prof_begin(K_KV_RELEASE_TABLE, st);
-        MOA_KLAUNCH(k_kv_release_table, dim3((B + 3) / 4), dim3(256), 0, st, a);
+        MOA_KLAUNCH(k_kv_release_table, dim3((B + PW - 1) / PW), dim3(PT), 0, st, a);
         prof_end(st);
     }
     const hipError_t e = hipGetLastError();
