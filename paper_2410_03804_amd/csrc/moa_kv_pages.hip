@@ -416,8 +416,7 @@ __device__ __forceinline__ int first_gone(const ReleaseArgs &a, int b, bool repo
 __global__ __launch_bounds__(PT) void k_kv_release_list(ReleaseArgs a, int per)          // sequences of a workgroup
 {
     __shared__ uint32_t sums[2][PW];
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int b0 = (int)blockIdx.x * per, b1 = min(b0 + per, a.B);
+    const int tid = threadIdx.x, lane = tid & 63, b0 = (int)blockIdx.x * per, b1 = min(b0 + per, a.B);
     BlockScan scan{sums};
     int have = *a.n_free;
     if ((uint32_t)have > (uint32_t)a.n_pages) {
@@ -433,7 +432,6 @@ __global__ __launch_bounds__(PT) void k_kv_release_list(ReleaseArgs a, int per) 
 #pragma unroll
         for (int o = 32; o >= 1; o >>= 1) lowest = min(lowest, __shfl_xor(lowest, o));
         for (int e0 = 0; e0 < a.max_pages - lowest; e0 += 256)
-#pragma unroll 4
             for (int k = 0; k < rows; ++k) {
                 const int32_t *row = a.table + (int64_t)(w0 + k) * a.max_pages;
                 const int p0 = __builtin_amdgcn_readlane(mine, k) + e0 + lane;

@@ -5,8 +5,7 @@
 // In single precision from end to end, rounded once to the storage type; only the angle is formed and reduced in double precision, since at
 // position 2^20 a single-precision one is off by 0.06.  A token's cosines and sines are worked out once, by the threads of the workgroup
 // that has it, and serve all of its heads.
-#include "moa_common.h"
-#include "../../include/moa.h"
+#include "moa_kv_device.h"
 
 #include <math.h>
 
@@ -20,6 +19,7 @@ struct RopeNormArgs {
     const void *g[2];                // [dh] or NULL
     int64_t ldx[2], ldy[2];          // elements
     int heads[2];
+    FastDiv by_heads[2];
     int64_t T;
     const int32_t *pos;              // [T]
     int dh, half;                    // elements of a head, pairs that are rotated
@@ -106,92 +106,102 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope_pieces(RopeNormArgs a)
     constexpr int VE = 4 * W / sizeof(T), U = 2;
     __shared__ __attribute__((aligned(16))) float2 cs[TPB * 128];
     const int64_t t0 = (int64_t)blockIdx.x * TPB;
-    const int tokens = (int)(a.T - t0 < TPB ? a.T - t0 : TPB), R = a.heads[0] + a.heads[1], n = tokens * R;
+    const int tokens = (int)(a.T - t0 < TPB ? a.T - t0 : TPB);
     const int c = threadIdx.x % LPR, pairs = a.dh / (2 * VE), turned = a.half / VE;
     const bool on = c < pairs, turn = c < turned;
     const int pa = turn ? c : turned + c, step = turn ? turned : pairs - turned;      // pieces: pa and pa + step
-    struct Row { const T *x; T *y; int t, w; };
-    auto row_of = [&](int r) {
-        const int t = r / R, hh = r - t * R, w = hh >= a.heads[0], h = w ? hh - a.heads[0] : hh;
-        return Row{(const T *)a.x[w] + (t0 + t) * a.ldx[w] + (int64_t)h * a.dh, (T *)a.y[w] + (t0 + t) * a.ldy[w] + (int64_t)h * a.dh, t, w};
-    };
-    Piece x[U][2];
-    auto load = [&](int r, Piece (&v)[2]) {
-        v[0] = v[1] = Piece{};
-        if (r >= n || !on) return;
-        const T *p = row_of(r).x;
-        v[0] = *(const Piece *)(p + pa * VE);
-        v[1] = *(const Piece *)(p + (pa + step) * VE);
-    };
     auto value = [](const Piece &v, int e) {
         return sizeof(T) == 4 ? __uint_as_float(v[e]) : __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
     };
     constexpr int RP = 256 / LPR;                        // rows at a time
     const int first = threadIdx.x / LPR;
+    // queries, then keys (or in workgroups of their own): which of them, and with what weights, is the same for a whole workgroup
+    const int w0 = gridDim.y > 1 ? (int)blockIdx.y : 0, w1 = gridDim.y > 1 ? w0 + 1 : 2;
+#pragma unroll 1
+    for (int w = w0; w < w1; ++w) {
+        const int heads = a.heads[w], n = tokens * heads;
+        const T *const g = (const T *)a.g[w];
+        struct Row { Piece x[2]; int64_t y; int t; } row[U];
+        auto load = [&](int r, Row &v) {
+            v.x[0] = v.x[1] = Piece{};
+            if (r >= n || !on) return;
+            v.t = (int)a.by_heads[w]((uint32_t)r);
+            const int64_t h = (int64_t)(r - v.t * heads) * a.dh + pa * VE;
+            const T *p = (const T *)a.x[w] + (t0 + v.t) * a.ldx[w] + h;
+            v.y = (t0 + v.t) * a.ldy[w] + h;
+            v.x[0] = *(const Piece *)p;
+            v.x[1] = *(const Piece *)(p + step * VE);
+        };
 #pragma unroll
-    for (int u = 0; u < U; ++u) load(first + u * RP, x[u]);
-    Piece g[2][2];
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        g[w][0] = g[w][1] = Piece{};
-        if (!a.g[w] || !on) continue;
-        g[w][0] = *(const Piece *)((const T *)a.g[w] + pa * VE);
-        g[w][1] = *(const Piece *)((const T *)a.g[w] + (pa + step) * VE);
-    }
-    if (a.half) {
-        angles(a, t0, tokens, cs);
-        __syncthreads();
-    }
-    for (int r0 = first; r0 < n; r0 += U * RP) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int r = r0 + u * RP;
-            float y[2][VE];
-            float ss = 0.f;
+        for (int u = 0; u < U; ++u) load(first + u * RP, row[u]);
+        float gf[2][VE];
+        if (g) {
+            Piece gp[2] = {};
+            if (on) {
+                gp[0] = *(const Piece *)(g + pa * VE);
+                gp[1] = *(const Piece *)(g + (pa + step) * VE);
+            }
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int e = 0; e < VE; ++e) {
-                    y[i][e] = value(x[u][i], e);
-                    ss = fmaf(y[i][e], y[i][e], ss);
-                }
-            load(r + U * RP, x[u]);
+                for (int e = 0; e < VE; ++e) gf[i][e] = value(gp[i], e);
+        }
+        if (w == w0 && a.half) {
+            angles(a, t0, tokens, cs);
+            __syncthreads();
+        }
+        for (int r0 = first; r0 < n; r0 += U * RP) {
 #pragma unroll
-            for (int o = LPR / 2; o >= 1; o >>= 1) ss += __shfl_xor(ss, o);
-            if (r >= n || !on) continue;
-            const Row at = row_of(r);
-            if (a.g[at.w]) {
-                const float inv = 1.f / sqrtf(ss / (float)a.dh + a.eps);
+            for (int u = 0; u < U; ++u) {
+                const int r = r0 + u * RP;
+                float y[2][VE];
+                float ss = 0.f;
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int e = 0; e < VE; ++e) y[i][e] = y[i][e] * inv * (at.w ? value(g[1][i], e) : value(g[0][i], e));
-            }
-            if (turn) {
-                const f32x4 *f = (const f32x4 *)(cs + at.t * a.half + c * VE);
+                    for (int e = 0; e < VE; ++e) {
+                        y[i][e] = value(row[u].x[i], e);
+                        if (g) ss = fmaf(y[i][e], y[i][e], ss);
+                    }
+                const int64_t to0 = row[u].y;
+                const int t = row[u].t;
+                load(r + U * RP, row[u]);
+                if (g) {
 #pragma unroll
-                for (int e = 0; e < VE; e += 2) {
-                    const f32x4 f2 = f[e / 2];
+                    for (int o = LPR / 2; o >= 1; o >>= 1) ss += __shfl_xor(ss, o);
+                    const float inv = 1.f / sqrtf(ss / (float)a.dh + a.eps);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const float lo = y[0][e + i], hi = y[1][e + i], cn = f2[2 * i], sn = f2[2 * i + 1];
-                        y[0][e + i] = fmaf(lo, cn, -hi * sn);
-                        y[1][e + i] = fmaf(hi, cn, lo * sn);
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int e = 0; e < VE; ++e) y[i][e] = y[i][e] * inv * gf[i][e];
+                }
+                if (r >= n || !on) continue;
+                if (turn) {
+                    const f32x4 *f = (const f32x4 *)(cs + t * a.half + c * VE);
+#pragma unroll
+                    for (int e = 0; e < VE; e += 2) {
+                        const f32x4 f2 = f[e / 2];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const float lo = y[0][e + i], hi = y[1][e + i], cn = f2[2 * i], sn = f2[2 * i + 1];
+                            y[0][e + i] = fmaf(lo, cn, -hi * sn);
+                            y[1][e + i] = fmaf(hi, cn, lo * sn);
+                        }
                     }
                 }
-            }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                Piece o;
+                for (int i = 0; i < 2; ++i) {
+                    Piece o;
 #pragma unroll
-                for (int e = 0; e < W; ++e) {
-                    if constexpr (sizeof(T) == 4) o[e] = __float_as_uint(y[i][e]);
-                    else o[e] = pack_bf16x2(y[i][2 * e], y[i][2 * e + 1]);
+                    for (int e = 0; e < W; ++e) {
+                        if constexpr (sizeof(T) == 4) o[e] = __float_as_uint(y[i][e]);
+                        else o[e] = pack_bf16x2(y[i][2 * e], y[i][2 * e + 1]);
+                    }
+                    Piece *const to = (Piece *)((T *)a.y[w] + to0 + i * step * VE);
+                    // (of many tokens no cache holds the results until they are read: 42.6 us without, 36.9 with, where reads said so too 38.8)
+                    if constexpr (TPB > 1) __builtin_nontemporal_store(o, to);
+                    else *to = o;
                 }
-                Piece *const to = (Piece *)(at.y + (pa + i * step) * VE);
-                // (of many tokens no cache holds the results until they are read: 42.6 us without, 36.9 with, where reads said so too 38.8)
-                if constexpr (TPB > 1) __builtin_nontemporal_store(o, to);
-                else *to = o;
             }
         }
     }
@@ -200,10 +210,17 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope_pieces(RopeNormArgs a)
 template <typename T, int W, int LPR>
 hipError_t launch_pieces(const RopeNormArgs &a, hipStream_t st)
 {
-    const bool many = a.T >= 2048;
+    // Four tokens a workgroup where there are many, so that its threads' angles are one each; sixteen where four have too few heads for its
+    // threads (16000 tokens of 8 heads of 80 dims: 20.0 us and 14.6; 8192 of 40 of 128 31.0 and 36.0).  Of few, one, queries and keys apart (16: 7.5 us
+    // one behind the other, 4.9).  40 heads, one token a workgroup against four: 512 tokens 6.4 us and 8.6, 1024 10.3 and 8.9, 1536 14.5 and 10.4.
+    const int heads = a.heads[0] > a.heads[1] ? a.heads[0] : a.heads[1];
+    const bool many = a.T >= 1024, few = a.T >= 4096 && heads * 4 * LPR < 512;
+    const int tokens = few ? 16 : many ? 4 : 1;
+    const dim3 grid((unsigned)((a.T + tokens - 1) / tokens), many ? 1 : 2);
     prof_begin(K_QK_NORM_ROPE, st);
-    if (many) MOA_KLAUNCH((k_qk_norm_rope_pieces<T, W, LPR, 4>), dim3((unsigned)((a.T + 3) / 4)), dim3(256), 0, st, a);
-    else MOA_KLAUNCH((k_qk_norm_rope_pieces<T, W, LPR, 1>), dim3((unsigned)a.T), dim3(256), 0, st, a);
+    if (few) MOA_KLAUNCH((k_qk_norm_rope_pieces<T, W, LPR, 16>), grid, dim3(256), 0, st, a);
+    else if (many) MOA_KLAUNCH((k_qk_norm_rope_pieces<T, W, LPR, 4>), grid, dim3(256), 0, st, a);
+    else MOA_KLAUNCH((k_qk_norm_rope_pieces<T, W, LPR, 1>), grid, dim3(256), 0, st, a);
     prof_end(st);
     return hipGetLastError();
 }
@@ -282,7 +299,8 @@ int32_t moa_qk_norm_rope(int32_t dtype, const void *q, int64_t q_stride, int32_t
     if (n_kv_heads) bits |= (uintptr_t)k | (uintptr_t)k_out;
     bits |= (uintptr_t)gq | (uintptr_t)gk;
     if ((bits & (es - 1)) || ((uintptr_t)pos & 3)) return api_fail(MOA_ERR_SHAPE, "qk_norm_rope: pointers must be aligned to their elements");
-    RopeNormArgs a = {{q, k}, {q_out, k_out}, {gq, gk}, {q_stride, k_stride}, {q_out_stride, k_out_stride}, {n_q_heads, n_kv_heads}, T, pos,
+    RopeNormArgs a = {{q, k}, {q_out, k_out}, {gq, gk}, {q_stride, k_stride}, {q_out_stride, k_out_stride}, {n_q_heads, n_kv_heads},
+                      {FastDiv(n_q_heads ? n_q_heads : 1), FastDiv(n_kv_heads ? n_kv_heads : 1)}, T, pos,
                             head_dim, rot_dim / 2, rms_eps, {}};
     for (int i = 0; i < 7 && rot_dim; ++i) a.power[i] = exp(-log((double)rope_theta) * ((1 << i) / (0.5 * rot_dim)));
     prof_set_site(S_QK_NORM_ROPE);
