@@ -3,7 +3,8 @@
 // As moa_decode_attn.hip, with keys and values code * scale, a scale for each block of rows of a page and KV head:
 //   s_j = (q . c_j) ks_j log2(e) / sqrt(dh),  l = sum 2^(s_j - m),  o = sum (2^(s_j - m) vs_j) d_j / l,
 // c_j, d_j the codes of key and value j and ks_j, vs_j their blocks' scales: a scale is multiplied into the score or the weight, once
-// a key, and not into every element.  The list of tiles, the runs and the second launch are moa_decode_attn's.
+// a key, and not into every element.  On the matrix cores the codes are widened to bf16, which holds every one of them: a product of two e4m3
+// numbers would need queries and weights in 8 bits too.
 #include "moa_decode_device.h"
 #include "moa_kvq_device.h"
 #include "moa_kvq_plan.h"
@@ -19,7 +20,9 @@ struct KvqDecodeArgs {
 };
 
 // ---------------------------------------------------------------- element by element
-// A row of keys or values is spread over LPR lanes, four codes each; 64 / LPR keys at a time.  WORDS: they can be read as one word.
+// For head dims that are not in sixteens and for codes or queries that are not aligned: a row of keys or values is spread over LPR lanes, four codes
+// each; 64 / LPR keys at a time.  WORDS: they can be read as one word.  (Sums over lanes bound it: at 128 dims, where it is not used otherwise, 8 x
+// 32768 tokens with 64 heads 1040 us.)
 template <typename T, int LPR, bool WORDS>
 __global__ __launch_bounds__(256, 2) void k_kvq_decode(KvqDecodeArgs k)
 {
@@ -260,6 +263,10 @@ struct Walk {
 // matrix cores.  A wavefront has LDS of its own for NST tiles, and no barrier.  Codes go straight into LDS: a tile's keys take the place of
 // those NST tiles before as soon as these have been used, their scales and its values likewise, and its table entries come another NST tiles
 // before that.
+// HBM bounds it: 8 sequences of 32768 tokens, 64 heads, 538 MB, 90 us (6.0 TB/s over all of it, 5 us of which are its beginning; FETCH_SIZE is the
+// bytes of the codes and scales); vector units are busy 51 % of SIMD time, the matrix pipe 14 %, no LDS bank is waited for.  At 64 dims the
+// vector units bound it, whose work is per key and not per byte: 64 x 4000 tokens, 131 MB, 31 us.  (Four wavefronts a run, as moa_decode_attn: 64
+// ragged sequences up to 8192 125 us, now 95.)
 // ONE: a workgroup of four wavefronts per pair, a quarter of its tiles each, joined in LDS.  Else a wavefront per run, which is a workgroup: what
 // is fetched goes on from one pair to the next.
 // DH: head_dim as it lies in LDS; the rows in the pool may be shorter (PAD, a multiple of 16): their last pieces are then zeros.
@@ -562,7 +569,8 @@ __global__ __launch_bounds__(ONE ? 256 : 64, DH == 256 ? 1 : 2) void k_kvq_decod
 
 // ---------------------------------------------------------------- the second launch
 // A workgroup joins the partial results of one or more query heads of a pair: as many as leave 512 workgroups, where there are so many pairs.
-// Us, a workgroup a head against one a pair: 512 pairs of 4 heads, five parts each, 8.4 and 4.8; 64 pairs of 8 heads, 32 parts, 5.2 and 9.0.
+// Us, a workgroup a head against one a pair: 512 pairs of 4 heads, five parts each, 8.4 and 4.8; 64 pairs of 8 heads, 32 parts, 5.2 and 9.0.  Where
+// parts are many, maxima and sums by one wavefront a head bound it: 2 pairs of 3 heads, 850 parts, 23 us, by all of them 8.
 constexpr int JT = 512;
 template <typename T>
 __global__ __launch_bounds__(JT) void k_kvq_join(DecodeArgs a, int per, int chunks)      // heads of a workgroup; such workgroups of a pair

@@ -13,6 +13,11 @@ struct KvqPlan {
 };
 
 // mfma: rows of codes and queries can be read 16 bytes at a time.
+// One workgroup of four wavefronts per pair, without a second launch (5 us), where that is a short walk, or not a long one and there are pairs
+// enough.  Else 2048 runs of a wavefront each, eight a compute unit, on the matrix cores (at 256 dims 1024, whose registers fit once a
+// SIMD), 1024 of four wavefronts element by element.  Measured, us, 8b heads: per pair 1 x 300 7.3, 1 x 512 9.5, 64 x 500 14.9, 64 x 1000
+// 24.9; runs + join 1 x 1084 6.2 + 5.9, 1 x 2000 5.1 + 5.2.  4096 and 8192 runs: 8 x 32768 with 64 heads 98 and 105 against 92, 64 ragged
+// sequences up to 8192 105 and 112 against 105.
 inline KvqPlan kvq_plan(int B, int Hkv, int dh, int cap, int H, bool mfma)
 {
     auto align256 = [](size_t n) { return (n + 255) & ~(size_t)255; };
