@@ -192,10 +192,10 @@ __device__ __forceinline__ void encode_block(const KvqAppendArgs &a, int b, int 
 }
 
 // ONE: a workgroup per sequence, which may then also move its length on.  Else gridDim.x of them per sequence, and a launch for the lengths.
-// What bounds it is the chain of a wavefront's loads (length, table and rows, scale), then its maximum over lanes: by trace 4.6 us for a token of
+// What bounds it is the chain of a wavefront's loads (length, table and rows, scale), then its maximum over lanes: by trace 4.9 us for a token of
 // each of 64 sequences, 8.2 for up to seven nodes of each of 16, 11.9 + 3.9 for 5100 rows of four prompts (31 MB, 6 us by the copy rate;
 // wavefronts wait 54 % of their time, vector units are busy 53 %).  A page of fewer than 16 rows is a block of its own: pages of one row, 41000
-// of them, 260 us.
+// of them, 285 us (252 MB, 49 us by the copy rate).
 template <typename T, int VE, int IT, int THREADS, bool ONE>
 __global__ __launch_bounds__(THREADS) void k_kvq_append(KvqAppendArgs a)
 {
@@ -284,7 +284,7 @@ struct KvqReadArgs {
 // VE codes at a time, 16 bytes of results, or 1 where rows are not in such pieces.  HBM bounds it: 16 sequences of 100 to 1500 tokens, 79 MB, 23 us
 // with 16 codes a load and 32 bytes of results behind each other, 21.8 with 16 bytes, 16.8 when the stores say that nothing of it is read
 // again soon, 15 with two of them a thread instead of four.
-// (64 sequences of up to 251 tokens, 53 MB, 12.4 us by trace: 4.3 TB/s.)
+// (64 sequences of up to 251 tokens, 53 MB, 12.8 us by trace: 4.1 TB/s.)
 constexpr int READ_U = 2;
 template <typename T, int VE>
 __global__ __launch_bounds__(256) void k_kvq_read(KvqReadArgs a)

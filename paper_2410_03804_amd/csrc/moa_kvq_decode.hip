@@ -570,7 +570,8 @@ __global__ __launch_bounds__(ONE ? 256 : 64, DH == 256 ? 1 : 2) void k_kvq_decod
 // ---------------------------------------------------------------- the second launch
 // A workgroup joins the partial results of one or more query heads of a pair: as many as leave 512 workgroups, where there are so many pairs.
 // Us, a workgroup a head against one a pair: 512 pairs of 4 heads, five parts each, 8.4 and 4.8; 64 pairs of 8 heads, 32 parts, 5.2 and 9.0.  Where
-// parts are many, maxima and sums by one wavefront a head bound it: 2 pairs of 3 heads, 850 parts, 23 us, by all of them 8.
+// parts are many, maxima and sums by one wavefront a head bound it: 2 pairs of 3 heads, 845 parts, 23 us; by all of them, and of the 512 parts that
+// there now are, 8.
 constexpr int JT = 512;
 template <typename T>
 __global__ __launch_bounds__(JT) void k_kvq_join(DecodeArgs a, int per, int chunks)      // heads of a workgroup; such workgroups of a pair
