@@ -490,7 +490,9 @@ __global__ __launch_bounds__(PT) void k_kv_release_table(ReleaseArgs a)
     // there are pages, whoever comes last.
     const int all = (int)all_s;
     if (threadIdx.x || (all == 0 && blockIdx.x)) return;
+    // (Within its bounds before anything is added: a claim near 2^31 would come out below zero.)
     (void)atomicMax(a.n_free, 0);
+    (void)atomicMin(a.n_free, a.n_pages);
     if (atomicAdd(a.n_free, all) + all > a.n_pages) {
         if (all) flag(MOA_DEV_BAD_PAGE);
         (void)atomicMin(a.n_free, a.n_pages);

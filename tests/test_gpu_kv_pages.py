@@ -256,3 +256,17 @@ def test_captured():
         table = s.t_table.cpu().numpy()
         assert slot.tolist() == [int(table[b, (3 * step + i) // 16]) * 16 + (3 * step + i) % 16 for b in range(8) for i in range(3)]
     assert s.status.item() == 0
+
+
+@pytest.mark.parametrize("claims,holds", [(-(2 ** 31), 0), (-1, 0), (99, 10), (2 ** 31 - 1, 10)])
+@pytest.mark.parametrize("B", [2, 60])                        # one launch; two, whose additions come from several workgroups
+def test_a_release_to_a_list_that_claims_the_impossible(B, claims, holds):
+    s = Pages(B, 10, 16, 400, seed=8, free=10)
+    s.n_free.fill_(claims)
+    s.t_table[0, 5], s.t_table[B - 1, 399] = 3, 4
+    moa.kv_release(s.t_table, s.t_len, 16, s.free, s.n_free, dev_status=s.status)
+    more = moa.DEV_BAD_PAGE if holds == 10 else 0
+    assert s.status.item() == moa.DEV_BAD_LENGTH | more and torch.all(s.t_table == -1)
+    assert s.n_free.item() == min(holds + 2, 10)
+    if holds == 0:
+        assert s.free[:2].tolist() == [4, 3]
