@@ -330,7 +330,7 @@ def _plain_reserve(st):
     need = needs.sum(dim=1)
     upto = torch.cumsum(need, dim=0)
     ok = (need == 0) | (upto <= st["n_free"].long())
-    taken = torch.where(ok, need, torch.zeros_like(need)).sum()
+    taken = (torch.where(ok, upto, torch.zeros_like(upto))).amax()
     which = (torch.cumsum(needs.reshape(-1).long(), dim=0) - 1).view(B, mp)
     at = (st["n_free"].long() - 1 - which).clamp(min=0)
     table.copy_(torch.where(needs & ok[:, None], free[at], table))
