@@ -383,8 +383,9 @@ int32_t moa_kv_evict(const moa_kv_cache_t *cache, int32_t budget, int32_t recent
  *     some get none (MOA_DEV_CACHE_FULL), those that lack none are not held up.  *n_free falls by what was taken.
  *   n_got [B] (may be n_new itself): the tokens of b, or 0 where it got no pages.
  *   pos, slot [T] (either may be NULL): row t's position, seen[b] + i (seen NULL: len[b] + i) for token i of b, and its slot in the pool, page *
- *     page_size + row in the page; -1 where b got no pages or an entry is no page of the pool (MOA_DEV_BAD_PAGE).  Rows behind the last
- *     token get position 0 and slot -1.
+ *     page_size + row in the page; -1 where b got no pages or an entry is no page of the pool.  Rows behind the last token get position 0
+ *     and slot -1.
+ *   An entry that a row of the batch lies in and that is no page of the pool: MOA_DEV_BAD_PAGE, whatever else is asked for.
  * moa_kv_release: entries behind the page of slot len[b] - 1 that name a page lose it (-1); the pages go back, so that the first of them by
  *   sequence and slot is the next one to be taken.  For a sequence that is done, set its len to 0 first; behind moa_kv_evict or a rejected draft
  *   it gives back what they left.  A page that several sequences share is for the caller to take out of all tables but one: *n_free never

@@ -220,19 +220,13 @@ __global__ __launch_bounds__(PT) void k_kv_reserve(ReserveArgs a)
 // ---------------------------------------------------------------- in three: a wavefront a sequence counts what it wants and lacks, into tok_off and n_got
 // 64 prompts of 200 to 2048 tokens, 131072 rows of positions and slots: 3.0 + 3.7 + 5.0 us by trace (one workgroup for all but positions and slots 10.7
 // + 4.0, and 283 + 5 for 668 prompts in pages of one row, which now take 13).
-__device__ __forceinline__ int count_lacking(const ReserveArgs &a, int b, int len, int n, bool report)
+__device__ __forceinline__ int count_lacking(const ReserveArgs &a, int b, int len, int n)
 {
     const int lane = threadIdx.x & 63, p0 = (int)a.page((uint32_t)len), pages = a.pages_of(len, n);
     const int32_t *row = a.table + (int64_t)b * a.max_pages + p0;
     int count = 0;
-    bool bad = false;
 #pragma unroll 4
-    for (int p = lane; p < pages; p += 64) {
-        const int32_t id = row[p];
-        count += id < 0;
-        bad |= id >= a.n_pages;
-    }
-    if (bad && report) a.flag(MOA_DEV_BAD_PAGE);
+    for (int p = lane; p < pages; p += 64) count += row[p] < 0;
     return (int)from_last_lane(wave_scan((uint32_t)count));
 }
 
@@ -241,7 +235,7 @@ __global__ __launch_bounds__(256) void k_kv_reserve_count(ReserveArgs a)
     const int b = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
     if (b >= a.B) return;
     int len;
-    const int n = a.wanted(b, len), lacks = count_lacking(a, b, len, n, true);
+    const int n = a.wanted(b, len), lacks = count_lacking(a, b, len, n);
     if ((threadIdx.x & 63) == 0) {
         a.tok_off[b] = n;
         a.n_got[b] = lacks;
@@ -283,7 +277,7 @@ __global__ __launch_bounds__(PT) void k_kv_reserve_sum(ReserveArgs a)
             }
             __syncthreads();
             if (cut_s[0] >= 0) {
-                const int lacks = count_lacking(a, cut_s[0], a.length(cut_s[0], false), cut_s[1], false);
+                const int lacks = count_lacking(a, cut_s[0], a.length(cut_s[0], false), cut_s[1]);
                 if (b == cut_s[0]) need = (uint32_t)lacks;
                 __syncthreads();
             }
@@ -322,18 +316,20 @@ __global__ __launch_bounds__(PT) void k_kv_reserve_write(ReserveArgs a)
     __syncthreads();                               // everybody has read n_got
     if (tid == 0) a.n_got[b] = top < 0 ? 0 : n;
     BlockScan scan{sums};
-    if (top >= 0) {
-        const int pages = a.pages_of(len, n), from = *a.n_free + top;
-        int32_t *row = a.table + (int64_t)b * a.max_pages + (int)a.page((uint32_t)len);
-        uint32_t rank = 0;
-        for (int p0 = 0; p0 < pages; p0 += step) {
-            const int p = p0 + tid;
-            const bool lacks = p < pages && row[p] < 0;
-            const BlockScan::Sum r = scan(lacks ? 1u : 0u);
-            if (lacks) row[p] = a.page_from(from - (int)(rank + r.before));
-            rank += r.all;
-        }
+    const int pages = a.pages_of(len, n), from = *a.n_free + top;
+    int32_t *row = a.table + (int64_t)b * a.max_pages + (int)a.page((uint32_t)len);
+    uint32_t rank = 0;
+    bool bad = false;                              // (said here: of the batch's rows, which the count did not know)
+    for (int p0 = 0; p0 < pages; p0 += step) {
+        const int p = p0 + tid;
+        const int32_t id = p < pages ? row[p] : 0;
+        bad |= id >= a.n_pages;
+        if (top < 0) continue;
+        const BlockScan::Sum r = scan(id < 0 ? 1u : 0u);
+        if (id < 0) row[p] = a.page_from(from - (int)(rank + r.before));
+        rank += r.all;
     }
+    if (bad) a.flag(MOA_DEV_BAD_PAGE);
     if (!a.pos && !a.slot) return;
     __syncthreads();                               // the table is written
     for (int i = tid; i < n; i += step) a.token(off + i, b, off, top >= 0);
