@@ -568,7 +568,7 @@ __global__ __launch_bounds__(ONE ? 256 : 64, DH == 256 ? 1 : 2) void k_kvq_decod
 }
 
 // ---------------------------------------------------------------- the second launch
-// A workgroup joins the partial results of one or more query heads of a pair: as many as leave 512 workgroups, where there are so many pairs.
+// A workgroup joins the partial results of one or more query heads of a pair: as many as leave 512 workgroups, where there are so many.
 // Us, a workgroup a head against one a pair: 512 pairs of 4 heads, five parts each, 8.4 and 4.8; 64 pairs of 8 heads, 32 parts, 5.2 and 9.0.  Where
 // parts are many, maxima and sums by one wavefront a head bound it: 2 pairs of 3 heads, 845 parts, 23 us; by all of them, and of the 512 parts that
 // there now are, 8.
@@ -726,18 +726,17 @@ hipError_t launch_elements(const KvqDecodeArgs &k, int grid, hipStream_t st)
 }
 
 template <typename T>
-hipError_t launch_decode(const KvqDecodeArgs &k, bool mfma, hipStream_t st)
+hipError_t launch_decode(const KvqDecodeArgs &k, const KvqPlan &p, hipStream_t st)
 {
     const DecodeArgs &a = k.d;
     const int grid = a.runs ? a.runs : a.c.B * a.HB;
     hipError_t e;
-    if (mfma) e = a.c.dh <= 64 ? launch_mfma<T, 64>(k, st) : a.c.dh <= 128 ? launch_mfma<T, 128>(k, st) : launch_mfma<T, 256>(k, st);
+    if (p.mfma) e = a.c.dh <= 64 ? launch_mfma<T, 64>(k, st) : a.c.dh <= 128 ? launch_mfma<T, 128>(k, st) : launch_mfma<T, 256>(k, st);
     else e = a.c.dh <= 64 ? launch_elements<T, 16>(k, grid, st) : a.c.dh <= 128 ? launch_elements<T, 32>(k, grid, st) : launch_elements<T, 64>(k, grid, st);
     if (e != hipSuccess || !a.runs) return e;
-    if (!mfma) return launch_decode_join(a, sizeof(T) == 2, st);
+    if (!p.mfma) return launch_decode_join(a, sizeof(T) == 2, st);
     prof_begin(K_KVQ_JOIN, st);
-    const int pairs = a.c.B * a.HB, heads = (int)((int64_t)pairs * a.HG / 512), per = heads < 1 ? 1 : heads < a.HG ? heads : a.HG, chunks = (a.HG + per - 1) / per;
-    MOA_KLAUNCH(k_kvq_join<T>, dim3(pairs * chunks), dim3(JT), 0, st, a, per, chunks);
+    MOA_KLAUNCH(k_kvq_join<T>, dim3(a.c.B * a.HB * p.chunks), dim3(JT), 0, st, a, p.per, p.chunks);
     prof_end(st);
     return hipGetLastError();
 }
@@ -802,7 +801,7 @@ int32_t moa_kvq_decode_attn(const moa_kvq_cache_t *cache, int32_t n_q_heads, con
                              cache->k_scale, cache->v_scale, kvq_blocks(cache->page_size)};
     prof_set_site(S_KVQ);
     hipStream_t st = (hipStream_t)stream;
-    const hipError_t e = cache->dtype == MOA_BF16 ? launch_decode<bf16_t>(k, p.mfma, st) : launch_decode<float>(k, p.mfma, st);
+    const hipError_t e = cache->dtype == MOA_BF16 ? launch_decode<bf16_t>(k, p, st) : launch_decode<float>(k, p, st);
     return e == hipSuccess ? MOA_OK : api_fail(MOA_ERR_HIP, hipGetErrorString(e));
 }
 

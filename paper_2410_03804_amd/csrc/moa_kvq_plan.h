@@ -5,9 +5,12 @@
 
 namespace moa {
 
+constexpr int KVQ_JOINS = 512;         // workgroups that the second launch is to have
+
 struct KvqPlan {
     bool mfma;                         // on the matrix cores, else element by element
     int HG, rtiles, runs;              // query heads in a tile; tiles per KV head; workgroups, 0: one per pair
+    int per, chunks;                   // of the second launch behind the matrix cores' runs: query heads of a workgroup, such workgroups of a pair
     size_t part_o, part_ml;            // bytes
     size_t total() const { return part_o + part_ml; }
 };
@@ -31,6 +34,10 @@ inline KvqPlan kvq_plan(int B, int Hkv, int dh, int cap, int H, bool mfma)
     p.runs = cap <= walk ? 0 : !mfma ? 1024 : dh <= 128 ? 2048 : 1024;
     p.part_o = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * dh * 4) : 0;
     p.part_ml = p.runs ? align256((size_t)(p.runs + pairs) * p.HG * 2 * 4) : 0;
+    // As many heads a workgroup as leave 512 of them, where there are so many.
+    const int64_t heads = pairs * p.HG / KVQ_JOINS;
+    p.per = heads < 1 ? 1 : heads < p.HG ? (int)heads : p.HG;
+    p.chunks = (p.HG + p.per - 1) / p.per;
     return p;
 }
 
