@@ -6,6 +6,7 @@
 // position 2^20 a single-precision one is off by 0.06.  A token's cosines and sines are worked out once, by the threads of the workgroup
 // that has it, and serve all of its heads.
 #include "moa_kv_device.h"
+#include "moa_rope_plan.h"
 
 #include <math.h>
 
@@ -211,60 +212,42 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope_pieces(RopeNormArgs a)
 }
 
 template <typename T, int W, int LPR>
-hipError_t launch_pieces(const RopeNormArgs &a, hipStream_t st)
+hipError_t launch_pieces(const RopeNormArgs &a, const RopePlan &p, hipStream_t st)
 {
-    // Four tokens a workgroup where there are many, so that its threads' angles are one each; sixteen where four have too few heads for its
-    // threads (16000 tokens of 8 heads of 80 dims: 20.0 us and 14.6; 8192 of 40 of 128 31.0 and 36.0).  Of few, one, queries and keys apart (16: 7.5 us
-    // one behind the other, 4.9).  40 heads, one token a workgroup against four: 512 tokens 6.4 us and 8.6, 1024 10.3 and 8.9, 1536 14.5 and 10.4.
-    const int heads = a.heads[0] > a.heads[1] ? a.heads[0] : a.heads[1];
-    const bool many = a.T >= 1024, few = a.T >= 4096 && heads * 4 * LPR < 512;
-    const int tokens = few ? 16 : many ? 4 : 1;
-    const dim3 grid((unsigned)((a.T + tokens - 1) / tokens), many ? 1 : 2);
+    const dim3 grid((unsigned)((a.T + p.tokens - 1) / p.tokens), p.apart ? 2 : 1);
     prof_begin(K_QK_NORM_ROPE, st);
-    if (few) MOA_KLAUNCH((k_qk_norm_rope_pieces<T, W, LPR, 16>), grid, dim3(256), 0, st, a);
-    else if (many) MOA_KLAUNCH((k_qk_norm_rope_pieces<T, W, LPR, 4>), grid, dim3(256), 0, st, a);
+    if (p.tokens == 16) MOA_KLAUNCH((k_qk_norm_rope_pieces<T, W, LPR, 16>), grid, dim3(256), 0, st, a);
+    else if (p.tokens == 4) MOA_KLAUNCH((k_qk_norm_rope_pieces<T, W, LPR, 4>), grid, dim3(256), 0, st, a);
     else MOA_KLAUNCH((k_qk_norm_rope_pieces<T, W, LPR, 1>), grid, dim3(256), 0, st, a);
     prof_end(st);
     return hipGetLastError();
 }
 
-// every address in pieces of W words, and pairs of pieces that are rotated or pass
 template <typename T, int W>
-bool in_pieces(const RopeNormArgs &a)
-{
-    constexpr int VE = 4 * W / sizeof(T);
-    uintptr_t bits = 0;
-    int64_t elems = 0;
-    for (int w = 0; w < 2; ++w)
-        if (a.heads[w]) {
-            bits |= (uintptr_t)a.x[w] | (uintptr_t)a.y[w] | (uintptr_t)a.g[w];
-            elems |= a.ldx[w] | a.ldy[w];
-        }
-    return a.dh % (2 * VE) == 0 && a.half % VE == 0 && !(bits & (4 * W - 1)) && elems % VE == 0;
-}
-
-template <typename T, int W>
-hipError_t launch_width(const RopeNormArgs &a, hipStream_t st)
+hipError_t launch_width(const RopeNormArgs &a, const RopePlan &p, hipStream_t st)
 {
     constexpr int MOST = 256 * sizeof(T) / (8 * W);      // pairs of pieces that a head can have
-    const int pairs = a.dh * (int)sizeof(T) / (8 * W);
-    if (pairs <= 4) return launch_pieces<T, W, 4>(a, st);
-    if (pairs <= 8) return launch_pieces<T, W, 8>(a, st);
+    if (p.lanes == 4) return launch_pieces<T, W, 4>(a, p, st);
+    if (p.lanes == 8) return launch_pieces<T, W, 8>(a, p, st);
+    if constexpr (MOST > 32)
+        if (p.lanes == 64) return launch_pieces<T, W, 64>(a, p, st);
     if constexpr (MOST > 16)
-        if (pairs > 16) {
-            if constexpr (MOST > 32)
-                if (pairs > 32) return launch_pieces<T, W, 64>(a, st);
-            return launch_pieces<T, W, 32>(a, st);
-        }
-    return launch_pieces<T, W, 16>(a, st);
+        if (p.lanes == 32) return launch_pieces<T, W, 32>(a, p, st);
+    return launch_pieces<T, W, 16>(a, p, st);
 }
 
 template <typename T>
 hipError_t launch(const RopeNormArgs &a, hipStream_t st)
 {
-    if (in_pieces<T, 4>(a)) return launch_width<T, 4>(a, st);
-    // (16145 tokens of 8 heads of 80 dims, 40 of them rotated: 44 us in the kernel for any sizes)
-    if (in_pieces<T, 2>(a)) return launch_width<T, 2>(a, st);
+    uint64_t bits = 0, elems = 0;
+    for (int w = 0; w < 2; ++w)
+        if (a.heads[w]) {
+            bits |= (uintptr_t)a.x[w] | (uintptr_t)a.y[w] | (uintptr_t)a.g[w];
+            elems |= (uint64_t)(a.ldx[w] | a.ldy[w]);
+        }
+    const RopePlan p = rope_plan(sizeof(T), a.dh, a.half, bits, elems, a.T, a.heads[0] > a.heads[1] ? a.heads[0] : a.heads[1]);
+    if (p.words == 4) return launch_width<T, 4>(a, p, st);
+    if (p.words == 2) return launch_width<T, 2>(a, p, st);
     prof_begin(K_QK_NORM_ROPE, st);
     MOA_KLAUNCH(k_qk_norm_rope<T>, dim3((unsigned)a.T), dim3(256), 0, st, a);
     prof_end(st);
