@@ -372,7 +372,8 @@ int32_t moa_kv_evict(const moa_kv_cache_t *cache, int32_t budget, int32_t recent
  * (Sec. 2.1, one token per forward pass; Sec. 2.2, the tokens of a draft) builds its tables without a trip to the host.  A table entry below
  * 0 names no page.  free_pages [n_pages] is a stack of the pages that nobody has, of which the first *n_free count; it, the table [B,
  * max_pages] and *n_free belong to the caller, who has them start somewhere (all pages free, all entries -1).  A table serves the caches of
- * all layers.  len [B] is the slots in use, as in moa_kv_cache_t, within max_pages * page_size (clamped, MOA_DEV_BAD_LENGTH).
+ * all layers; each of these has a len of its own, which its append moves on: with one for all, a second layer's rows would land behind
+ * the first's.  len [B] here is any of them, the slots in use before the step's appends, within max_pages * page_size (clamped, MOA_DEV_BAD_LENGTH).
  *
  * moa_kv_reserve: sequence b is about to get n_new[b] tokens, into slots len[b] ..; the batch holds them packed, one sequence behind the
  *   other, in T rows.
@@ -384,7 +385,7 @@ int32_t moa_kv_evict(const moa_kv_cache_t *cache, int32_t budget, int32_t recent
  *   n_got [B] (may be n_new itself): the tokens of b, or 0 where it got no pages.
  *   pos, slot [T] (either may be NULL): row t's position, seen[b] + i (seen NULL: len[b] + i) for token i of b, and its slot in the pool, page *
  *     page_size + row in the page; -1 where b got no pages or an entry is no page of the pool.  Rows behind the last token get position 0
- *     and slot -1.
+ *     and slot -1.  (No call here reads slot, appends go by the table: it is for kernels of the caller's that write rows themselves.)
  *   An entry that a row of the batch lies in and that is no page of the pool: MOA_DEV_BAD_PAGE, whatever else is asked for.
  * moa_kv_release: entries behind the page of slot len[b] - 1 that name a page lose it (-1); the pages go back, so that the first of them by
  *   sequence and slot is the next one to be taken.  For a sequence that is done, set its len to 0 first; behind moa_kv_evict or a rejected draft
@@ -392,8 +393,10 @@ int32_t moa_kv_evict(const moa_kv_cache_t *cache, int32_t budget, int32_t recent
  *   passes n_pages (what would is dropped, MOA_DEV_BAD_PAGE), but a page that is in the list twice is handed out twice.  The whole table
  *   is read.
  * Calls on one list (or one table) are to be ordered by the caller, as by one stream.
- * Both are one launch of one workgroup, beyond 1024 sequences or 8192 rows three (beyond 16384 table entries, two).  Limits: B <= 2^20, T <=
- * 2^21, max_pages * page_size <= 2^30, n_pages * page_size and B * max_pages < 2^31 (MOA_ERR_SHAPE). */
+ * Reserving is one launch of one workgroup, and three beyond 1024 sequences or 8192 rows (where neither pos nor slot is asked for, only if the
+ * table has more than 16384 entries too); releasing is one, and two where several sequences have more than 16384 entries together, in time
+ * that grows with the table whatever goes back.  Limits: B <= 2^20, T <= 2^21, max_pages * page_size <= 2^30, n_pages * page_size and B *
+ * max_pages < 2^31 (MOA_ERR_SHAPE). */
 int32_t moa_kv_reserve(int32_t B, int32_t n_pages, int32_t page_size, int32_t max_pages, const int32_t *len /*[B]*/,
                        const int32_t *n_new /*[B]*/, const int32_t *seen /*[B] or NULL*/, int32_t *table, int32_t *free_pages,
                        int32_t *n_free, int32_t T, int32_t *tok_off, int32_t *n_got, int32_t *pos, int32_t *slot,
@@ -409,7 +412,8 @@ int32_t moa_kv_release(int32_t B, int32_t n_pages, int32_t page_size, int32_t ma
  *   pairs (c, c + rot_dim/2), c < rot_dim/2, are rotated by pos[t] * rope_theta^(-2c/rot_dim); dims from rot_dim on are y.
  * rot_dim = 0: the norm alone.  In single precision, the angle in double, rounded once.  q_out may be q with the same stride, k_out k; other
  * overlaps are not allowed.  0 heads: q (or k) is not looked at.  T = 0 is a no-op.  MOA_ERR_SHAPE: head_dim outside [1, 256], rot_dim odd or beyond
- * head_dim, strides smaller than the heads take, T > 2^23.  Squares are summed in single precision (elements up to 1e18). */
+ * head_dim, strides smaller than the heads take, T > 2^23.  Squares are summed in single precision (elements up to 1e18, and heads whose
+ * largest is at least 1e-18 where rms_eps is 0). */
 int32_t moa_qk_norm_rope(int32_t dtype, const void *q, int64_t q_stride, int32_t n_q_heads, const void *k, int64_t k_stride,
                          int32_t n_kv_heads, int64_t T, int32_t head_dim, const void *gq, const void *gk, float rms_eps,
                          const int32_t *pos /*[T]*/, float rope_theta, int32_t rot_dim, void *q_out, int64_t q_out_stride,
@@ -419,7 +423,7 @@ int32_t moa_qk_norm_rope(int32_t dtype, const void *q, int64_t q_stride, int32_t
  * (sign, 4 bits of exponent, 3 of mantissa; up to 448, NaN, no infinity); the MOA_KVQ_BLOCK rows r with the same r / MOA_KVQ_BLOCK of a page and KV head have one
  * scale for their keys and one for their values (the last block of a page may be shorter), and a code stands for code * scale.
  *   k, v             [n_pages, Hkv, page_size, dh] codes;
- *   k_scale, v_scale [n_pages, Hkv, ceil(page_size / MOA_KVQ_BLOCK)] fp32, positive and finite; of blocks that hold no row they do not matter;
+ *   k_scale, v_scale [n_pages, Hkv, ceil(page_size / MOA_KVQ_BLOCK)] fp32, positive, at most 2^127; of blocks that hold no row they do not matter;
  *   table, len       as in moa_kv_cache_t; `dtype` is that of the rows given, of queries and of results.
  * Limits as there, and M (or T) <= 2^24, times n_kv_heads <= 2^29, for the append, P_cap * head_dim < 2^31 for the read, B * n_q_heads * ceil(cap / 32)
  * <= 2^30 for the attention.  No accounts, and so no eviction by them.
@@ -437,7 +441,8 @@ int32_t moa_qk_norm_rope(int32_t dtype, const void *q, int64_t q_stride, int32_t
  *   that moa_tree_verify_attn reads (with P_cap); rows behind these, and of slots without a page (MOA_DEV_BAD_PAGE), are left as they were.  len[b] > P_cap:
  *   MOA_DEV_CACHE_FULL.  Exact wherever dtype holds the number.
  * moa_kvq_decode_attn is moa_decode_attn (without accounts) over such a cache: q, out [B, H*dh], one softmax over the len[b] slots; empty sequences, slots
- *   without a page, scores without a softmax and NaN as there.  Scores, weights and sums are fp32, scales are multiplied into them.  Workspace:
+ *   without a page, scores without a softmax and NaN as there.  Scores, weights and sums are fp32, scales are multiplied into them: precise for
+ *   query elements up to 1e33 (a score is summed before its scale comes in) and values of 1e-30 up to 1e38 / len[b].  Workspace:
  *   moa_kvq_decode_attn_workspace_bytes, 256-byte aligned. */
 #define MOA_KVQ_BLOCK 16
 typedef struct {
