@@ -442,8 +442,9 @@ int32_t moa_qk_norm_rope(int32_t dtype, const void *q, int64_t q_stride, int32_t
  *   MOA_DEV_CACHE_FULL.  Exact wherever dtype holds the number.
  * moa_kvq_decode_attn is moa_decode_attn (without accounts) over such a cache: q, out [B, H*dh], one softmax over the len[b] slots; empty sequences, slots
  *   without a page, scores without a softmax and NaN as there.  Scores, weights and sums are fp32, scales are multiplied into them: precise for
- *   query elements up to 1e33 (a score is summed before its scale comes in) and values of 1e-30 up to 1e38 / len[b].  Workspace:
- *   moa_kvq_decode_attn_workspace_bytes, 256-byte aligned. */
+ *   query elements up to 1e33 (a score is summed before its scale comes in) and values of 1e-30 up to 1e38 / len[b].  Beyond some hundred
+ *   sequences with capacities above 1024 its time goes with B * B, whatever their lengths.  Workspace: moa_kvq_decode_attn_workspace_bytes,
+ *   256-byte aligned. */
 #define MOA_KVQ_BLOCK 16
 typedef struct {
     int32_t dtype;                    /* MOA_F32 | MOA_BF16                                  */

@@ -218,7 +218,7 @@ __global__ __launch_bounds__(PT) void k_kv_reserve(ReserveArgs a)
 }
 
 // ---------------------------------------------------------------- in three: a wavefront a sequence counts what it wants and lacks, into tok_off and n_got
-// 64 prompts of 200 to 2048 tokens, 131072 rows of positions and slots: 3.0 + 3.7 + 5.0 us by trace (one workgroup for all but positions and slots 10.7
+// 64 prompts of 200 to 2048 tokens, 131072 rows of positions and slots: 2.7 + 3.7 + 4.8 us by trace (one workgroup for all but positions and slots 10.7
 // + 4.0, and 283 + 5 for 668 prompts in pages of one row, which now take 13).
 __device__ __forceinline__ int count_lacking(const ReserveArgs &a, int b, int len, int n)
 {
@@ -399,7 +399,8 @@ __global__ __launch_bounds__(PT) void k_kv_release(ReleaseArgs a)
 
 // The same by a launch that writes the list and one that takes the pages out of the table, where that is large: a workgroup has some of the
 // sequences, and counts for itself what goes back of the ones behind them, whose pages lie deeper: one compute unit's reads of most of the table
-// bound it.  805 sequences of 424 entries 121 us by one workgroup, 40 + 4 so; 128 of 500 9.6 + 4.1; 128 or 64 workgroups instead of 256: 42, 46.
+// bound it.  805 sequences of 425 entries 121 us by one workgroup, 40 + 4 so; 745 of 823 60 + 5; 128 of 501 9.7 + 4.1; 128 or 64 workgroups instead of 256
+// (805 of 425): 42, 46.
 constexpr int FEW_ENTRIES = 16384;
 __device__ __forceinline__ int first_gone(const ReleaseArgs &a, int b, bool report)
 {

@@ -193,7 +193,7 @@ __device__ __forceinline__ void encode_block(const KvqAppendArgs &a, int b, int 
 
 // ONE: a workgroup per sequence, which may then also move its length on.  Else gridDim.x of them per sequence, and a launch for the lengths.
 // What bounds it is the chain of a wavefront's loads (length, table and rows, scale), then its maximum over lanes: by trace 4.9 us for a token of
-// each of 64 sequences, 8.2 for up to seven nodes of each of 16, 11.9 + 3.9 for 5100 rows of four prompts (31 MB, 6 us by the copy rate;
+// each of 64 sequences in slabs, 8.2 for up to seven nodes of each of 16, 11.9 + 3.9 for 5100 rows of four prompts (31 MB, 6 us by the copy rate;
 // wavefronts wait 54 % of their time, vector units are busy 53 %).  A page of fewer than 16 rows is a block of its own: pages of one row, 41000
 // of them, 285 us (252 MB, 49 us by the copy rate).
 template <typename T, int VE, int IT, int THREADS, bool ONE>
@@ -233,7 +233,8 @@ __global__ __launch_bounds__(256) void k_kvq_append_len(KvqAppendArgs a)
 template <typename T, int VE, int IT>
 hipError_t launch_append(const KvqAppendArgs &a, hipStream_t st)
 {
-    // blocks that the rows of a sequence can be in
+    // blocks that the rows of a sequence can be in (of packed rows any number may be one's: a token for each of 64 sequences so takes two launches, 6.4 + 4.9
+    // us by events, where slabs take one, 7.1)
     const int64_t units = ((int64_t)a.M * (int)a.c.blocks.d / (int)a.c.c.page.d + 3) * a.c.c.Hkv * 2;
     // A workgroup's round of 16 blocks is about 2.5 us, the other launch 4; of a path's nodes few are accepted.
     const bool one = units <= (a.path ? 128 : 48);

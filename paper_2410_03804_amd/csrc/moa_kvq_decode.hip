@@ -173,7 +173,8 @@ typedef int i32x2 __attribute__((ext_vector_type(2)));
 // The list of all tiles of 32 keys of all pairs, dealt to the runs so that none has more than one more than another.  A pair takes up one more
 // place than it has tiles, since going on to it costs a wavefront up to a tile's time (its queries are waited for, its predecessor's result is
 // written): 64 ragged sequences up to 8192, some of which are short, 105 us without and 94 with.  (At least two or four places a run: one
-// sequence of 1084 5.6 us without, 7.5 and 10; of 27000 with 2 KV heads 6.9, 10.8 and 14.4.)
+// sequence of 1084 5.6 us without, 7.5 and 10; of 27000 with 2 KV heads 6.9, 10.8 and 14.4.)  Every run goes over the lengths of all sequences to find its
+// first, and so does every workgroup of the second launch: 8b heads, lengths up to 32, 64 sequences 5.5 + 4.6 us, 512 12.7 + 21.7, 4096 98.5 + 783.
 struct PlaceList {
     uint32_t total, log2;                // places; runs that they are dealt to: a.runs, or as many as leave none without
     static __device__ __forceinline__ uint32_t of(int len) { return tiles_of<WK>(len) + (len > 0); }
@@ -265,7 +266,8 @@ struct Walk {
 // before that.
 // HBM bounds it: 8 sequences of 32768 tokens, 64 heads, 538 MB, 90 us (6.0 TB/s over all of it, 5 us of which are its beginning; FETCH_SIZE is the
 // bytes of the codes and scales); vector units are busy 51 % of SIMD time, the matrix pipe 14 %, no LDS bank is waited for.  At 64 dims the
-// vector units bound it, whose work is per key and not per byte: 64 x 4000 tokens, 131 MB, 31 us.  (Four wavefronts a run, as moa_decode_attn: 64
+// vector units bound it, whose work is per key and not per byte: 64 x 4000 tokens, 131 MB, 31 us.  With more than 16 query heads a KV head, keys and
+// values are read once for every 16: 32 on one, 64 x 32000 tokens, 526 MB, 148 us.  (Four wavefronts a run, as moa_decode_attn: 64
 // ragged sequences up to 8192 125 us, now 95.)
 // ONE: a workgroup of four wavefronts per pair, a quarter of its tiles each, joined in LDS.  Else a wavefront per run, which is a workgroup: what
 // is fetched goes on from one pair to the next.
